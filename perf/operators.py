@@ -78,7 +78,7 @@ def draw(rng):
     if kind == "attend":
         Bz = rng.choice([1, 1, 2, 3, 7, 16, 32])
         n_q, Hq = rng.choice([1, 1, 1, 2, 5, 8]), Hkv * rng.choice([1, 2, 3, 4, 4, 8])
-        cap = 16 * _log_int(rng, 1, min(4112, 32768 // Bz, 32 * 900 * 32 * 128 // (Bz * n_q * Hq * d)))
+        cap = 16 * _log_int(rng, 1, min(4112, 32768 // Bz, 32 * 560 * 32 * 128 // (Bz * n_q * Hq * d)))
         return dict(kind=kind, Bz=Bz, cap=cap, n_q=n_q, Hq=Hq, Hkv=Hkv, d=d, group=group, dtype=dtype, ragged=rng.random() < 0.6, weights=rng.random() < 0.5)
     if kind == "evict":
         Bz = rng.choice([1, 2, 5, 8])
