@@ -346,6 +346,88 @@ int str_stack_prefill_host(str_ctx *ctx, const str_stack_desc *d, const void *hi
                            void *hidden_out_host, int32_t *idx_map_out_host, void *workspace,
                            size_t workspace_bytes, void *stream);
 
+/* ------------------------------------------------------------------------------------------
+ * Decoding against the reduced context: what a decoder that takes over the hand-off of str_stack_prefill_ex runs at the
+ * attention layers (a key/value cache held in 4 bits: rows in, rows out, attention, eviction) and at the Mamba layers
+ * (the recurrence one token at a time).  Same conventions.  The calls below may be made while another device is current
+ * (they use the context's and put the caller's back), and may be captured into a CUDA graph.
+ * ------------------------------------------------------------------------------------------ */
+
+/* 4-bit cache.  Per sequence and key head `cap` rows (a multiple of 16), head-major; a row holds d elements (64 or 128)
+ * of a key or value in groups of `group` (32, 64 or 128, at most d) consecutive elements, each group as 4-bit codes with
+ * a bf16 zero and a bf16 scale: element = zero + scale * code.
+ *   k_codes, v_codes    device [Bz,Hkv,cap,d/2] bytes, 16-byte aligned
+ *   k_scales, v_scales  device [Bz,Hkv,cap,d/group] 32-bit words, scale in the high half, zero in the low half, 16-byte aligned
+ *   pos                 device [Bz,cap] int32, original token id of each row, or NULL
+ *   weight              device [Bz,Hkv,cap] fp32, attention weight each row has drawn so far, or NULL
+ * Order of the codes in a row (ng = d/32): keys, element 32 g + 8 c + j (c < 4, j < 8) is nibble j of 32-bit word c*ng + g;
+ * values, element 32 g + 4 r + i (r < 8, i < 4) is nibble i of 16-bit word r*ng + g.  Nibble 0 is the lowest.
+ * Which rows of a sequence are in use is the caller's to keep (`row_start`, `lens` below): the calls read the counts they
+ * are given and change none.  Rows that are not in use are never read and may hold anything. */
+typedef struct {
+    int Bz, cap, Hkv, d, group;
+} str_kv4_shape;
+typedef struct {
+    void *k_codes, *v_codes, *k_scales, *v_scales;
+    int32_t *pos;
+    float *weight;
+} str_kv4_cache;
+
+/* Rows in.  Quantises k, v device [Bz,T_new,Hkv,d] dtype (post-RoPE keys; the layout of the hand-off) and stores token j
+ * of sequence b in cache row row_start[b] + j, for j < n_new[b] (n_new NULL: all T_new).  Per group: zero = the largest bf16
+ * value <= the minimum, scale = bf16((max - zero) / 15), code = clamp(rint((x - zero) / scale), 0, 15); a group with a NaN
+ * or an infinity (or a range beyond fp32) reads back as NaN.  Stored rows start with weight 0; with `positions`
+ * (device [Bz,T_new] int32, or NULL) their ids go to cache->pos.
+ * A row outside [0,cap) is not stored, and STR_ERR_INVALID_ARG is recorded in the status word.  The rows of one call must
+ * not overlap.  Errors: INVALID_ARG, UNSUPPORTED_SHAPE. */
+int str_kv4_append(str_ctx *ctx, const str_kv4_shape *s, int dtype, int T_new, const void *k, const void *v,
+                   const int32_t *positions, const int32_t *row_start, const int32_t *n_new, const str_kv4_cache *cache,
+                   void *stream);
+
+/* Rows back out, as str_attn_prefill_rows takes keys and values: k_out, v_out device [Bz,n_out,Hkv,d] dtype, token j of
+ * sequence b from cache row row_start[b] + j for j < n_rows[b] (NULL: all), zeros behind it.  zero + scale * code is formed
+ * in fp32 and rounded to dtype once.  Rows outside [0,cap) give zeros and are recorded as above. */
+int str_kv4_read(str_ctx *ctx, const str_kv4_shape *s, int dtype, int n_out, const int32_t *row_start, const int32_t *n_rows,
+                 const str_kv4_cache *cache, void *k_out, void *v_out, void *stream);
+
+/* Attention of the newest n_q tokens of each sequence over its cache, which already holds their own rows:
+ *   o[i] = sum_t softmax_t(q_i . k_t * softmax_scale) v_t over the rows t <= lens[b] - n_q + i,
+ * k, v the values the codes stand for.  q, o device [Bz,n_q,Hq,d] dtype; lens device [Bz] int32, rows in use.  A token with
+ * no row to see (an empty sequence; lens[b] < n_q) gives zeros.  A count outside [0,cap] is held to that range and recorded
+ * in the status word.  Meant for few tokens (every 16 query rows of a key head read the cache once); for long
+ * prompts use str_kv4_read and str_attn_prefill_rows.
+ *   weight_out  device [Bz,Hkv,cap] fp32 or NULL: weight_out[b,h,t] = cache->weight[b,h,t] + the softmax weights that the
+ *               n_q tokens' query heads of key head h put on row t, for t < lens[b]; other rows are left as they are.  May be
+ *               cache->weight itself.  Same bits on every run.
+ * Workspace: size from the query (want_weights nonzero when weight_out is given), 256-byte aligned. */
+size_t str_kv4_attn_workspace_size(const str_kv4_shape *s, int Hq, int n_q, int want_weights);
+int str_kv4_attn(str_ctx *ctx, const str_kv4_shape *s, int dtype, int Hq, int n_q, const void *q, const str_kv4_cache *cache,
+                 const int32_t *lens, float softmax_scale, void *o, float *weight_out, void *workspace,
+                 size_t workspace_bytes, void *stream);
+
+/* Eviction by accumulated attention weight.  Of the lens[b] rows of each sequence min(lens[b], keep) stay: the protected
+ * ones (the last n_recent, and with n_evictable, device [Bz] int32 or NULL, all rows from n_evictable[b] on; the newest
+ * `keep` of them when they are more), then those with the largest score_t = sum_h cache->weight[b,h,t] (summed in fp64 in
+ * head order, rounded to fp32; among equal scores the lower row; NaN counts as the lowest, infinities as +-FLT_MAX).
+ * Their codes, scales, weights and positions are copied bit for bit, in row order, to the rows 0 .. of `out`, a cache of
+ * the same Bz, Hkv, d, group and capacity cap_out >= keep; rows of `out` behind them are left as they were.
+ *   lens_out device [Bz] int32; kept_idx_out device [Bz,keep] int32, ascending, -1 behind the last.
+ * `out` shares no memory with `cache`.  out->weight and out->pos may be NULL (not copied).
+ * Errors: INVALID_ARG (keep > cap, keep > cap_out, n_recent > keep, shared buffers), UNSUPPORTED_SHAPE, WORKSPACE_TOO_SMALL. */
+size_t str_kv4_evict_workspace_size(const str_kv4_shape *s, int keep);
+int str_kv4_evict(str_ctx *ctx, const str_kv4_shape *s, const str_kv4_cache *cache, const int32_t *lens, int keep,
+                  int n_recent, const int32_t *n_evictable, int cap_out, const str_kv4_cache *out, int32_t *lens_out,
+                  int32_t *kept_idx_out, void *workspace, size_t workspace_bytes, void *stream);
+
+/* The recurrence of (1) for a few tokens from a state in memory, which stays in registers between the tokens:
+ *   S_t = exp(dt_t A_h) S_{t-1} + (dt_t x_t) b_t^T,   y_t = S_t c_t (+ D_h x_t);
+ * linear attention with a decay per head in its recurrent form (str_mamba2_prefill is the chunked one).  Tensors as in
+ * (1) with T tokens; state device [Bz,H,p,n] fp32 in, state_out the same out, which may be `state` itself.  Q is ignored.
+ * All arithmetic is fp32.  Meant for few tokens: time grows with T.  Errors: INVALID_ARG (T <= 0 too),
+ * UNSUPPORTED_SHAPE (n > 512). */
+int str_mamba2_step(str_ctx *ctx, const str_ssd_shape *s, const void *x, const float *dt, const float *A, const void *B,
+                    const void *C, const float *D, const float *state, void *y, float *state_out, void *stream);
+
 /* Optional device timing by kernel category.  While enabled, every leaf entry point records a CUDA
  * event pair around its launches on the caller's stream (str_profile_enable allocates events lazily on
  * first use).  str_profile_collect synchronises on the recorded events, adds the elapsed milliseconds

@@ -54,6 +54,14 @@ class StackDesc(ctypes.Structure):
                    ("ffn_dim", c_int)])
 
 
+class Kv4Shape(ctypes.Structure):
+    _fields_ = [(k, c_int) for k in ("Bz", "cap", "Hkv", "d", "group")]
+
+
+class Kv4CachePtrs(ctypes.Structure):
+    _fields_ = [(k, c_void_p) for k in ("k_codes", "v_codes", "k_scales", "v_scales", "pos", "weight")]
+
+
 class StackIO(ctypes.Structure):
     _fields_ = [("positions_in", c_void_p), ("idx_map_in", c_void_p), ("mamba_final_states", c_void_p),
                 ("attn_k_out", c_void_p), ("attn_v_out", c_void_p), ("attn_pos_out", c_void_p)]
@@ -76,7 +84,21 @@ EXPORTS = [
     "str_rope_split", "str_attn_prefill_workspace_size", "str_attn_prefill", "str_attn_prefill_rows",
     "str_stack_workspace_size", "str_stack_prefill", "str_stack_prefill_ex", "str_stack_host_workspace_size",
     "str_stack_prefill_host",
+    "str_kv4_append", "str_kv4_read", "str_kv4_attn_workspace_size", "str_kv4_attn", "str_kv4_evict_workspace_size", "str_kv4_evict",
+    "str_mamba2_step",
 ]
+
+# The decode calls run once per layer and token: declared argument types let ctypes convert plain integers itself.
+_I, _F, _Z, _P = c_int, c_float, c_size_t, c_void_p
+_ARGTYPES = {
+    "str_kv4_append": [_P, _P, _I, _I, _P, _P, _P, _P, _P, _P, _P],
+    "str_kv4_read": [_P, _P, _I, _I, _P, _P, _P, _P, _P, _P],
+    "str_kv4_attn_workspace_size": [_P, _I, _I, _I],
+    "str_kv4_attn": [_P, _P, _I, _I, _I, _P, _P, _P, _F, _P, _P, _P, _Z, _P],
+    "str_kv4_evict_workspace_size": [_P, _I],
+    "str_kv4_evict": [_P, _P, _P, _P, _I, _I, _P, _I, _P, _P, _P, _P, _Z, _P],
+    "str_mamba2_step": [_P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P],
+}
 
 _LIB = None
 
@@ -94,6 +116,8 @@ def lib():
         for name in EXPORTS:
             if name.endswith("_workspace_size"):
                 getattr(L, name).restype = c_size_t
+        for name, args in _ARGTYPES.items():
+            getattr(L, name).argtypes = args
         _LIB = L
     return _LIB
 
@@ -423,6 +447,151 @@ def str_attn_prefill_rows(ctx, q_rows, row_pos, k, v, softmax_scale):
                                        c_float(softmax_scale), _p(o), _p(ws), c_size_t(ws.numel()), _stream()),
            "str_attn_prefill_rows")
     return o
+
+
+def _arg(ctx, t, shape, dtype, what):
+    """Device address of an argument of a decode call, after the checks that the C side cannot make."""
+    if t.dtype != dtype:
+        raise TypeError("%s: expected %s, got %s" % (what, dtype, t.dtype))
+    if t.device.type != "cuda" or t.device.index != ctx.device:
+        raise ValueError("%s: expected a tensor on cuda:%d, got %s" % (what, ctx.device, t.device))
+    if tuple(t.shape) != shape:
+        raise ValueError("%s: expected shape %s, got %s" % (what, shape, tuple(t.shape)))
+    if not t.is_contiguous():
+        raise ValueError("%s: tensors must be contiguous" % what)
+    return t.data_ptr()
+
+
+def _ctx_stream(ctx):
+    """Address of the current stream of the context's device, whichever device is current."""
+    return torch._C._cuda_getCurrentRawStream(ctx.device)
+
+
+def _scratch(ctx, nbytes):
+    """Workspace of one call, from torch's stream-ordered pool: calls on several streams, and captured graphs, share none.
+    (None when the call needs none.)"""
+    return torch.empty(nbytes, dtype=torch.uint8, device="cuda:%d" % ctx.device) if nbytes else None
+
+
+class Kv4Cache:
+    """The tensors of a 4-bit key/value cache (layout in ``include/str.h``): codes [Bz,Hkv,cap,d/2] uint8, one int32 word
+    (bf16 scale, bf16 zero) per group [Bz,Hkv,cap,d/group], and optionally the original token ids ``pos`` [Bz,cap] int32 and
+    the accumulated attention ``weight`` [Bz,Hkv,cap] fp32.  The tensors stay the caller's; how many rows of each sequence
+    are in use is the caller's to keep."""
+
+    def __init__(self, k_codes, v_codes, k_scales, v_scales, pos=None, weight=None):
+        if k_codes.dim() != 4 or k_scales.dim() != 4 or k_scales.shape[3] == 0:
+            raise ValueError("Kv4Cache: codes [Bz,Hkv,cap,d/2] and scales [Bz,Hkv,cap,d/group] expected")
+        Bz, Hkv, cap, half = k_codes.shape
+        d, dev = 2 * half, k_codes.device
+        words = (Bz, Hkv, cap, k_scales.shape[3])
+        for name, t, shape, dtype in (("k_codes", k_codes, (Bz, Hkv, cap, half), torch.uint8), ("v_codes", v_codes, (Bz, Hkv, cap, half), torch.uint8),
+                                      ("k_scales", k_scales, words, torch.int32), ("v_scales", v_scales, words, torch.int32),
+                                      ("pos", pos, (Bz, cap), torch.int32), ("weight", weight, (Bz, Hkv, cap), torch.float32)):
+            if t is None and name in ("pos", "weight"):
+                continue
+            if tuple(t.shape) != shape or t.dtype != dtype or t.device != dev or not t.is_contiguous():
+                raise ValueError("Kv4Cache: %s must be a contiguous %s tensor %s on %s" % (name, dtype, shape, dev))
+        if dev.type != "cuda":
+            raise ValueError("Kv4Cache: the tensors must be on a CUDA device")
+        if d % words[3]:
+            raise ValueError("Kv4Cache: %d groups do not divide a row of %d elements" % (words[3], d))
+        self.k_codes, self.v_codes, self.k_scales, self.v_scales, self.pos, self.weight = k_codes, v_codes, k_scales, v_scales, pos, weight
+        self.Bz, self.Hkv, self.cap, self.d, self.group, self.device = Bz, Hkv, cap, d, d // words[3], dev
+        self._shape = Kv4Shape(Bz, cap, Hkv, d, self.group)
+        self._ptrs = Kv4CachePtrs(*(t.data_ptr() if t is not None else None for t in (k_codes, v_codes, k_scales, v_scales, pos, weight)))
+        self.shape_ref, self.ptrs_ref = ctypes.addressof(self._shape), ctypes.addressof(self._ptrs)
+
+    @classmethod
+    def empty(cls, ctx, Bz, cap, Hkv, d, group=32, pos=True, weight=True):
+        """A cache of `cap` unused rows per sequence on the context's device."""
+        dev = "cuda:%d" % ctx.device
+        rows = (Bz, Hkv, cap)
+        codes = [torch.zeros(rows + (d // 2,), dtype=torch.uint8, device=dev) for _ in range(2)]
+        words = [torch.zeros(rows + (d // group,), dtype=torch.int32, device=dev) for _ in range(2)]
+        return cls(*codes, *words, torch.zeros((Bz, cap), dtype=torch.int32, device=dev) if pos else None,
+                   torch.zeros(rows, dtype=torch.float32, device=dev) if weight else None)
+
+    def _on(self, ctx):
+        if self.device.index != ctx.device:
+            raise ValueError("Kv4Cache: the cache is on %s, the context on cuda:%d" % (self.device, ctx.device))
+
+
+def str_kv4_append(ctx, cache, k, v, row_start, positions=None, n_new=None):
+    """Quantises k, v [Bz,T,Hkv,d] and stores them in the rows row_start[b] .. of the cache (the first n_new[b] of them)."""
+    cache._on(ctx)
+    T = k.shape[1]
+    shape = (cache.Bz, T, cache.Hkv, cache.d)
+    dt = _dt(k)
+    _check(lib().str_kv4_append(ctx.handle, cache.shape_ref, dt, T, _arg(ctx, k, shape, k.dtype, "k"), _arg(ctx, v, shape, k.dtype, "v"),
+                                None if positions is None else _arg(ctx, positions, (cache.Bz, T), torch.int32, "positions"),
+                                _arg(ctx, row_start, (cache.Bz,), torch.int32, "row_start"),
+                                None if n_new is None else _arg(ctx, n_new, (cache.Bz,), torch.int32, "n_new"), cache.ptrs_ref, _ctx_stream(ctx)),
+           "str_kv4_append")
+
+
+def str_kv4_read(ctx, cache, row_start, T, dtype, n_rows=None):
+    """(k, v) [Bz,T,Hkv,d] of ``dtype`` from the rows row_start[b] .. of the cache; zeros behind the first n_rows[b]."""
+    cache._on(ctx)
+    k = torch.empty((cache.Bz, T, cache.Hkv, cache.d), dtype=dtype, device=cache.device)
+    v = torch.empty_like(k)
+    _check(lib().str_kv4_read(ctx.handle, cache.shape_ref, _dt(k), T, _arg(ctx, row_start, (cache.Bz,), torch.int32, "row_start"),
+                              None if n_rows is None else _arg(ctx, n_rows, (cache.Bz,), torch.int32, "n_rows"), cache.ptrs_ref,
+                              k.data_ptr(), v.data_ptr(), _ctx_stream(ctx)), "str_kv4_read")
+    return k, v
+
+
+def str_kv4_attn(ctx, cache, q, lens, softmax_scale, weight_out=None):
+    """Attention of the newest tokens q [Bz,n_q,Hq,d] over the cache, lens[b] rows of which are in use (the tokens' own
+    included).  With ``weight_out`` [Bz,Hkv,cap] fp32 (``cache.weight`` itself, or another tensor) it receives cache.weight plus
+    the attention weights drawn by each row in use."""
+    cache._on(ctx)
+    if q.dim() != 4:
+        raise ValueError("q: expected [Bz,n_q,Hq,d]")
+    n_q, Hq = q.shape[1], q.shape[2]
+    L = lib()
+    o = torch.empty_like(q)
+    ws = _scratch(ctx, L.str_kv4_attn_workspace_size(cache.shape_ref, Hq, n_q, 0 if weight_out is None else 1))
+    _check(L.str_kv4_attn(ctx.handle, cache.shape_ref, _dt(q), Hq, n_q, _arg(ctx, q, (cache.Bz, n_q, Hq, cache.d), q.dtype, "q"), cache.ptrs_ref,
+                          _arg(ctx, lens, (cache.Bz,), torch.int32, "lens"), softmax_scale, o.data_ptr(),
+                          None if weight_out is None else _arg(ctx, weight_out, (cache.Bz, cache.Hkv, cache.cap), torch.float32, "weight_out"),
+                          None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), _ctx_stream(ctx)), "str_kv4_attn")
+    return o
+
+
+def str_kv4_evict(ctx, cache, lens, keep, n_recent, out, n_evictable=None):
+    """Copies the `keep` rows of each sequence with the largest accumulated weight (and the protected newest ones) to the
+    cache ``out``.  Returns (lens_out [Bz], kept [Bz,keep]: the rows' old indices, ascending, -1 behind the last)."""
+    cache._on(ctx)
+    out._on(ctx)
+    if (out.Bz, out.Hkv, out.d, out.group) != (cache.Bz, cache.Hkv, cache.d, cache.group):
+        raise ValueError("str_kv4_evict: the two caches have different shapes")
+    L = lib()
+    n = torch.empty((cache.Bz,), dtype=torch.int32, device=cache.device)
+    kept = torch.empty((cache.Bz, max(keep, 0)), dtype=torch.int32, device=cache.device)
+    ws = _scratch(ctx, L.str_kv4_evict_workspace_size(cache.shape_ref, keep))
+    _check(L.str_kv4_evict(ctx.handle, cache.shape_ref, cache.ptrs_ref, _arg(ctx, lens, (cache.Bz,), torch.int32, "lens"), keep, n_recent,
+                           None if n_evictable is None else _arg(ctx, n_evictable, (cache.Bz,), torch.int32, "n_evictable"), out.cap, out.ptrs_ref,
+                           n.data_ptr(), kept.data_ptr(), None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(),
+                           _ctx_stream(ctx)), "str_kv4_evict")
+    return n, kept
+
+
+def str_mamba2_step(ctx, x, dt, A, B, C, state, D=None, state_out=None):
+    """A few tokens of the Mamba-2 recurrence from ``state`` [Bz,H,p,n] fp32; returns (y [Bz,T,H,p], state_out).  Without
+    ``state_out`` the state is updated in place."""
+    Bz, T, H, p = x.shape
+    G, n = B.shape[2], B.shape[3]
+    s = SsdShape(Bz, T, H, p, n, G, 0, _dt(x))
+    if state_out is None:
+        state_out = state
+    y = torch.empty_like(x)
+    f32, sshape = torch.float32, (Bz, H, p, n)
+    _check(lib().str_mamba2_step(ctx.handle, ctypes.addressof(s), _arg(ctx, x, (Bz, T, H, p), x.dtype, "x"), _arg(ctx, dt, (Bz, T, H), f32, "dt"),
+                                 _arg(ctx, A, (H,), f32, "A"), _arg(ctx, B, (Bz, T, G, n), x.dtype, "B"), _arg(ctx, C, (Bz, T, G, n), x.dtype, "C"),
+                                 None if D is None else _arg(ctx, D, (H,), f32, "D"), _arg(ctx, state, sshape, f32, "state"), y.data_ptr(),
+                                 _arg(ctx, state_out, sshape, f32, "state_out"), _ctx_stream(ctx)), "str_mamba2_step")
+    return y, state_out
 
 
 class Stack:

@@ -1,0 +1,52 @@
+// The 4-bit key/value cache: packed layout, argument checks and device helpers shared by its kernels.
+//
+// A row (one token, one key head, keys or values) of d elements is d / 2 bytes of codes and d / group 32-bit words.  The
+// word of a group holds (scale bf16) << 16 | (zero bf16); the group's elements stand for zero + scale * code.
+// With ng = d / 32, the codes of a row are stored in the order in which the attention kernel's lanes take them:
+//   keys    element 32 g + 8 c + j (c < 4, j < 8) is nibble j of the 32-bit word c * ng + g: the lane that holds columns
+//           2c, 2c+1, 2c+8, 2c+9 of a matrix fragment finds its words of all 32-element runs side by side;
+//   values  element 32 g + 4 r + i (r < 8, i < 4) is nibble i of the 16-bit word r * ng + g: the lane that holds row r of
+//           a fragment finds its quarter-words side by side.
+#pragma once
+#include "common.cuh"
+
+// Makes the context's device current for the launches of one call and puts the caller's back.
+struct StrDeviceScope {
+    int prev;
+    bool ok;
+    explicit StrDeviceScope(const str_ctx *ctx) : prev(-1), ok(true) {
+        int cur = 0;
+        if (cudaGetDevice(&cur) != cudaSuccess) { ok = false; return; }
+        if (cur != ctx->device) {
+            ok = cudaSetDevice(ctx->device) == cudaSuccess;
+            prev = cur;
+        }
+    }
+    ~StrDeviceScope() { if (prev >= 0) cudaSetDevice(prev); }
+};
+
+// STR_OK, or why the shape of a cache is refused.
+static inline int kv4_check_shape(const str_kv4_shape *s) {
+    if (!s || s->Bz <= 0 || s->cap <= 0 || s->Hkv <= 0 || s->d <= 0 || s->group <= 0) return STR_ERR_INVALID_ARG;
+    if ((s->d != 64 && s->d != 128) || (s->group != 32 && s->group != 64 && s->group != 128) || s->group > s->d) return STR_ERR_UNSUPPORTED_SHAPE;
+    if (s->cap % 16 != 0 || s->Bz > 65535 || s->Hkv > 65535 || s->cap > (1 << 30)) return STR_ERR_UNSUPPORTED_SHAPE;
+    return STR_OK;
+}
+static inline bool kv4_pointers_ok(const str_kv4_cache *c) {
+    if (!c || !c->k_codes || !c->v_codes || !c->k_scales || !c->v_scales) return false;
+    if (((uintptr_t)c->k_codes | (uintptr_t)c->v_codes | (uintptr_t)c->k_scales | (uintptr_t)c->v_scales) & 15) return false;
+    return (((uintptr_t)c->pos | (uintptr_t)c->weight) & 3) == 0;
+}
+
+__device__ __forceinline__ float kv4_scale(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+__device__ __forceinline__ float kv4_zero(uint32_t w) { return __uint_as_float(w << 16); }
+
+// Row count of a sequence as the kernels use it: what the caller says, held to [0, cap]; a value outside is recorded.
+__device__ __forceinline__ int kv4_len(const int32_t *lens, int b, int cap, int *status) {
+    const int n = lens[b];
+    if (n < 0 || n > cap) {
+        if (threadIdx.x == 0) atomicCAS(status, 0, STR_ERR_INVALID_ARG);
+        return n < 0 ? 0 : cap;
+    }
+    return n;
+}
