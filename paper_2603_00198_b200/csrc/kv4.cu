@@ -13,24 +13,6 @@ namespace {
 
 constexpr int KV4_THREADS = 256;
 
-template <typename T>
-__device__ __forceinline__ void load8(const T *p, float (&x)[8]);
-template <>
-__device__ __forceinline__ void load8(const __nv_bfloat16 *p, float (&x)[8]) {
-    const uint4 u = __ldg((const uint4 *)p);
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        x[2 * i] = __uint_as_float(w[i] << 16);
-        x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-    }
-}
-template <>
-__device__ __forceinline__ void load8(const float *p, float (&x)[8]) {
-    const float4 a = __ldg((const float4 *)p), b = __ldg((const float4 *)p + 1);
-    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-    x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-}
 __device__ __forceinline__ void store8(__nv_bfloat16 *p, const float (&x)[8]) {
     uint32_t w[4];
 #pragma unroll
@@ -116,8 +98,8 @@ kv4_append_kernel(int Bz, int cap, int Hkv, int T_new, const T *__restrict__ k, 
 #pragma unroll
         for (int j = 0; j < 8; ++j) xk[j] = xv[j] = 0.f;
         if (live) {
-            load8(k + r * D + 8 * l, xk);
-            load8(v + r * D + 8 * l, xv);
+            kv4_load8(k + r * D + 8 * l, xk);
+            kv4_load8(v + r * D + 8 * l, xv);
         }
         uint32_t wk, wv;
         const uint32_t ck = quantise8<GROUP>(xk, wk);
