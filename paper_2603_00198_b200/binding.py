@@ -155,6 +155,7 @@ class Context:
         if not torch.cuda.is_available():
             raise RuntimeError("libstr needs a CUDA device; there is no CPU path")
         self.device = device
+        self._dev = torch.device("cuda", device)
         torch.cuda.set_device(device)
         self._h = c_void_p()
         _check(lib().str_create(c_int(device), ctypes.byref(self._h)), "str_create")
@@ -451,11 +452,11 @@ def str_attn_prefill_rows(ctx, q_rows, row_pos, k, v, softmax_scale):
 
 def _arg(ctx, t, shape, dtype, what):
     """Device address of an argument of a decode call, after the checks that the C side cannot make."""
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError("%s: expected %s, got %s" % (what, dtype, t.dtype))
-    if t.device.type != "cuda" or t.device.index != ctx.device:
+    if t.get_device() != ctx.device:
         raise ValueError("%s: expected a tensor on cuda:%d, got %s" % (what, ctx.device, t.device))
-    if tuple(t.shape) != shape:
+    if t.shape != shape:
         raise ValueError("%s: expected shape %s, got %s" % (what, shape, tuple(t.shape)))
     if not t.is_contiguous():
         raise ValueError("%s: tensors must be contiguous" % what)
@@ -470,7 +471,7 @@ def _ctx_stream(ctx):
 def _scratch(ctx, nbytes):
     """Workspace of one call, from torch's stream-ordered pool: calls on several streams, and captured graphs, share none.
     (None when the call needs none.)"""
-    return torch.empty(nbytes, dtype=torch.uint8, device="cuda:%d" % ctx.device) if nbytes else None
+    return torch.empty(nbytes, dtype=torch.uint8, device=ctx._dev) if nbytes else None
 
 
 class Kv4Cache:
@@ -501,6 +502,7 @@ class Kv4Cache:
         self._shape = Kv4Shape(Bz, cap, Hkv, d, self.group)
         self._ptrs = Kv4CachePtrs(*(t.data_ptr() if t is not None else None for t in (k_codes, v_codes, k_scales, v_scales, pos, weight)))
         self.shape_ref, self.ptrs_ref = ctypes.addressof(self._shape), ctypes.addressof(self._ptrs)
+        self.index, self._ws_sizes = dev.index, {}
 
     @classmethod
     def empty(cls, ctx, Bz, cap, Hkv, d, group=32, pos=True, weight=True):
@@ -513,8 +515,16 @@ class Kv4Cache:
                    torch.zeros(rows, dtype=torch.float32, device=dev) if weight else None)
 
     def _on(self, ctx):
-        if self.device.index != ctx.device:
+        if self.index != ctx.device:
             raise ValueError("Kv4Cache: the cache is on %s, the context on cuda:%d" % (self.device, ctx.device))
+
+    def _ws_size(self, name, *args):
+        """Workspace size of a call on this cache's shape, asked of the library once."""
+        key = (name,) + args
+        n = self._ws_sizes.get(key)
+        if n is None:
+            n = self._ws_sizes[key] = getattr(lib(), name)(self.shape_ref, *args)
+        return n
 
 
 def str_kv4_append(ctx, cache, k, v, row_start, positions=None, n_new=None):
@@ -549,10 +559,9 @@ def str_kv4_attn(ctx, cache, q, lens, softmax_scale, weight_out=None):
     if q.dim() != 4:
         raise ValueError("q: expected [Bz,n_q,Hq,d]")
     n_q, Hq = q.shape[1], q.shape[2]
-    L = lib()
     o = torch.empty_like(q)
-    ws = _scratch(ctx, L.str_kv4_attn_workspace_size(cache.shape_ref, Hq, n_q, 0 if weight_out is None else 1))
-    _check(L.str_kv4_attn(ctx.handle, cache.shape_ref, _dt(q), Hq, n_q, _arg(ctx, q, (cache.Bz, n_q, Hq, cache.d), q.dtype, "q"), cache.ptrs_ref,
+    ws = _scratch(ctx, cache._ws_size("str_kv4_attn_workspace_size", Hq, n_q, 0 if weight_out is None else 1))
+    _check(lib().str_kv4_attn(ctx.handle, cache.shape_ref, _dt(q), Hq, n_q, _arg(ctx, q, (cache.Bz, n_q, Hq, cache.d), q.dtype, "q"), cache.ptrs_ref,
                           _arg(ctx, lens, (cache.Bz,), torch.int32, "lens"), softmax_scale, o.data_ptr(),
                           None if weight_out is None else _arg(ctx, weight_out, (cache.Bz, cache.Hkv, cache.cap), torch.float32, "weight_out"),
                           None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), _ctx_stream(ctx)), "str_kv4_attn")
@@ -566,11 +575,10 @@ def str_kv4_evict(ctx, cache, lens, keep, n_recent, out, n_evictable=None):
     out._on(ctx)
     if (out.Bz, out.Hkv, out.d, out.group) != (cache.Bz, cache.Hkv, cache.d, cache.group):
         raise ValueError("str_kv4_evict: the two caches have different shapes")
-    L = lib()
     n = torch.empty((cache.Bz,), dtype=torch.int32, device=cache.device)
     kept = torch.empty((cache.Bz, max(keep, 0)), dtype=torch.int32, device=cache.device)
-    ws = _scratch(ctx, L.str_kv4_evict_workspace_size(cache.shape_ref, keep))
-    _check(L.str_kv4_evict(ctx.handle, cache.shape_ref, cache.ptrs_ref, _arg(ctx, lens, (cache.Bz,), torch.int32, "lens"), keep, n_recent,
+    ws = _scratch(ctx, cache._ws_size("str_kv4_evict_workspace_size", keep))
+    _check(lib().str_kv4_evict(ctx.handle, cache.shape_ref, cache.ptrs_ref, _arg(ctx, lens, (cache.Bz,), torch.int32, "lens"), keep, n_recent,
                            None if n_evictable is None else _arg(ctx, n_evictable, (cache.Bz,), torch.int32, "n_evictable"), out.cap, out.ptrs_ref,
                            n.data_ptr(), kept.data_ptr(), None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(),
                            _ctx_stream(ctx)), "str_kv4_evict")

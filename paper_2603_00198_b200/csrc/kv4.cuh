@@ -41,21 +41,26 @@ static inline bool kv4_pointers_ok(const str_kv4_cache *c) {
 __device__ __forceinline__ float kv4_scale(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 __device__ __forceinline__ float kv4_zero(uint32_t w) { return __uint_as_float(w << 16); }
 
-// Eight consecutive elements, widened.
-__device__ __forceinline__ void kv4_load8(const __nv_bfloat16 *p, float (&x)[8]) {
-    const uint4 u = __ldg((const uint4 *)p);
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+// Eight consecutive elements as they are stored, and widened.
+template <typename T> struct Kv4Raw8;
+template <> struct Kv4Raw8<__nv_bfloat16> { uint4 u; };
+template <> struct Kv4Raw8<float> { float4 a, b; };
+__device__ __forceinline__ Kv4Raw8<__nv_bfloat16> kv4_raw8(const __nv_bfloat16 *p) { return {__ldg((const uint4 *)p)}; }
+__device__ __forceinline__ Kv4Raw8<float> kv4_raw8(const float *p) { return {__ldg((const float4 *)p), __ldg((const float4 *)p + 1)}; }
+__device__ __forceinline__ void kv4_widen8(const Kv4Raw8<__nv_bfloat16> &r, float (&x)[8]) {
+    const uint32_t w[4] = {r.u.x, r.u.y, r.u.z, r.u.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         x[2 * i] = __uint_as_float(w[i] << 16);
         x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
     }
 }
-__device__ __forceinline__ void kv4_load8(const float *p, float (&x)[8]) {
-    const float4 a = __ldg((const float4 *)p), b = __ldg((const float4 *)p + 1);
-    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-    x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+__device__ __forceinline__ void kv4_widen8(const Kv4Raw8<float> &r, float (&x)[8]) {
+    x[0] = r.a.x; x[1] = r.a.y; x[2] = r.a.z; x[3] = r.a.w;
+    x[4] = r.b.x; x[5] = r.b.y; x[6] = r.b.z; x[7] = r.b.w;
 }
+template <typename T>
+__device__ __forceinline__ void kv4_load8(const T *p, float (&x)[8]) { kv4_widen8(kv4_raw8(p), x); }
 
 // Row count of a sequence as the kernels use it: what the caller says, held to [0, cap]; a value outside is recorded.
 __device__ __forceinline__ int kv4_len(const int32_t *lens, int b, int cap, int *status) {

@@ -29,6 +29,7 @@
 #pragma once
 #include <cuda_fp16.h>
 
+#include <atomic>
 #include <type_traits>
 
 #include "kv4.cuh"
@@ -784,8 +785,13 @@ int launch_attn(str_ctx *ctx, const AttnArgs &a, int G, const float *weight, flo
     const size_t smem = (size_t)AT_WARPS * AT_STAGES * Stage<D, GROUP>::BYTES;
     static_assert(AT_STAGES * Stage<D, GROUP>::BYTES >= COLS * D * 4, "a warp's output has to fit its ring");
     if (smem > (size_t)ctx->max_smem_optin) return STR_ERR_UNSUPPORTED_SHAPE;
-    // The attribute belongs to the device's copy of the kernel; every call sets the same value.
-    STR_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    // The attribute belongs to the device's copy of the kernel: set once per device and kernel (twice by two threads does no harm).
+    static std::atomic<uint64_t> opted[2];
+    const uint64_t bit = ctx->device < 64 ? 1ull << ctx->device : 0;
+    if (!(opted[a.scores != nullptr].load(std::memory_order_acquire) & bit)) {
+        STR_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+        opted[a.scores != nullptr].fetch_or(bit, std::memory_order_release);
+    }
     kernel<<<G, AT_WARPS * 32, smem, st>>>(a);
     int rc = str_launch_ok(ctx);
     if (rc != STR_OK) return rc;
