@@ -356,11 +356,11 @@ int str_stack_prefill_host(str_ctx *ctx, const str_stack_desc *d, const void *hi
 /* 4-bit cache.  Per sequence and key head `cap` rows (a multiple of 16), head-major; a row holds d elements (64 or 128)
  * of a key or value in groups of `group` (32, 64 or 128, at most d) consecutive elements, each group as 4-bit codes with
  * a bf16 zero and a bf16 scale: element = zero + scale * code.
- *   k_codes, v_codes    device [Bz,Hkv,cap,d/2] bytes, 16-byte aligned
- *   k_scales, v_scales  device [Bz,Hkv,cap,d/group] 32-bit words, scale in the high half, zero in the low half, 16-byte aligned
+ *   k_codes, v_codes    device [Bz,Hkv,cap,d/2] bytes
+ *   k_scales, v_scales  device [Bz,Hkv,cap,d/group] 32-bit words, scale (>= 0) in the high half, zero in the low half
  *   pos                 device [Bz,cap] int32, original token id of each row, or NULL
  *   weight              device [Bz,Hkv,cap] fp32, attention weight each row has drawn so far, or NULL
- * Order of the codes in a row (ng = d/32): keys, element 32 g + 8 c + j (c < 4, j < 8) is nibble j of 32-bit word c*ng + g;
+ * all 16-byte aligned.  Order of the codes in a row (ng = d/32): keys, element 32 g + 8 c + j (c < 4, j < 8) is nibble j of 32-bit word c*ng + g;
  * values, element 32 g + 4 r + i (r < 8, i < 4) is nibble i of 16-bit word r*ng + g.  Nibble 0 is the lowest.
  * Which rows of a sequence are in use is the caller's to keep (`row_start`, `lens` below): the calls read the counts they
  * are given and change none.  Rows that are not in use are never read and may hold anything. */

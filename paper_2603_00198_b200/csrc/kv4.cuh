@@ -34,8 +34,8 @@ static inline int kv4_check_shape(const str_kv4_shape *s) {
 }
 static inline bool kv4_pointers_ok(const str_kv4_cache *c) {
     if (!c || !c->k_codes || !c->v_codes || !c->k_scales || !c->v_scales) return false;
-    if (((uintptr_t)c->k_codes | (uintptr_t)c->v_codes | (uintptr_t)c->k_scales | (uintptr_t)c->v_scales) & 15) return false;
-    return (((uintptr_t)c->pos | (uintptr_t)c->weight) & 3) == 0;
+    return (((uintptr_t)c->k_codes | (uintptr_t)c->v_codes | (uintptr_t)c->k_scales | (uintptr_t)c->v_scales | (uintptr_t)c->pos |
+             (uintptr_t)c->weight) & 15) == 0;
 }
 
 __device__ __forceinline__ float kv4_scale(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }

@@ -155,7 +155,13 @@ def test_cache_arguments_are_refused(libstr):
     ev = lambda cache=c, out=c2, keep=16, recent=0, cap_out=16, lens=p, lens_out=p + 64, kept=p, ws=p, nb=big: libstr.str_kv4_evict(  # noqa: E731
         a(ctx), a(s), a(cache), lens, keep, recent, None, cap_out, a(out), lens_out, kept, ws, nb, None)
     assert ev(keep=65, cap_out=80) == -1 and ev(keep=17) == -1 and ev(recent=17) == -1 and ev(keep=-1) == -1 and ev(recent=-1) == -1
-    assert ev(cap_out=20) == -2 and ev(nb=16) == -3 and ev(ws=None) == -1 and ev(kept=None) == -1 and ev(lens_out=p) == -1
+    assert ev(cap_out=20) == -2 and ev(kept=None) == -1 and ev(lens_out=p) == -1
+    assert ev(cache=_cache_ptrs(weight=131076)) == -1                                                       # alignment
+    assert libstr.str_kv4_evict_workspace_size(a(s), 16) == 0
+    s.cap = 200000                                                                                          # a row over many CTAs: needs a workspace
+    need = libstr.str_kv4_evict_workspace_size(a(s), 16)
+    assert need >= 200000 * 4 and ev(nb=need - 1) == -3 and ev(ws=None) == -1 and ev(ws=p + 128) == -1
+    s.cap = 64
     assert ev(cache=_cache_ptrs(weight=None)) == -1 and ev(cache=_cache_ptrs(pos=None)) == -1
     for shared in ("k_codes", "v_codes", "k_scales", "v_scales", "pos", "weight"):
         assert ev(cache=_cache_ptrs(**{shared: getattr(c2, shared)})) == -1
