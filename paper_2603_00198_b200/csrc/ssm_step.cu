@@ -6,11 +6,16 @@
 // the tokens go by.  A row of the state (one of p) lies across a group of lanes, each holding vectors of VEC consecutive
 // columns, so that both the loads and the sum over n in y are along the lanes; a warp works on RPT rows per group at once,
 // all their loads in flight together.  All arithmetic is fp32; y is rounded to the storage type once.
+//
+// Bound by memory.  64 sequences of the 8B-class layer (537 MB of state in and out): 83.5 us = 6.46 TB/s, 0.99 of the measured
+// copy bandwidth.  Streaming loads and stores (neither alone does it) and blocks of 128 threads are what it takes: 99.8 us with 256
+// threads and plain accesses, 93.5 with 128 threads.  From 1 to 32 sequences they are never slower, with the states in L2 or
+// not (one sequence 3.2 us either way).
 #include "kv4.cuh"
 
 namespace {
 
-constexpr int STEP_THREADS = 256;
+constexpr int STEP_THREADS = 128;
 
 template <int VEC> struct Vec;
 template <> struct Vec<4> { typedef float4 type; };
@@ -36,7 +41,7 @@ mamba2_step_kernel(int T_new, int H, int p, int n, int G, const T *__restrict__ 
         for (int v = 0; v < NV; ++v) {
             const int col = (v * LPR + l) * VEC;
             V val = {};
-            if (row0 + r < p && col < n) val = *(const V *)(state + sbase + (long long)(row0 + r) * n + col);
+            if (row0 + r < p && col < n) val = __ldcs((const V *)(state + sbase + (long long)(row0 + r) * n + col));
             *(V *)S[r][v] = val;
         }
     const float Ah = A[h], Dh = Dskip ? Dskip[h] : 0.f;
@@ -80,7 +85,7 @@ mamba2_step_kernel(int T_new, int H, int p, int n, int G, const T *__restrict__ 
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int col = (v * LPR + l) * VEC;
-            if (row0 + r < p && col < n) *(V *)(state_out + sbase + (long long)(row0 + r) * n + col) = *(V *)S[r][v];
+            if (row0 + r < p && col < n) __stcs((V *)(state_out + sbase + (long long)(row0 + r) * n + col), *(V *)S[r][v]);
         }
 }
 
