@@ -399,7 +399,10 @@ int str_kv4_read(str_ctx *ctx, const str_kv4_shape *s, int dtype, int n_out, con
  *   weight_out  device [Bz,Hkv,cap] fp32 or NULL: weight_out[b,h,t] = cache->weight[b,h,t] + the softmax weights that the
  *               n_q tokens' query heads of key head h put on row t, for t < lens[b]; other rows are left as they are.  May be
  *               cache->weight itself.  Same bits on every run.
- * Workspace: size from the query (want_weights nonzero when weight_out is given), 256-byte aligned. */
+ * q and k may be of any size up to 1e30 (their products are formed relative to the largest element of a query row); q 16-byte
+ * aligned, at most 4096 query rows (tokens x heads) per key head.
+ * Workspace: size from the query (want_weights nonzero when weight_out is given: the scores, 4 bytes per query row and
+ * cache row), 256-byte aligned; calls that may run at the same time, two captured graphs among them, need their own. */
 size_t str_kv4_attn_workspace_size(const str_kv4_shape *s, int Hq, int n_q, int want_weights);
 int str_kv4_attn(str_ctx *ctx, const str_kv4_shape *s, int dtype, int Hq, int n_q, const void *q, const str_kv4_cache *cache,
                  const int32_t *lens, float softmax_scale, void *o, float *weight_out, void *workspace,

@@ -259,6 +259,41 @@ def test_attention_passes_nan_and_infinity_on(ctx):
     ctx.check_status()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("Hq,Hkv,d,group", [(2, 2, 64, 64), (4, 1, 128, 32), (8, 1, 128, 128), (24, 2, 64, 32)])
+def test_attention_rows_that_only_later_tokens_see_do_not_reach_the_earlier_ones(ctx, dtype, Hq, Hkv, d, group):
+    """NaN in the keys or values of the newest rows: a token that does not see such a row is as if it were not there."""
+    g = np.random.default_rng([Hq, d])
+    n_q, lens = 4, [70, 67, 64, 5]
+    k, v = _rows(g, (4, Hkv, 80, d), "f32", True), _rows(g, (4, Hkv, 80, d), "f32", False)
+    bad_k, bad_v = k.copy(), v.copy()
+    bad_k[0, 0, 69, 0], bad_v[1, Hkv - 1, 66, d - 1], bad_v[2, 0, 62, 1], bad_k[3, 0, 4, 3] = np.nan, np.inf, np.nan, -np.inf
+    q = inputs.to_grid(g.standard_normal((4, n_q, Hq, d)), dtype)
+    f, bad = Filled(g, lens, 80, Hkv, d, group, k=k, v=v), Filled(g, lens, 80, Hkv, d, group, k=bad_k, v=bad_v)
+    got = binding.str_kv4_attn(ctx, bad.cache, dev(q, dtype), _i32(lens), d ** -0.5).float().cpu().numpy()
+    good = binding.str_kv4_attn(ctx, f.cache, dev(q, dtype), _i32(lens), d ** -0.5).float().cpu().numpy()
+    R = Hq // Hkv
+    want = np.zeros(got.shape, dtype=bool)
+    want[0, 3, :R] = True                                           # row 69 of 70: the last token only, all elements
+    want[1, 3, (Hkv - 1) * R:, d - group:] = True                   # row 66 of 67, one group
+    want[2, 2:, :R, :group] = True                                  # row 62 of 64: the last two tokens
+    want[3, 3, :R] = True
+    assert np.array_equal(np.isnan(got), want)
+    assert np.array_equal(got[~want], good[~want])
+    ctx.check_status()
+
+
+@pytest.mark.parametrize("Bz,weights", [(33, True), (100, False), (257, True)])
+def test_attention_of_many_sequences(ctx, Bz, weights):
+    """More sequences than a warp has lanes, many of them empty, some long: the line of work is cut at odd places."""
+    g = np.random.default_rng(Bz)
+    lens = [int(n) for n in np.where(g.random(Bz) < 0.4, 0, g.integers(1, 400, Bz))]
+    lens[0], lens[-1], lens[Bz // 2] = 0, 3, 2000
+    f = Filled(g, lens, 2000, 1, 64, 32)
+    q = inputs.to_grid(g.standard_normal((Bz, 1, 4, 64)), "bf16")
+    check_attention(ctx, f, q, "bf16", 0.125, weights)
+
+
 def test_attention_weights_in_place_and_the_same_bits_every_time(ctx):
     g = np.random.default_rng(12)
     f = Filled(g, [2000, 0, 517], 2016, 4, 128, 32)
