@@ -5,10 +5,11 @@
 //   q . k   = sum_g ( scale_g (q_g . c_g) + zero_g sum(q_g) )
 //   o_e     = sum_t (p_t scale_t,g) (c_t,e - 8) + sum_t p_t (zero_t,g + 8 scale_t,g)      (g the group of element e)
 // and q . k likewise with c - 8: the codes are centred so that neither sum is the small difference of two large ones.
-// Both code products run on the matrix instruction, on codes turned into fp16 exactly: a nibble put into the mantissa of 1024
-// (one AND-OR) less 1032 (one packed add) is c - 8, or 16 (c - 8) for the nibble four bits further up; the powers of two go into q
-// and into the output.  (The nibble as it stands would be the subnormal c 2^-24 for nothing, but the matrix instruction lines
-// products up by the nominal exponent and then drops the last six to ten bits: measured, 5e-6 instead of 4e-7 of error.)
+// Both code products run on the matrix instruction, on codes turned into fp16 exactly: a byte put into the mantissa of 1024, its
+// low nibble taken off again as c - 8 and what is left is 16 (c - 8) of the high one (codes2: eight instructions for eight codes);
+// the powers of two go into q and into the output.  (The nibble as it stands would be the subnormal c 2^-24 for half of that, but the
+// matrix instruction lines products up by the nominal exponent and then drops the last six to ten bits: measured, 5e-6 instead
+// of 4e-7 of error.)
 // The other factor is fp16: q scaled by a power of two to just below 2^15 (bf16 values fit exactly; fp32 storage takes two
 // fp16 terms, 22 bits), and p scale 2^(11-E) with E the largest exponent of a value scale so far (one rounding of 2^-11 for
 // bf16 storage, two terms for fp32 storage).
@@ -72,16 +73,24 @@ __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
     const __half2 h = __floats2half2_rn(lo, hi);
     return *(const uint32_t *)&h;
 }
-// Two of a word's codes as fp16, less 8: the nibble goes into the mantissa of 1024 (ulp 1), which then is taken off again.
-// LOW: bits 0-3 of both halves, c - 8; otherwise bits 4-7, 16 (c - 8).  Exact.
-// `magic` is 0x64006400 in a register that the compiler does not see through: mask and bias then are one instruction.
+// Bytes 0, 2 (LOW) or 1, 3 of a word as fp16: 1024 + byte, the byte put into the mantissa.  `magic` is 0x64006400 in a register
+// that the compiler does not see through: mask and constant then are one instruction.
 template <bool LOW>
-__device__ __forceinline__ uint32_t codes2(uint32_t w, uint32_t magic) {
+__device__ __forceinline__ uint32_t bytes2(uint32_t w, uint32_t magic) {
+    if constexpr (!LOW) return __byte_perm(w, magic, 0x7351);
     uint32_t v;
-    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(v) : "r"(w), "n"(LOW ? 0x000F000F : 0x00F000F0), "r"(magic));   // (w & mask) | magic
-    const uint32_t k = LOW ? 0xE408E408u : 0xE480E480u;                         // -1032, -1152
-    const __half2 d = __hadd2(*(const __half2 *)&v, *(const __half2 *)&k);
-    return *(const uint32_t *)&d;
+    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(v) : "r"(w), "n"(0x00FF00FF), "r"(magic));        // (w & mask) | magic
+    return v;
+}
+// The two codes in each byte, c0 + 16 c1: with l = 1152 + c0 (`magic2` is 0x64806480), l - 1160 = c0 - 8 and
+// (1024 + byte) - l = 16 (c1 - 8), exactly.
+__device__ __forceinline__ void codes2(uint32_t byte, uint32_t magic2, uint32_t &lo, uint32_t &hi) {
+    uint32_t l;
+    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(l) : "r"(byte), "n"(0x000F000F), "r"(magic2));
+    const uint32_t k = 0xE488E488u;                                             // -1160
+    const __half2 a = __hadd2(*(const __half2 *)&l, *(const __half2 *)&k), b = __hsub2(*(const __half2 *)&byte, *(const __half2 *)&l);
+    lo = *(const uint32_t *)&a;
+    hi = *(const uint32_t *)&b;
 }
 // x0, x1 as one (TERMS 1) or the sum of two (TERMS 2) fp16 pairs.
 template <int TERMS>
@@ -214,8 +223,9 @@ kv4_attn_kernel(const AttnArgs a) {
     long long at = begin;
     const int tr = r ^ ((r >> 1) & 1), va = 2 * c + (c & 1), vb = 2 * c + 1 - (c & 1);    // tokens of slots r, 2c, 2c+1
     int slot = 0;
-    uint32_t phase = 0, magic;
+    uint32_t phase = 0, magic, magic2;
     asm volatile("mov.b32 %0, 0x64006400;" : "=r"(magic));
+    asm volatile("mov.b32 %0, 0x64806480;" : "=r"(magic2));
 
     while (at < end) {
         while (at >= b_end) {
@@ -393,9 +403,11 @@ kv4_attn_kernel(const AttnArgs a) {
 #pragma unroll
                     for (int k = 0; k < PACK * RPG; ++k) {                      // the runs of group g (and of its partner in the other half)
                         const int q = g * RPG + k % RPG + (k / RPG) * NGP * RPG;
-                        const uint32_t ha = ka[q] >> 8, hb = kb[q] >> 8;
-                        const uint32_t a0 = codes2<true>(ka[q], magic), a1 = codes2<true>(kb[q], magic), a2 = codes2<false>(ka[q], magic), a3 = codes2<false>(kb[q], magic);
-                        const uint32_t b0 = codes2<true>(ha, magic), b1 = codes2<true>(hb, magic), b2 = codes2<false>(ha, magic), b3 = codes2<false>(hb, magic);
+                        uint32_t a0, a1, a2, a3, b0, b1, b2, b3;
+                        codes2(bytes2<true>(ka[q], magic), magic2, a0, a2);
+                        codes2(bytes2<true>(kb[q], magic), magic2, a1, a3);
+                        codes2(bytes2<false>(ka[q], magic), magic2, b0, b2);
+                        codes2(bytes2<false>(kb[q], magic), magic2, b1, b3);
 #pragma unroll
                         for (int j = 0; j < NT; ++j)
 #pragma unroll
@@ -533,9 +545,11 @@ kv4_attn_kernel(const AttnArgs a) {
                         const int q = g * RPG + k % RPG + (k / RPG) * NGP * RPG;
                         const uint32_t sel = q & 1 ? 0x7632u : 0x5410u;
                         const uint32_t xl = __byte_perm(v0[q / 2], v1[q / 2], sel), xh = __byte_perm(v2[q / 2], v3[q / 2], sel);
-                        const uint32_t yl = xl >> 8, yh = xh >> 8;
-                        const uint32_t a0 = codes2<true>(xl, magic), a1 = codes2<false>(xl, magic), a2 = codes2<true>(xh, magic), a3 = codes2<false>(xh, magic);
-                        const uint32_t b0 = codes2<true>(yl, magic), b1 = codes2<false>(yl, magic), b2 = codes2<true>(yh, magic), b3 = codes2<false>(yh, magic);
+                        uint32_t a0, a1, a2, a3, b0, b1, b2, b3;
+                        codes2(bytes2<true>(xl, magic), magic2, a0, a1);
+                        codes2(bytes2<true>(xh, magic), magic2, a2, a3);
+                        codes2(bytes2<false>(xl, magic), magic2, b0, b1);
+                        codes2(bytes2<false>(xh, magic), magic2, b2, b3);
 #pragma unroll
                         for (int j = 0; j < NT; ++j) {
                             if constexpr (TERMS == 1) {
