@@ -41,6 +41,7 @@ namespace kv4_attn {
 constexpr int AT_TILE = 32;              // rows of a warp's tile
 constexpr int AT_STAGES = 2;             // tiles in flight per warp
 constexpr int WT_THREADS = 256;
+constexpr int JOIN_BATCH = 5;            // parts a warp of the join loads at once: 8 x 5 cover one of 8 key heads spread over the card
 constexpr float M_START = -3.0e38f;      // running maximum before the first row: finite, so that differences stay defined
 constexpr float M_SLACK = 3.0f;          // the running maximum moves only when a score beats it by this (log2): p <= 2^3
 
@@ -677,34 +678,56 @@ kv4_join_kernel(const AttnArgs a, int cols, int G, int NW, const float *weight, 
     __shared__ long long before, total;
     __shared__ float4 sums[WT_THREADS / 32][32];
     __shared__ float2 runs[WT_THREADS / 32][32];
+    const int len = clamp_len(a.lens[b], a.cap), places = unit_places(len), tiles = max(places - AT_UNIT_COST, 0);
+    if (blockIdx.x * 128 >= C * D && (!weight_out || blockIdx.x * (4 * WT_THREADS) >= len)) return;   // nothing for this block
     if (tid < 32) {
-        const long long t0 = places_before(a.lens, b, a.cap, tid), t1 = places_before(a.lens, a.Bz, a.cap, tid);
+        long long t0 = 0, t1 = 0;                                               // places before sequence b, and in all
+        for (int base = 0; base < a.Bz; base += 32) {
+            const int n = base + tid < a.Bz ? unit_places(clamp_len(a.lens[base + tid], a.cap)) : 0;
+            t0 += __reduce_add_sync(0xffffffffu, base + tid < b ? n : 0);
+            t1 += __reduce_add_sync(0xffffffffu, n);
+        }
         if (tid == 0) { before = t0 * HC; total = t1 * HC; }
     }
     __syncthreads();
-    const int len = clamp_len(a.lens[b], a.cap), places = unit_places(len), tiles = max(places - AT_UNIT_COST, 0);
     const int per = max(places_per_cta(total, G, NW), 1);
-    asm volatile("griddepcontrol.wait;" ::: "memory");                          // all that the first kernel wrote is there
     const int lane = tid & 31, warp = tid >> 5;
-    // The output, 128 elements at a time: warp w takes the parts w, w + 8, .. with a running maximum, then the warps are joined
-    // in order.
-    for (int i0 = blockIdx.x * 128; i0 < C * D; i0 += gridDim.x * 128) {
-        const int i = i0 + 4 * lane, col = i / D, block = col / cols;
-        const long long u = before + (long long)(h * a.chunks + block) * places + AT_UNIT_COST;        // the unit's first tile
-        const long long c0 = tiles ? divide(u, per) : 0, c1 = tiles ? divide(u + tiles - 1, per) : -1;
+    // The output, 128 elements at a time: warp w takes the parts w, w + 8, .. with a running maximum, JOIN_BATCH of them in flight,
+    // then the warps are joined in order.  Where the first elements' parts lie is worked out before the wait.
+    int i0 = blockIdx.x * 128, i, col, block;
+    long long u, c0, c1;
+    auto locate = [&]() {
+        i = i0 + 4 * lane;
+        col = i / D;
+        block = col / cols;
+        u = before + (long long)(h * a.chunks + block) * places + AT_UNIT_COST;                        // the unit's first tile
+        c0 = tiles ? divide(u, per) : 0;
+        c1 = tiles ? divide(u + tiles - 1, per) : -1;
+    };
+    locate();
+    asm volatile("griddepcontrol.wait;" ::: "memory");                          // all that the first kernel wrote is there
+    while (i0 < C * D) {
         float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
         float2 run = make_float2(M_START, 0.f);
         const bool mine = i < C * D && c0 != c1;                                // else finished by the one CTA that had it
-        if (mine) {
-#pragma unroll 4
-            for (long long k = c0 + warp; k <= c1; k += WT_THREADS / 32) {
+        for (long long k0 = c0 + warp; mine && k0 <= c1; k0 += JOIN_BATCH * (WT_THREADS / 32)) {
+            float2 v[JOIN_BATCH];
+            float4 w[JOIN_BATCH];
+#pragma unroll
+            for (int n = 0; n < JOIN_BATCH; ++n) {
+                const long long k = k0 + n * (WT_THREADS / 32);
+                if (k > c1) continue;
                 const long long place = (2 * k + (k * per < u ? 1 : 0)) * cols + col - block * cols;
-                const float2 v = a.part_ml[place];
-                const float4 w = *(const float4 *)(a.part + place * D + i % D);
-                const float top = fmaxf(run.x, v.x), f = ex2(run.x - top), g = ex2(v.x - top);
-                run = make_float2(top, fmaf(run.y, f, v.y * g));
-                sum.x = fmaf(sum.x, f, w.x * g); sum.y = fmaf(sum.y, f, w.y * g);
-                sum.z = fmaf(sum.z, f, w.z * g); sum.w = fmaf(sum.w, f, w.w * g);
+                v[n] = a.part_ml[place];
+                w[n] = *(const float4 *)(a.part + place * D + i % D);
+            }
+#pragma unroll
+            for (int n = 0; n < JOIN_BATCH; ++n) {
+                if (k0 + n * (WT_THREADS / 32) > c1) continue;
+                const float top = fmaxf(run.x, v[n].x), f = ex2(run.x - top), g = ex2(v[n].x - top);
+                run = make_float2(top, fmaf(run.y, f, v[n].y * g));
+                sum.x = fmaf(sum.x, f, w[n].x * g); sum.y = fmaf(sum.y, f, w[n].y * g);
+                sum.z = fmaf(sum.z, f, w[n].z * g); sum.w = fmaf(sum.w, f, w[n].w * g);
             }
         }
         __syncthreads();                                                        // the sums of the round before have been read
@@ -727,6 +750,8 @@ kv4_join_kernel(const AttnArgs a, int cols, int G, int NW, const float *weight, 
             T *dst = (T *)a.o + (((long long)b * a.n_q + col / R) * a.Hq + h * R + col % R) * D + i % D;
             stf(dst, sum.x * inv); stf(dst + 1, sum.y * inv); stf(dst + 2, sum.z * inv); stf(dst + 3, sum.w * inv);
         }
+        i0 += gridDim.x * 128;
+        locate();
     }
     if (!weight_out) return;
     // The columns' maxima and sums: a warp a column, the lanes over its parts.
