@@ -517,6 +517,43 @@ def micro_case(ctx, pk, name, Bz=1, n_vis=32768, final_bp=5000, attn_denominator
         flops = 2.0 * Bz * T * N * D
         nbytes = 2.0 * (Bz * T * (D + N) + N * D)
         bound = "tensor"
+    elif name in ("kv4_append", "kv4_attn", "kv4_evict"):
+        # the 4-bit cache of one attention layer: all T rows in and out again, one decode step over them with the weights
+        # gathered, eviction down to a final-bp share
+        Hq, Hkv, d, group = at_["Hq"], at_["Hkv"], at_["d"], 32
+        cap = -(-T // 16) * 16
+        k, v = (torch.randn(Bz, T, Hkv, d, device=dev).to(bf) for _ in range(2))
+        cache, zero = binding.Kv4Cache.empty(ctx, Bz, cap, Hkv, d, group), torch.zeros(Bz, dtype=torch.int32, device=dev)
+        binding.str_kv4_append(ctx, cache, k, v, zero)
+        row = 2.0 * Hkv * (d // 2 + 4 * (d // group))
+        lens = torch.full((Bz,), T, dtype=torch.int32, device=dev)
+        if name == "kv4_append":
+            def fn():
+                binding.str_kv4_append(ctx, cache, k, v, zero)
+                return binding.str_kv4_read(ctx, cache, zero, T, bf)
+            nbytes = Bz * T * (8.0 * Hkv * d + 2 * row)
+        elif name == "kv4_attn":
+            q = torch.randn(Bz, 1, Hq, d, device=dev).to(bf)
+            out = torch.empty_like(cache.weight)
+            fn = lambda: binding.str_kv4_attn(ctx, cache, q, lens, 1.0 / np.sqrt(d), weight_out=out)
+            flops = Bz * T * 4.0 * Hq * d
+            nbytes = Bz * T * (row + 8.0 * Hkv)
+        else:
+            K = max(1, T * (final_bp or 5000) // 10000)
+            cache.weight.copy_(torch.randn_like(cache.weight) ** 4)
+            out = binding.Kv4Cache.empty(ctx, Bz, -(-K // 16) * 16, Hkv, d, group)
+            fn = lambda: binding.str_kv4_evict(ctx, cache, lens, K, min(K, M), out)
+            nbytes = Bz * (4.0 * Hkv * T + K * (2 * row + 4 * Hkv + 12))
+    elif name == "mamba_step":
+        H, p, n, G = ms_["H"], ms_["p"], ms_["n"], ms_["G"]
+        x = torch.randn(Bz, 1, H, p, device=dev).to(bf)
+        Bm, Cm = (torch.randn(Bz, 1, G, n, device=dev).to(bf) for _ in range(2))
+        dt = torch.empty(Bz, 1, H, device=dev).uniform_(1e-3, 1e-1)
+        A = -torch.exp(torch.empty(H, device=dev).uniform_(0.0, float(np.log(16.0))))
+        state = torch.randn(Bz, H, p, n, device=dev)
+        fn = lambda: binding.str_mamba2_step(ctx, x, dt, A, Bm, Cm, state)
+        flops = 5.0 * Bz * H * p * n
+        nbytes = 8.0 * Bz * H * p * n
     else:
         raise SystemExit("unknown --micro " + name)
     flush = torch.empty(256 << 20, dtype=torch.uint8, device=dev)
@@ -588,7 +625,7 @@ def main():
     ap.add_argument("--graph", action="store_true", help="also time the step replayed from a CUDA graph")
     ap.add_argument("--no-kernels-alone", action="store_true", help="skip the per-kernel timings after the headline run")
     ap.add_argument("--micro", default="", help="time one kernel alone: ssd | mamba_score | mamba_dyn_score | attn_score | attn_fwd | "
-                                                "topk | compact | gemm")
+                                                "topk | compact | gemm | kv4_append | kv4_attn | kv4_evict | mamba_step")
     args = ap.parse_args()
     if args.warmup < 3 and args.impl == "ours":
         args.warmup = 3
