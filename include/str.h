@@ -378,7 +378,7 @@ typedef struct {
  * value <= the minimum, scale = bf16((max - zero) / 15), code = clamp(rint((x - zero) / scale), 0, 15); a group with a NaN
  * or an infinity (or a range beyond fp32) reads back as NaN.  Stored rows start with weight 0; with `positions`
  * (device [Bz,T_new] int32, or NULL) their ids go to cache->pos.
- * A row outside [0,cap) is not stored, and STR_ERR_INVALID_ARG is recorded in the status word.  The rows of one call must
+ * A row outside [0,cap) is not stored, and STR_ERR_INVALID_ARG is recorded for str_check_status (later calls run on).  The rows of one call must
  * not overlap.  Errors: INVALID_ARG, UNSUPPORTED_SHAPE. */
 int str_kv4_append(str_ctx *ctx, const str_kv4_shape *s, int dtype, int T_new, const void *k, const void *v,
                    const int32_t *positions, const int32_t *row_start, const int32_t *n_new, const str_kv4_cache *cache,
@@ -394,7 +394,7 @@ int str_kv4_read(str_ctx *ctx, const str_kv4_shape *s, int dtype, int n_out, con
  *   o[i] = sum_t softmax_t(q_i . k_t * softmax_scale) v_t over the rows t <= lens[b] - n_q + i,
  * k, v the values the codes stand for.  q, o device [Bz,n_q,Hq,d] dtype; lens device [Bz] int32, rows in use.  A token with
  * no row to see (an empty sequence; lens[b] < n_q) gives zeros.  A count outside [0,cap] is held to that range and recorded
- * in the status word.  Meant for few tokens (every 16 query rows of a key head read the cache once); for long
+ * as above.  Meant for few tokens (every 16 query rows of a key head read the cache once); for long
  * prompts use str_kv4_read and str_attn_prefill_rows.
  *   weight_out  device [Bz,Hkv,cap] fp32 or NULL: weight_out[b,h,t] = cache->weight[b,h,t] + the softmax weights that the
  *               n_q tokens' query heads of key head h put on row t, for t < lens[b]; other rows are left as they are.  May be
@@ -408,14 +408,16 @@ int str_kv4_attn(str_ctx *ctx, const str_kv4_shape *s, int dtype, int Hq, int n_
                  const int32_t *lens, float softmax_scale, void *o, float *weight_out, void *workspace,
                  size_t workspace_bytes, void *stream);
 
-/* Eviction by accumulated attention weight.  Of the lens[b] rows of each sequence min(lens[b], keep) stay: the protected
- * ones (the last n_recent, and with n_evictable, device [Bz] int32 or NULL, all rows from n_evictable[b] on; the newest
- * `keep` of them when they are more), then those with the largest score_t = sum_h cache->weight[b,h,t] (summed in fp64 in
- * head order, rounded to fp32; among equal scores the lower row; NaN counts as the lowest, infinities as +-FLT_MAX).
+/* Eviction by accumulated attention weight.  Of the lens[b] rows of each sequence (a count outside [0,cap] as above)
+ * min(lens[b], keep) stay: the protected ones (the last n_recent, and with n_evictable, device [Bz] int32 or NULL, all rows
+ * from n_evictable[b] on; the newest `keep` of them when they are more), then those with the largest score_t =
+ * sum_h cache->weight[b,h,t] (summed in fp64 in head order, rounded to fp32; among equal scores the lower row; NaN counts
+ * as the lowest, infinities as +-FLT_MAX).
  * Their codes, scales, weights and positions are copied bit for bit, in row order, to the rows 0 .. of `out`, a cache of
  * the same Bz, Hkv, d, group and capacity cap_out >= keep; rows of `out` behind them are left as they were.
  *   lens_out device [Bz] int32; kept_idx_out device [Bz,keep] int32, ascending, -1 behind the last.
  * `out` shares no memory with `cache`.  out->weight and out->pos may be NULL (not copied).
+ * Workspace: none for capacities of up to 131072 rows, beyond that size from the query, 256-byte aligned.
  * Errors: INVALID_ARG (keep > cap, keep > cap_out, n_recent > keep, shared buffers), UNSUPPORTED_SHAPE, WORKSPACE_TOO_SMALL. */
 size_t str_kv4_evict_workspace_size(const str_kv4_shape *s, int keep);
 int str_kv4_evict(str_ctx *ctx, const str_kv4_shape *s, const str_kv4_cache *cache, const int32_t *lens, int keep,

@@ -507,6 +507,8 @@ class Kv4Cache:
     @classmethod
     def empty(cls, ctx, Bz, cap, Hkv, d, group=32, pos=True, weight=True):
         """A cache of `cap` unused rows per sequence on the context's device."""
+        if group not in (32, 64, 128) or d % group:
+            raise ValueError("Kv4Cache: groups of 32, 64 or 128 elements that divide the row, not %s of %s" % (group, d))
         dev = "cuda:%d" % ctx.device
         rows = (Bz, Hkv, cap)
         codes = [torch.zeros(rows + (d // 2,), dtype=torch.uint8, device=dev) for _ in range(2)]

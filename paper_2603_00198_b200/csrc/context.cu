@@ -72,14 +72,14 @@ extern "C" const char *str_strerror(int code) {
 extern "C" int str_check_status(str_ctx *ctx, void *stream) {
     if (!ctx) return STR_ERR_INVALID_ARG;
     cudaStream_t st = (cudaStream_t)stream;
-    int host = 0;
-    STR_CUDA_OK(cudaMemcpyAsync(&host, ctx->status_dev, sizeof(int), cudaMemcpyDeviceToHost, st));
+    int host[2] = {0, 0};      // what makes kernels leave (a wait that ran out) | wrong counts in device arrays
+    STR_CUDA_OK(cudaMemcpyAsync(host, ctx->status_dev, sizeof(host), cudaMemcpyDeviceToHost, st));
     STR_CUDA_OK(cudaStreamSynchronize(st));
-    if (host != 0) {
-        STR_CUDA_OK(cudaMemsetAsync(ctx->status_dev, 0, sizeof(int), st));
+    if (host[0] != 0 || host[1] != 0) {
+        STR_CUDA_OK(cudaMemsetAsync(ctx->status_dev, 0, sizeof(host), st));
         STR_CUDA_OK(cudaStreamSynchronize(st));
     }
-    return host;
+    return host[0] != 0 ? host[0] : host[1];
 }
 
 extern "C" int str_profile_enable(str_ctx *ctx, int on) {

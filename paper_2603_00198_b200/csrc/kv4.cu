@@ -163,7 +163,7 @@ kv4_append_kernel(int cap, int T_new, const T *__restrict__ k, const T *__restri
         const int t = t0 + i * ROWS;
         live[i] = t < n;
         if (live[i] && ((long long)start + t < 0 || (long long)start + t >= cap)) {
-            atomicCAS(status, 0, STR_ERR_INVALID_ARG);
+            kv4_report(status);
             live[i] = false;
         }
         rk[i] = rv[i] = {};
@@ -215,7 +215,7 @@ kv4_read_kernel(int cap, int n_out, const int32_t *__restrict__ row_start, const
         ck[i] = cv[i] = wk[i] = wv[i] = 0u;                                     // reads as zero
         if (t >= n_out || t >= n) continue;
         if (row < 0 || row >= cap) {
-            atomicCAS(status, 0, STR_ERR_INVALID_ARG);
+            kv4_report(status);
             continue;
         }
         const long long at = base + row;

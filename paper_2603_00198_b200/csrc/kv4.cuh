@@ -38,6 +38,11 @@ static inline bool kv4_pointers_ok(const str_kv4_cache *c) {
              (uintptr_t)c->weight) & 15) == 0;
 }
 
+// Do two buffers share memory?
+static inline bool kv4_overlap(const void *a, size_t na, const void *b, size_t nb) {
+    return a && b && (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
+}
+
 __device__ __forceinline__ float kv4_scale(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 __device__ __forceinline__ float kv4_zero(uint32_t w) { return __uint_as_float(w << 16); }
 
@@ -62,11 +67,15 @@ __device__ __forceinline__ void kv4_widen8(const Kv4Raw8<float> &r, float (&x)[8
 template <typename T>
 __device__ __forceinline__ void kv4_load8(const T *p, float (&x)[8]) { kv4_widen8(kv4_raw8(p), x); }
 
+// A count or row that the caller got wrong: recorded in the second status word, which str_check_status reads too.  (The first
+// makes the tensor-core kernels of the context leave at once; a wrong count is no reason for that.)
+__device__ __forceinline__ void kv4_report(int *status) { atomicCAS(status + 1, 0, STR_ERR_INVALID_ARG); }
+
 // Row count of a sequence as the kernels use it: what the caller says, held to [0, cap]; a value outside is recorded.
 __device__ __forceinline__ int kv4_len(const int32_t *lens, int b, int cap, int *status) {
     const int n = lens[b];
     if (n < 0 || n > cap) {
-        if (threadIdx.x == 0) atomicCAS(status, 0, STR_ERR_INVALID_ARG);
+        if (threadIdx.x == 0) kv4_report(status);
         return n < 0 ? 0 : cap;
     }
     return n;

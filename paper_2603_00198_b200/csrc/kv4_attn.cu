@@ -23,6 +23,8 @@ extern "C" int str_kv4_attn(str_ctx *ctx, const str_kv4_shape *s, int dtype, int
     if (Hq <= 0 || Hq % s->Hkv != 0 || !kv4_pointers_ok(cache) || !lens || (weight_out && !cache->weight)) return STR_ERR_INVALID_ARG;
     if (n_q == 0) return STR_OK;
     if (!q || !o || ((uintptr_t)q & 15)) return STR_ERR_INVALID_ARG;
+    const size_t weight_bytes = (size_t)s->Bz * s->Hkv * s->cap * sizeof(float);
+    if (weight_out && weight_out != cache->weight && kv4_overlap(weight_out, weight_bytes, cache->weight, weight_bytes)) return STR_ERR_INVALID_ARG;
     if ((long long)(Hq / s->Hkv) * n_q > 4096) return STR_ERR_UNSUPPORTED_SHAPE;      // columns of the join's shared memory
     if (!workspace || ((uintptr_t)workspace & 255)) return STR_ERR_INVALID_ARG;
     const kv4_attn::Ws w = kv4_attn::ws_layout(s, Hq, n_q, kv4_attn::AT_MAX_GRID, weight_out != nullptr);

@@ -187,7 +187,7 @@ kv4_attn_kernel(const AttnArgs a) {
     }
     if (blockIdx.x == 0)
         for (int i = tid; i < a.Bz; i += NW * 32)
-            if (a.lens[i] < 0 || a.lens[i] > a.cap) atomicCAS(a.status, 0, STR_ERR_INVALID_ARG);
+            if (a.lens[i] < 0 || a.lens[i] > a.cap) kv4_report(a.status);
     // Every warp finds for itself where the CTA's places begin: the sequence and its first place.
     const int len32 = lane < a.Bz ? clamp_len(a.lens[lane], a.cap) : 0, places32 = unit_places(len32);
     long long total = __reduce_add_sync(0xffffffffu, places32);                 // below 2^31: a sequence has at most 2^25 tiles
@@ -301,8 +301,8 @@ kv4_attn_kernel(const AttnArgs a) {
             sum += __shfl_xor_sync(0xffffffffu, sum, 2);
             if (c == 0 && (PACK == 1 || r < 4)) {
                 col_part[qs][8 * qj + r] = sum;
-                if (qs == 0)                                                    // |scale| log2(e) 2^(exponent - 14); a scale of zero keeps -inf x 0 away
-                    col_mul[8 * qj + r] = (fmaxf(fabsf(a.scale_log2), 1e-37f) * 6.103515625e-05f) * __uint_as_float((uint32_t)ex << 23);
+                if (qs == 0)                                                    // |scale| log2(e) 2^(exponent - 14); never zero: -inf x 0 is NaN
+                    col_mul[8 * qj + r] = fmaxf((fabsf(a.scale_log2) * 6.103515625e-05f) * __uint_as_float((uint32_t)ex << 23), 1.2e-38f);
             }
             if (PACK == 2 && (r >> 2) != qs / RPG / NGP) {                      // these columns meet the other half of the groups
 #pragma unroll

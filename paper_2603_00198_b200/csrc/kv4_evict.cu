@@ -292,9 +292,14 @@ extern "C" int str_kv4_evict(str_ctx *ctx, const str_kv4_shape *s, const str_kv4
     const int rc = kv4_check_shape(s);
     if (rc != STR_OK) return rc;
     if (!kv4_pointers_ok(cache) || !kv4_pointers_ok(out) || !cache->weight || !lens || !lens_out) return STR_ERR_INVALID_ARG;
-    if ((out->pos && !cache->pos) || cache->k_codes == out->k_codes || cache->v_codes == out->v_codes ||
-        cache->k_scales == out->k_scales || cache->v_scales == out->v_scales || cache->weight == out->weight ||
-        (out->pos && cache->pos == out->pos) || lens == lens_out)
+    if ((out->pos && !cache->pos) || lens == lens_out || cap_out <= 0) return STR_ERR_INVALID_ARG;
+    const size_t heads = (size_t)s->Bz * s->Hkv, rows = heads * s->cap, rows_out = heads * cap_out, words = s->d / s->group * 4;
+    if (kv4_overlap(cache->k_codes, rows * (s->d / 2), out->k_codes, rows_out * (s->d / 2)) ||
+        kv4_overlap(cache->v_codes, rows * (s->d / 2), out->v_codes, rows_out * (s->d / 2)) ||
+        kv4_overlap(cache->k_scales, rows * words, out->k_scales, rows_out * words) ||
+        kv4_overlap(cache->v_scales, rows * words, out->v_scales, rows_out * words) ||
+        kv4_overlap(cache->weight, rows * 4, out->weight, rows_out * 4) ||
+        kv4_overlap(cache->pos, (size_t)s->Bz * s->cap * 4, out->pos, (size_t)s->Bz * cap_out * 4))
         return STR_ERR_INVALID_ARG;
     if (keep < 0 || keep > s->cap || keep > cap_out || n_recent < 0 || n_recent > keep) return STR_ERR_INVALID_ARG;
     if (cap_out % 16 != 0) return STR_ERR_UNSUPPORTED_SHAPE;

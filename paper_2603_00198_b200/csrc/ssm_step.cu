@@ -126,6 +126,8 @@ extern "C" int str_mamba2_step(str_ctx *ctx, const str_ssd_shape *s, const void 
     if (s->Bz <= 0 || s->T <= 0 || s->H <= 0 || s->p <= 0 || s->n <= 0 || s->G <= 0 || s->H % s->G != 0 ||
         (s->dtype != STR_F32 && s->dtype != STR_BF16))
         return STR_ERR_INVALID_ARG;
+    const size_t state_bytes = (size_t)s->Bz * s->H * s->p * s->n * sizeof(float);
+    if (state_out != state && kv4_overlap(state, state_bytes, state_out, state_bytes)) return STR_ERR_INVALID_ARG;
     if (s->n > 512 || s->Bz > 65535 || s->H > 65535) return STR_ERR_UNSUPPORTED_SHAPE;
     StrDeviceScope dev(ctx);
     if (!dev.ok) return STR_ERR_CUDA;

@@ -230,6 +230,9 @@ def test_attention_scale_may_be_negative_or_zero(ctx):
     check_attention(ctx, f, q, "bf16", -0.3, True)
     check_attention(ctx, f, q, "bf16", 0.0, True)
     check_attention(ctx, f, np.zeros_like(q), "bf16", 1.0, True)
+    check_attention(ctx, f, np.zeros_like(q), "bf16", 0.0, True)
+    check_attention(ctx, f, q, "f32", 1e-30, False)
+    check_attention(ctx, f, (q * np.float32(1e-25)), "f32", 1e-20, True)
 
 
 def test_attention_scores_that_grow_along_the_row(ctx):
@@ -548,6 +551,63 @@ def test_decode_calls_replay_from_two_graphs_and_run_on_other_streams(ctx):
     ctx.check_status()
 
 
+def test_a_wrong_count_does_not_stop_other_calls(ctx):
+    """Recorded for str_check_status, but the tensor-core kernels of the context go on working meanwhile."""
+    f = Filled(np.random.default_rng(61), [16, 0], 16, 1, 64, 32)
+    q = dev(np.ones((2, 1, 1, 64), dtype=np.float32))
+    binding.str_kv4_attn(ctx, f.cache, q, _i32([17, 0]), 0.1)
+    a, w = torch.ones(128, 256, device="cuda").bfloat16(), torch.ones(256, 256, device="cuda").bfloat16()
+    assert bool((binding.str_gemm(ctx, a, w) == 256).all())
+    with pytest.raises(binding.StrError) as e:
+        ctx.check_status()
+    assert e.value.code == -1
+    ctx.check_status()
+
+
+_FIRST_CALLS = """
+import sys, torch
+sys.path.insert(0, ".")
+from paper_2603_00198_b200 import binding
+ctx = binding.Context(0)
+torch.manual_seed(0)
+def make():
+    cache = binding.Kv4Cache.empty(ctx, 2, 512, 2, 64, 32)
+    out = binding.Kv4Cache.empty(ctx, 2, 64, 2, 64, 32)
+    k = torch.randn(2, 300, 2, 64, device="cuda", generator=torch.Generator("cuda").manual_seed(1))
+    q = torch.randn(2, 2, 6, 64, device="cuda", generator=torch.Generator("cuda").manual_seed(2))
+    st = torch.randn(2, 4, 8, 16, device="cuda", generator=torch.Generator("cuda").manual_seed(3))
+    x, dt, A, B = torch.ones(2, 1, 4, 8, device="cuda"), torch.ones(2, 1, 4, device="cuda"), -torch.ones(4, device="cuda"), torch.ones(2, 1, 2, 16, device="cuda")
+    return cache, out, k, q, st, x, dt, A, B
+zero, lens = torch.zeros(2, dtype=torch.int32, device="cuda"), torch.tensor([300, 17], dtype=torch.int32, device="cuda")
+def run(cache, out, k, q, st, x, dt, A, B):
+    binding.str_kv4_append(ctx, cache, k, -k, zero)
+    o = binding.str_kv4_attn(ctx, cache, q, lens, 0.125, weight_out=cache.weight)
+    n, kept = binding.str_kv4_evict(ctx, cache, lens, 50, 4, out)
+    r = binding.str_kv4_read(ctx, out, zero, 50, torch.float32, n_rows=n)
+    y, _ = binding.str_mamba2_step(ctx, x, dt, A, B, B, st)
+    return o, n, kept, r[0], r[1], y
+graph, args = torch.cuda.CUDAGraph(), make()
+torch.cuda.synchronize()
+with torch.cuda.graph(graph):
+    captured = run(*args)
+graph.replay()
+torch.cuda.synchronize()
+eager = run(*make())
+assert all(torch.equal(a, b) for a, b in zip(captured, eager))
+ctx.check_status()
+print("first calls captured")
+"""
+
+
+def test_the_first_calls_of_a_process_may_be_captured():
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    res = subprocess.run([sys.executable, "-c", _FIRST_CALLS], cwd=root, capture_output=True, text=True, timeout=300)
+    assert res.returncode == 0 and "first calls captured" in res.stdout, res.stderr[-3000:]
+
+
 def test_binding_refuses_what_the_kernels_cannot_read(ctx):
     g = np.random.default_rng(60)
     f, q, k, v, step, state = _decode_args(g)
@@ -568,6 +628,16 @@ def test_binding_refuses_what_the_kernels_cannot_read(ctx):
         binding.Kv4Cache(f.cache.k_codes, f.cache.v_codes[:, :1], f.cache.k_scales, f.cache.v_scales)
     with pytest.raises(binding.StrError):
         binding.str_kv4_evict(ctx, f.cache, lens, 16, 0, f.cache)                               # onto itself
+    for bad in (dict(group=48), dict(group=256), dict(group=16)):
+        with pytest.raises(ValueError):
+            binding.Kv4Cache.empty(ctx, 1, 16, 1, 128, **bad)
+    pool = torch.zeros(2 * 2 * 512 * 2, device="cuda")                                           # weights that half overlap
+    half = binding.Kv4Cache(f.cache.k_codes, f.cache.v_codes, f.cache.k_scales, f.cache.v_scales, f.cache.pos, pool[:2048].view(2, 2, 512))
+    with pytest.raises(binding.StrError):
+        binding.str_kv4_attn(ctx, half, q, lens, 0.1, weight_out=pool[1024:3072].view(2, 2, 512))
+    states = torch.zeros(3 * 2 * 4 * 16 * 32, device="cuda")
+    with pytest.raises(binding.StrError):
+        binding.str_mamba2_step(ctx, *step, states[:4096].view(2, 4, 16, 32), state_out=states[2048:6144].view(2, 4, 16, 32))
     with pytest.raises(ValueError):
         binding.str_kv4_evict(ctx, f.cache, lens, 16, 0, binding.Kv4Cache.empty(ctx, 2, 16, 2, 64, 64))
     with pytest.raises((TypeError, ValueError)):

@@ -159,8 +159,11 @@ def test_cache_arguments_are_refused(libstr):
     assert ev(cache=_cache_ptrs(weight=131076)) == -1                                                       # alignment
     assert libstr.str_kv4_evict_workspace_size(a(s), 16) == 0
     s.cap = 200000                                                                                          # a row over many CTAs: needs a workspace
+    far = _cache_ptrs(**{k: 1 << (36 + i) for i, (k, _) in enumerate(binding.Kv4CachePtrs._fields_)})
+    ev2 = lambda ws=p, nb=big, cache=c: ev(cache=cache, out=far, ws=ws, nb=nb)  # noqa: E731
     need = libstr.str_kv4_evict_workspace_size(a(s), 16)
-    assert need >= 200000 * 4 and ev(nb=need - 1) == -3 and ev(ws=None) == -1 and ev(ws=p + 128) == -1
+    assert need >= 200000 * 4 and ev2(nb=need - 1) == -3 and ev2(ws=None) == -1 and ev2(ws=p + 128) == -1
+    assert ev2(cache=_cache_ptrs(v_codes=far.v_codes + 1024), nb=need - 1) == -1                             # buffers that overlap in part
     s.cap = 64
     assert ev(cache=_cache_ptrs(weight=None)) == -1 and ev(cache=_cache_ptrs(pos=None)) == -1
     for shared in ("k_codes", "v_codes", "k_scales", "v_scales", "pos", "weight"):
