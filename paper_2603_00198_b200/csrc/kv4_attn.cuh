@@ -662,6 +662,7 @@ kv4_attn_kernel(const AttnArgs a) {
         }
         tc::fence_proxy_async();                                                // what was written to the rings comes before the next copies into them
         __syncthreads();                                                        // the rings and the sums are free again
+        if (abort_flag) return;                                                 // a wait gave up: its barriers are not to be used again
     }
 }
 

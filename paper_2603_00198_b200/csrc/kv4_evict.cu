@@ -329,9 +329,11 @@ extern "C" int str_kv4_evict(str_ctx *ctx, const str_kv4_shape *s, const str_kv4
         if (src != STR_OK) return src;
     } else {
         StrProfScope prof_scope(ctx, STR_CAT_TOPK, stream);
-        // smallest cluster (power of two, at most 8 CTAs) and run length that cover the capacity
+        // Smallest cluster (power of two, at most 8 CTAs) in which a thread has `run` rows: one where all clusters fit the card at
+        // once (one sequence of 4096 rows 9.5 us against 11.8 with runs of four), else four (32 sequences of 8448 rows 80 against 83).
+        const int run = s->Bz * SEL_MAX_CTAS <= ctx->sm_count ? 1 : 4;
         int ncta = 1;
-        while (ncta < SEL_MAX_CTAS && ncta * SEL_THREADS * 4 < s->cap) ncta *= 2;
+        while (ncta < SEL_MAX_CTAS && ncta * SEL_THREADS * run < s->cap) ncta *= 2;
         const int per_thread = ceil_div(s->cap, ncta * SEL_THREADS);
         auto launch = per_thread <= 1 ? launch_select<1> : per_thread <= 2 ? launch_select<2> : per_thread <= 4 ? launch_select<4>
                     : per_thread <= 8 ? launch_select<8> : launch_select<16>;
