@@ -375,11 +375,11 @@ typedef struct {
 
 /* Rows in.  Quantises k, v device [Bz,T_new,Hkv,d] dtype (post-RoPE keys; the layout of the hand-off) and stores token j
  * of sequence b in cache row row_start[b] + j, for j < n_new[b] (n_new NULL: all T_new).  Per group: zero = the largest bf16
- * value <= the minimum, scale = bf16((max - zero) / 15), code = clamp(rint((x - zero) / scale), 0, 15); a group with a NaN
+ * value <= the minimum, scale = bf16((max - zero) * fp32(1/15)), code = clamp(rint((x - zero) / scale), 0, 15); a group with a NaN
  * or an infinity (or a range beyond fp32) reads back as NaN.  Stored rows start with weight 0; with `positions`
  * (device [Bz,T_new] int32, or NULL) their ids go to cache->pos.
- * A row outside [0,cap) is not stored, and STR_ERR_INVALID_ARG is recorded for str_check_status (later calls run on).  The rows of one call must
- * not overlap.  Errors: INVALID_ARG, UNSUPPORTED_SHAPE. */
+ * A row outside [0,cap) is not stored, and STR_ERR_INVALID_ARG is recorded for str_check_status (later calls run on).
+ * The rows of one call must not overlap.  Errors: INVALID_ARG, UNSUPPORTED_SHAPE. */
 int str_kv4_append(str_ctx *ctx, const str_kv4_shape *s, int dtype, int T_new, const void *k, const void *v,
                    const int32_t *positions, const int32_t *row_start, const int32_t *n_new, const str_kv4_cache *cache,
                    void *stream);

@@ -28,7 +28,7 @@ def kv4_quantise(x, group):
     g = np.where(bad[..., None], np.float32(0), g)
     with np.errstate(over="ignore"):
         zero = bf16_floor(g.min(-1))
-        span = (g.max(-1) - zero) / np.float32(15)
+        span = (g.max(-1) - zero) * (np.float32(1) / np.float32(15))
         over = ~np.isfinite(span)
         scale = bf16_round(np.where(over, np.float32(0), span))
         over |= ~np.isfinite(scale)

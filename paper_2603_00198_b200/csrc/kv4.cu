@@ -1,7 +1,7 @@
 // The 4-bit key/value cache: rows in (str_kv4_append) and rows back out (str_kv4_read).
 //
 // Per group of `group` elements x of a row: zero = the largest bf16 value <= min x (exact for bf16 rows), scale =
-// bf16((max x - zero) / 15), code = clamp(rint((x - zero) / scale), 0, 15).  zero is rounded down so that no element lies
+// bf16((max x - zero) * (1/15)), code = clamp(rint((x - zero) / scale), 0, 15).  zero is rounded down so that no element lies
 // below it; scale is rounded to nearest (off by at most 2^-9: the top code moves by 0.03 of a step).  Both bounds of what
 // the work costs are memory: every row is read once and written once.
 //
@@ -99,9 +99,7 @@ __device__ __forceinline__ uint32_t quantise8(const Kv4Raw8<T> &raw, uint32_t &w
     group_extremes<GROUP>(raw, lo, hi, finite);
     kv4_widen8(raw, x);
     const float zero = __bfloat162float(__float2bfloat16_rd(lo));
-    const float span = hi - zero, s0 = span * (1.f / 15.f);
-    const float step = span > 1e-28f ? fmaf(fmaf(-s0, 15.f, span), 1.f / 15.f, s0) : span / 15.f;     // span / 15 correctly rounded, as below
-    const float scale = __bfloat162float(__float2bfloat16_rn(step));
+    const float scale = __bfloat162float(__float2bfloat16_rn((hi - zero) * (1.f / 15.f)));
     if (!finite || !(scale <= 3.4e38f)) {  // a NaN or infinity in the group, or extremes too far apart
         word = 0x7FFF0000u;                         // NaN scale: the whole group reads back as NaN
         return 0u;

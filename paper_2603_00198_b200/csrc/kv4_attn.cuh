@@ -400,34 +400,40 @@ kv4_attn_kernel(const AttnArgs a) {
                 float s[NT][4];
 #pragma unroll
                 for (int g = 0; g < NGP; ++g) {
+                    const float sa = kv4_scale(wa[g]), za = fmaf(8.f, sa, kv4_zero(wa[g])), sb = kv4_scale(wb[g]), zb = fmaf(8.f, sb, kv4_zero(wb[g]));
                     float acc[NT][4];
 #pragma unroll
-                    for (int k = 0; k < PACK * RPG; ++k) {                      // the runs of group g (and of its partner in the other half)
-                        const int q = g * RPG + k % RPG + (k / RPG) * NGP * RPG;
+                    for (int k = 0; k < PACK * RPG; ++k) {                      // the runs of group g (and with each that of its partner in the other half)
+                        const int q = (g + k % PACK * NGP) * RPG + k / PACK;
+                        // The instruction truncates its sums.  For bf16 storage a group is summed in it whole; for fp32 storage only a
+                        // run, low terms first, and the runs outside it.
+                        const bool fresh = TERMS == 2 ? k % PACK == 0 : k == 0, done = TERMS == 2 ? k % PACK == PACK - 1 : k == PACK * RPG - 1;
                         uint32_t a0, a1, a2, a3, b0, b1, b2, b3;
                         codes2(bytes2<true>(ka[q], magic), magic2, a0, a2);
                         codes2(bytes2<true>(kb[q], magic), magic2, a1, a3);
                         codes2(bytes2<false>(ka[q], magic), magic2, b0, b2);
                         codes2(bytes2<false>(kb[q], magic), magic2, b1, b3);
 #pragma unroll
-                        for (int j = 0; j < NT; ++j)
+                        for (int j = 0; j < NT; ++j) {
 #pragma unroll
-                            for (int t = 0; t < TERMS; ++t) {
+                            for (int t = TERMS - 1; t >= 0; --t) {
                                 uint32_t qf[4];                                 // from shared memory every time: registers are what is short
                                 load_words<4>(q_at + ((j * NG + q) * TERMS + t) * 512, qf);
-                                if (k == 0 && t == 0) mma_f16_first(acc[j], a0, a1, a2, a3, qf[0], qf[1]);
+                                if (fresh && t == TERMS - 1) mma_f16_first(acc[j], a0, a1, a2, a3, qf[0], qf[1]);
                                 else mma_f16(acc[j], a0, a1, a2, a3, qf[0], qf[1]);
                                 mma_f16(acc[j], b0, b1, b2, b3, qf[2], qf[3]);
                             }
-                    }
-                    const float sa = kv4_scale(wa[g]), za = fmaf(8.f, sa, kv4_zero(wa[g])), sb = kv4_scale(wb[g]), zb = fmaf(8.f, sb, kv4_zero(wb[g]));
+                            if (done) {
 #pragma unroll
-                    for (int j = 0; j < NT; ++j)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float y = e < 2 ? za : zb;
-                            s[j][e] = fmaf(e < 2 ? sa : sb, acc[j][e], g == 0 ? y * q_sum[j][g][e & 1] : fmaf(y, q_sum[j][g][e & 1], s[j][e]));
+                                for (int e = 0; e < 4; ++e) {
+                                    const float y = e < 2 ? za : zb;
+                                    if (k / PACK == (TERMS == 2 ? 0 : RPG - 1))
+                                        s[j][e] = g == 0 ? y * q_sum[j][g][e & 1] : fmaf(y, q_sum[j][g][e & 1], s[j][e]);
+                                    s[j][e] = fmaf(e < 2 ? sa : sb, acc[j][e], s[j][e]);
+                                }
+                            }
                         }
+                    }
                 }
 #pragma unroll
                 for (int j = 0; j < NT; ++j)
