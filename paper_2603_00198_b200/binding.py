@@ -1,4 +1,4 @@
-"""Thin ctypes binding over libstr.so: argument marshalling only.
+"""Thin binding over libstr.so: argument marshalling only (ctypes; the decode calls go through ``csrc/marshal.cpp``).
 
 Every function has the name of the C entry point it calls (see ``include/str.h``) and takes torch
 CUDA tensors, which serve purely as device memory; all arithmetic runs in the library's kernels.
@@ -88,7 +88,7 @@ EXPORTS = [
     "str_mamba2_step",
 ]
 
-# The decode calls run once per layer and token: declared argument types let ctypes convert plain integers itself.
+# Declared argument types of the decode entry points, for direct calls with plain integers as addresses.
 _I, _F, _Z, _P = c_int, c_float, c_size_t, c_void_p
 _ARGTYPES = {
     "str_kv4_append": [_P, _P, _I, _I, _P, _P, _P, _P, _P, _P, _P],
@@ -120,6 +120,25 @@ def lib():
             getattr(L, name).argtypes = args
         _LIB = L
     return _LIB
+
+
+_MARSHAL = None
+
+
+def _marshal():
+    """Load _marshal.so (argument checks, outputs and calls of the decode entry points, ``csrc/marshal.cpp``) once."""
+    global _MARSHAL
+    if _MARSHAL is None:
+        try:
+            from . import _marshal as m
+        except ImportError as e:
+            raise ImportError("_marshal.so: %s; run `python -m paper_2603_00198_b200.build`" % e) from e
+        L = lib()
+        m.setup(_check, torch.OutOfMemoryError, *(ctypes.cast(getattr(L, name), c_void_p).value for name in (
+            "str_kv4_append", "str_kv4_read", "str_kv4_attn_workspace_size", "str_kv4_attn", "str_kv4_evict_workspace_size",
+            "str_kv4_evict", "str_mamba2_step")))
+        _MARSHAL = m
+    return _MARSHAL
 
 
 def _dt(t):
@@ -175,6 +194,10 @@ class Context:
     @property
     def handle(self):
         return self._h
+
+    @property
+    def address(self):
+        return self._h.value or 0
 
     def workspace(self, nbytes):
         nbytes = max(int(nbytes), 256)
@@ -450,30 +473,6 @@ def str_attn_prefill_rows(ctx, q_rows, row_pos, k, v, softmax_scale):
     return o
 
 
-def _arg(ctx, t, shape, dtype, what):
-    """Device address of an argument of a decode call, after the checks that the C side cannot make."""
-    if t.dtype is not dtype:
-        raise TypeError("%s: expected %s, got %s" % (what, dtype, t.dtype))
-    if t.get_device() != ctx.device:
-        raise ValueError("%s: expected a tensor on cuda:%d, got %s" % (what, ctx.device, t.device))
-    if t.shape != shape:
-        raise ValueError("%s: expected shape %s, got %s" % (what, shape, tuple(t.shape)))
-    if not t.is_contiguous():
-        raise ValueError("%s: tensors must be contiguous" % what)
-    return t.data_ptr()
-
-
-def _ctx_stream(ctx):
-    """Address of the current stream of the context's device, whichever device is current."""
-    return torch._C._cuda_getCurrentRawStream(ctx.device)
-
-
-def _scratch(ctx, nbytes):
-    """Workspace of one call, from torch's stream-ordered pool: calls on several streams, and captured graphs, share none.
-    (None when the call needs none.)"""
-    return torch.empty(nbytes, dtype=torch.uint8, device=ctx._dev) if nbytes else None
-
-
 class Kv4Cache:
     """The tensors of a 4-bit key/value cache (layout in ``include/str.h``): codes [Bz,Hkv,cap,d/2] uint8, one int32 word
     (bf16 scale, bf16 zero) per group [Bz,Hkv,cap,d/group], and optionally the original token ids ``pos`` [Bz,cap] int32 and
@@ -502,7 +501,7 @@ class Kv4Cache:
         self._shape = Kv4Shape(Bz, cap, Hkv, d, self.group)
         self._ptrs = Kv4CachePtrs(*(t.data_ptr() if t is not None else None for t in (k_codes, v_codes, k_scales, v_scales, pos, weight)))
         self.shape_ref, self.ptrs_ref = ctypes.addressof(self._shape), ctypes.addressof(self._ptrs)
-        self.index, self._ws_sizes = dev.index, {}
+        self.index = dev.index
 
     @classmethod
     def empty(cls, ctx, Bz, cap, Hkv, d, group=32, pos=True, weight=True):
@@ -520,37 +519,17 @@ class Kv4Cache:
         if self.index != ctx.device:
             raise ValueError("Kv4Cache: the cache is on %s, the context on cuda:%d" % (self.device, ctx.device))
 
-    def _ws_size(self, name, *args):
-        """Workspace size of a call on this cache's shape, asked of the library once."""
-        key = (name,) + args
-        n = self._ws_sizes.get(key)
-        if n is None:
-            n = self._ws_sizes[key] = getattr(lib(), name)(self.shape_ref, *args)
-        return n
-
 
 def str_kv4_append(ctx, cache, k, v, row_start, positions=None, n_new=None):
     """Quantises k, v [Bz,T,Hkv,d] and stores them in the rows row_start[b] .. of the cache (the first n_new[b] of them)."""
     cache._on(ctx)
-    T = k.shape[1]
-    shape = (cache.Bz, T, cache.Hkv, cache.d)
-    dt = _dt(k)
-    _check(lib().str_kv4_append(ctx.handle, cache.shape_ref, dt, T, _arg(ctx, k, shape, k.dtype, "k"), _arg(ctx, v, shape, k.dtype, "v"),
-                                None if positions is None else _arg(ctx, positions, (cache.Bz, T), torch.int32, "positions"),
-                                _arg(ctx, row_start, (cache.Bz,), torch.int32, "row_start"),
-                                None if n_new is None else _arg(ctx, n_new, (cache.Bz,), torch.int32, "n_new"), cache.ptrs_ref, _ctx_stream(ctx)),
-           "str_kv4_append")
+    _marshal().append(ctx.address, ctx.device, cache.shape_ref, cache.ptrs_ref, k, v, row_start, positions, n_new)
 
 
 def str_kv4_read(ctx, cache, row_start, T, dtype, n_rows=None):
     """(k, v) [Bz,T,Hkv,d] of ``dtype`` from the rows row_start[b] .. of the cache; zeros behind the first n_rows[b]."""
     cache._on(ctx)
-    k = torch.empty((cache.Bz, T, cache.Hkv, cache.d), dtype=dtype, device=cache.device)
-    v = torch.empty_like(k)
-    _check(lib().str_kv4_read(ctx.handle, cache.shape_ref, _dt(k), T, _arg(ctx, row_start, (cache.Bz,), torch.int32, "row_start"),
-                              None if n_rows is None else _arg(ctx, n_rows, (cache.Bz,), torch.int32, "n_rows"), cache.ptrs_ref,
-                              k.data_ptr(), v.data_ptr(), _ctx_stream(ctx)), "str_kv4_read")
-    return k, v
+    return _marshal().read(ctx.address, ctx.device, cache.shape_ref, cache.ptrs_ref, row_start, T, dtype, n_rows)
 
 
 def str_kv4_attn(ctx, cache, q, lens, softmax_scale, weight_out=None):
@@ -558,16 +537,7 @@ def str_kv4_attn(ctx, cache, q, lens, softmax_scale, weight_out=None):
     included).  With ``weight_out`` [Bz,Hkv,cap] fp32 (``cache.weight`` itself, or another tensor) it receives cache.weight plus
     the attention weights drawn by each row in use."""
     cache._on(ctx)
-    if q.dim() != 4:
-        raise ValueError("q: expected [Bz,n_q,Hq,d]")
-    n_q, Hq = q.shape[1], q.shape[2]
-    o = torch.empty_like(q)
-    ws = _scratch(ctx, cache._ws_size("str_kv4_attn_workspace_size", Hq, n_q, 0 if weight_out is None else 1))
-    _check(lib().str_kv4_attn(ctx.handle, cache.shape_ref, _dt(q), Hq, n_q, _arg(ctx, q, (cache.Bz, n_q, Hq, cache.d), q.dtype, "q"), cache.ptrs_ref,
-                          _arg(ctx, lens, (cache.Bz,), torch.int32, "lens"), softmax_scale, o.data_ptr(),
-                          None if weight_out is None else _arg(ctx, weight_out, (cache.Bz, cache.Hkv, cache.cap), torch.float32, "weight_out"),
-                          None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), _ctx_stream(ctx)), "str_kv4_attn")
-    return o
+    return _marshal().attn(ctx.address, ctx.device, cache.shape_ref, cache.ptrs_ref, q, lens, softmax_scale, weight_out)
 
 
 def str_kv4_evict(ctx, cache, lens, keep, n_recent, out, n_evictable=None):
@@ -577,31 +547,15 @@ def str_kv4_evict(ctx, cache, lens, keep, n_recent, out, n_evictable=None):
     out._on(ctx)
     if (out.Bz, out.Hkv, out.d, out.group) != (cache.Bz, cache.Hkv, cache.d, cache.group):
         raise ValueError("str_kv4_evict: the two caches have different shapes")
-    n = torch.empty((cache.Bz,), dtype=torch.int32, device=cache.device)
-    kept = torch.empty((cache.Bz, max(keep, 0)), dtype=torch.int32, device=cache.device)
-    ws = _scratch(ctx, cache._ws_size("str_kv4_evict_workspace_size", keep))
-    _check(lib().str_kv4_evict(ctx.handle, cache.shape_ref, cache.ptrs_ref, _arg(ctx, lens, (cache.Bz,), torch.int32, "lens"), keep, n_recent,
-                           None if n_evictable is None else _arg(ctx, n_evictable, (cache.Bz,), torch.int32, "n_evictable"), out.cap, out.ptrs_ref,
-                           n.data_ptr(), kept.data_ptr(), None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(),
-                           _ctx_stream(ctx)), "str_kv4_evict")
-    return n, kept
+    return _marshal().evict(ctx.address, ctx.device, cache.shape_ref, cache.ptrs_ref, lens, keep, n_recent, n_evictable, out.cap, out.ptrs_ref)
 
 
 def str_mamba2_step(ctx, x, dt, A, B, C, state, D=None, state_out=None):
     """A few tokens of the Mamba-2 recurrence from ``state`` [Bz,H,p,n] fp32; returns (y [Bz,T,H,p], state_out).  Without
     ``state_out`` the state is updated in place."""
-    Bz, T, H, p = x.shape
-    G, n = B.shape[2], B.shape[3]
-    s = SsdShape(Bz, T, H, p, n, G, 0, _dt(x))
     if state_out is None:
         state_out = state
-    y = torch.empty_like(x)
-    f32, sshape = torch.float32, (Bz, H, p, n)
-    _check(lib().str_mamba2_step(ctx.handle, ctypes.addressof(s), _arg(ctx, x, (Bz, T, H, p), x.dtype, "x"), _arg(ctx, dt, (Bz, T, H), f32, "dt"),
-                                 _arg(ctx, A, (H,), f32, "A"), _arg(ctx, B, (Bz, T, G, n), x.dtype, "B"), _arg(ctx, C, (Bz, T, G, n), x.dtype, "C"),
-                                 None if D is None else _arg(ctx, D, (H,), f32, "D"), _arg(ctx, state, sshape, f32, "state"), y.data_ptr(),
-                                 _arg(ctx, state_out, sshape, f32, "state_out"), _ctx_stream(ctx)), "str_mamba2_step")
-    return y, state_out
+    return _marshal().step(ctx.address, ctx.device, x, dt, A, B, C, state, D, state_out), state_out
 
 
 class Stack:

@@ -1,0 +1,122 @@
+"""The extension module that marshals the decode calls: what it refuses, and how, without a GPU.  (The calls themselves, their
+outputs and the refusals of tensors on a device are tested with the operators.)"""
+import ctypes
+import os
+import subprocess
+import sys
+
+import pytest
+import torch
+
+from paper_2603_00198_b200 import binding
+
+
+def _i32(*shape):
+    return torch.zeros(shape, dtype=torch.int32)
+
+
+class _Shape:
+    def __init__(self):
+        self.s = binding.Kv4Shape(2, 32, 2, 64, 32)
+        self.c = binding.Kv4CachePtrs()
+        self.args = (0, 0, ctypes.addressof(self.s), ctypes.addressof(self.c))
+
+
+def test_wrong_argument_counts_and_types_are_refused():
+    m, sh = binding._marshal(), _Shape()
+    for f in (m.append, m.read, m.attn, m.evict, m.step):
+        with pytest.raises(TypeError, match="arguments"):
+            f(1, 2)
+    with pytest.raises(TypeError, match="k: expected a tensor, got list"):
+        m.append(*sh.args, [1.0], None, None, None, None)
+    with pytest.raises(TypeError, match="q: expected a tensor, got NoneType"):
+        m.attn(*sh.args, None, _i32(2), 0.1, None)
+    with pytest.raises(TypeError):
+        m.read("handle", *sh.args[1:], _i32(2), 1, torch.float32, None)
+    with pytest.raises(TypeError, match="dtype"):
+        m.read(*sh.args, _i32(2), 1, "float32", None)
+    with pytest.raises(TypeError, match="unsupported dtype"):
+        m.read(*sh.args, _i32(2), 1, torch.float16, None)
+    with pytest.raises(TypeError, match="unsupported dtype"):
+        m.attn(*sh.args, torch.zeros(2, 1, 2, 64, dtype=torch.float64), _i32(2), 0.1, None)
+
+
+def test_sizes_out_of_range_are_refused():
+    m, sh = binding._marshal(), _Shape()
+    for T in (-1, 1 << 31, 1 << 70):
+        with pytest.raises((ValueError, OverflowError)):
+            m.read(*sh.args, _i32(2), T, torch.float32, None)
+    for keep, recent in ((1 << 31, 0), (0, 1 << 31), (0, -(1 << 40))):
+        with pytest.raises(ValueError, match="out of range"):
+            m.evict(*sh.args, _i32(2), keep, recent, None, 32, sh.args[3])
+    for bad in (torch.zeros(2, 1, 64), torch.zeros(64)):
+        with pytest.raises(ValueError, match="dimensions"):
+            m.attn(*sh.args, bad, _i32(2), 0.1, None)
+        with pytest.raises(ValueError, match="dimensions"):
+            m.append(*sh.args, bad, bad, _i32(2), None, None)
+        with pytest.raises(ValueError, match="dimensions"):
+            m.step(0, 0, bad, bad, bad, bad, bad, bad, None, bad)
+
+
+def test_host_tensors_are_refused():
+    m, sh = binding._marshal(), _Shape()
+    q, lens = torch.zeros(2, 1, 2, 64), _i32(2)
+    x, B, st = torch.zeros(2, 1, 4, 16), torch.zeros(2, 1, 1, 16), torch.zeros(2, 4, 16, 16)
+    for call in (lambda: m.append(*sh.args, q, q, lens, None, None), lambda: m.attn(*sh.args, q, lens, 0.1, None),
+                 lambda: m.read(*sh.args, lens, 1, torch.float32, None), lambda: m.evict(*sh.args, lens, 8, 0, None, 32, sh.args[3]),
+                 lambda: m.step(0, 0, x, torch.zeros(2, 1, 4), torch.zeros(4), B, B, st, None, st)):
+        with pytest.raises(ValueError, match="expected a tensor on cuda:0, got cpu"):
+            call()
+
+
+def test_refused_calls_hold_no_references():
+    m, sh = binding._marshal(), _Shape()
+    q, lens = torch.zeros(2, 1, 2, 64), _i32(2)
+    before = sys.getrefcount(q), sys.getrefcount(lens), sys.getrefcount(binding._check)
+    for _ in range(50):
+        with pytest.raises(ValueError):
+            m.attn(*sh.args, q, lens, 0.1, None)
+    assert (sys.getrefcount(q), sys.getrefcount(lens), sys.getrefcount(binding._check)) == before
+
+
+def test_a_call_before_setup_is_refused():
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    code = ("import torch\nfrom paper_2603_00198_b200 import _marshal as m\n"
+            "try:\n    m.step(*[0] * 10)\nexcept RuntimeError as e:\n    assert 'setup' in str(e)\n    print('refused')\n"
+            "try:\n    m.setup(print, 0, *[0] * 7)\nexcept ValueError:\n    print('refused')\n")
+    res = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
+    assert res.returncode == 0 and res.stdout.split() == ["refused", "refused"], res.stderr[-3000:]
+
+
+@pytest.mark.gpu
+def test_outputs_are_new_tensors_and_threads_may_call_at_once():
+    """Four threads, each on its own stream, step their own states: the lock is free during a call, and no two share a buffer."""
+    import threading
+    ctx = binding.Context(0)
+    Bz, H, p, n = 2, 4, 16, 32
+    g = torch.Generator().manual_seed(3)
+    x, dt, A = torch.randn(Bz, 1, H, p, generator=g).cuda(), torch.rand(Bz, 1, H, generator=g).cuda(), -torch.rand(H, generator=g).cuda()
+    B, C = torch.randn(Bz, 1, 1, n, generator=g).cuda(), torch.randn(Bz, 1, 1, n, generator=g).cuda()
+    torch.cuda.synchronize()
+    res, errors = [None] * 4, []
+
+    def work(i):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                st = torch.zeros(Bz, H, p, n, device="cuda")
+                ys = [binding.str_mamba2_step(ctx, x, dt, A, B, C, st)[0] for _ in range(200)]
+                torch.cuda.current_stream().synchronize()
+                assert len({y.data_ptr() for y in ys}) == 200
+                res[i] = (torch.stack(ys).cpu(), st.cpu())
+        except Exception as e:                               # reported by the test's own thread
+            errors.append(e)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join(120)
+    assert not errors, errors
+    for ys, st in res[1:]:
+        assert torch.equal(ys, res[0][0]) and torch.equal(st, res[0][1])
+    ctx.check_status()
