@@ -227,7 +227,7 @@ PyObject *evict(PyObject *const *a) {
         Unlocked free;
         const size_t need = f_evict_ws(s, (int)keep);
         n = empty({s->Bz}, at::kInt, c.device);
-        kept = empty({s->Bz, keep > 0 ? keep : 0}, at::kInt, c.device);
+        kept = empty({s->Bz, keep > 0 && keep <= s->cap ? keep : 0}, at::kInt, c.device);         // more than cap rows are refused below
         if (need) ws = empty({(int64_t)need}, at::kByte, c.device);
         rc = f_evict(c.h, s, cache, (const int32_t *)lens, (int)keep, (int)recent, (const int32_t *)evictable, (int)cap_out, out,
                      (int32_t *)n.data_ptr(), (int32_t *)kept.data_ptr(), need ? ws.data_ptr() : nullptr, need, stream_of(c.device));

@@ -120,3 +120,16 @@ def test_outputs_are_new_tensors_and_threads_may_call_at_once():
     for ys, st in res[1:]:
         assert torch.equal(ys, res[0][0]) and torch.equal(st, res[0][1])
     ctx.check_status()
+
+
+@pytest.mark.gpu
+def test_a_refused_eviction_allocates_nothing_for_its_rows():
+    ctx = binding.Context(0)
+    cache, out = binding.Kv4Cache.empty(ctx, 2, 32, 2, 64), binding.Kv4Cache.empty(ctx, 2, 16, 2, 64)
+    lens = torch.full((2,), 20, dtype=torch.int32, device="cuda")
+    torch.cuda.reset_peak_memory_stats()
+    before = torch.cuda.memory_allocated()
+    for keep in (-1, 17, 33, (1 << 31) - 1):                 # more than the target, the source, any memory holds
+        with pytest.raises(binding.StrError):
+            binding.str_kv4_evict(ctx, cache, lens, keep, 0, out)
+    assert torch.cuda.max_memory_allocated() - before < 4096
