@@ -634,7 +634,7 @@ def test_binding_refuses_what_the_kernels_cannot_read(ctx):
     pool = torch.zeros(2 * 2 * 512 * 2, device="cuda")                                           # weights that half overlap
     half = binding.Kv4Cache(f.cache.k_codes, f.cache.v_codes, f.cache.k_scales, f.cache.v_scales, f.cache.pos, pool[:2048].view(2, 2, 512))
     with pytest.raises(binding.StrError):
-        binding.str_kv4_attn(ctx, half, q, lens, 0.1, weight_out=pool[1024:3072].view(2, 2, 512))
+        binding.str_kv4_attn(ctx, half, q, lens, 0.1, weight_out=pool[1024:][:2048].view(2, 2, 512))
     states = torch.zeros(3 * 2 * 4 * 16 * 32, device="cuda")
     with pytest.raises(binding.StrError):
         binding.str_mamba2_step(ctx, *step, states[:4096].view(2, 4, 16, 32), state_out=states[2048:6144].view(2, 4, 16, 32))
