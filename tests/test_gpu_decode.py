@@ -132,6 +132,53 @@ def test_append_values_that_are_not_finite_poison_their_group_only(ctx):
     assert np.array_equal(cache.k_scales[0, :, 4].cpu().numpy(), want[0])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,group", SHAPES)
+def test_append_a_non_finite_element_anywhere_poisons_its_group_only(ctx, dtype, d, group):
+    """Row t has one NaN, inf or -inf at element t (values: at element d - 1 - t): every lane and piece in turn."""
+    g = np.random.default_rng([7, d, group])
+    k, v = _rows(g, (1, d, 2, d), dtype, True), _rows(g, (1, d, 2, d), dtype, False)
+    words = []
+    for x, at in ((k, np.arange(d)), (v, np.arange(d)[::-1])):
+        x[0, np.arange(d), 1, at] = np.where(np.arange(d) % 3 == 0, np.nan, np.where(np.arange(d) % 3 == 1, np.inf, -np.inf))
+        clean = np.where(np.isfinite(x), x, 0.0)
+        code, zero, scale = decode.kv4_quantise(np.swapaxes(clean, 1, 2), group)
+        w = decode.kv4_words(zero, scale).view(np.int32)[0]                           # [Hkv, d, d / group]
+        w[1, np.arange(d), at // group] = 0x7FFF0000
+        words.append(w)
+    cache = binding.Kv4Cache.empty(ctx, 1, d, 2, d, group)
+    binding.str_kv4_append(ctx, cache, dev(k, dtype), dev(v, dtype), _i32([0]))
+    assert np.array_equal(cache.k_scales[0].cpu().numpy(), words[0])
+    assert np.array_equal(cache.v_scales[0].cpu().numpy(), words[1])
+    ctx.check_status()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_at_sixteen_byte_addresses(ctx, dtype):
+    """The alignment that the interface asks for and no more: inputs and outputs 16 bytes behind a 256-byte boundary."""
+    g = np.random.default_rng(11)
+    T, Hkv, d = 19, 3, 64
+    off = 16 // (2 if dtype == "bf16" else 4)
+    k, v = (dev(_rows(g, (1, T, Hkv, d), dtype, keys), dtype) for keys in (True, False))
+    shift = lambda t: torch.cat([torch.zeros(off, dtype=t.dtype, device="cuda"), t.flatten()])[off:].view(t.shape)
+    ks, vs = shift(k), shift(v)
+    assert ks.data_ptr() % 32 == 16 and vs.data_ptr() % 32 == 16
+    caches = [binding.Kv4Cache.empty(ctx, 1, 32, Hkv, d) for _ in range(2)]
+    start = _i32([5])
+    binding.str_kv4_append(ctx, caches[0], k, v, start)
+    binding.str_kv4_append(ctx, caches[1], ks, vs, start)
+    for n in ("k_codes", "v_codes", "k_scales", "v_scales"):
+        assert torch.equal(getattr(caches[0], n), getattr(caches[1], n)), n
+    want = binding.str_kv4_read(ctx, caches[0], start, T, TORCH[dtype])
+    buf = [torch.full((k.numel() + 2 * off,), 7.0, dtype=TORCH[dtype], device="cuda") for _ in range(2)]
+    rc = binding.lib().str_kv4_read(ctx.handle, caches[0].shape_ref, binding._dt(k), T, start.data_ptr(), None, caches[0].ptrs_ref,
+                                    buf[0][off:].data_ptr(), buf[1][off:].data_ptr(), torch.cuda.current_stream().cuda_stream)
+    assert rc == 0
+    for b, w in zip(buf, want):
+        assert torch.equal(b[off:off + k.numel()].view(k.shape), w) and (b[:off] == 7.0).all() and (b[off + k.numel():] == 7.0).all()
+    ctx.check_status()
+
+
 def test_append_and_read_outside_the_capacity_are_skipped_and_reported(ctx):
     cache = binding.Kv4Cache.empty(ctx, 2, 16, 1, 64, 32)
     x = dev(np.ones((2, 4, 1, 64), dtype=np.float32))
