@@ -500,7 +500,9 @@ kv4_attn_kernel(const AttnArgs a) {
                             t = fmaxf(t, m[j][i]);
                             f[i] = ex2(m[j][i] - t);
                             m[j][i] = t;
-                            bar[j][i] = (t + M_SLACK) / q_mul[j][i];            // a scale of zero: beyond reach
+                            // rounded down twice, so that a score up to the bar lies no more than the slack above t once it has been
+                            // multiplied and rounded (to nearest, scores of 3e7 could lie 8 above); a scale of zero: beyond reach
+                            bar[j][i] = __fdiv_rd(__fadd_rd(t, M_SLACK), q_mul[j][i]);
                             l[j][i] *= f[i];
 #pragma unroll
                             for (int g = 0; g < NGP; ++g) z[j][g][i] *= f[i];

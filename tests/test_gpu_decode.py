@@ -282,6 +282,43 @@ def test_attention_scale_may_be_negative_or_zero(ctx):
     check_attention(ctx, f, (q * np.float32(1e-25)), "f32", 1e-20, True)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("scale", [0.41, 0.47, 0.53, -0.93])
+@pytest.mark.parametrize("top", [1e6, 1.8e7, 2.6e7, 4.5e7, 1e8])
+def test_attention_of_scores_whose_neighbours_lie_far_apart(ctx, dtype, scale, top):
+    """Rows 0-15 of a sequence share a score of about `top` (log2 units), rows 16-31 one that is a few units higher.
+
+    A raw score S = 32 (z0 + z1) is formed exactly (groups of equal elements, scale 0; q all ones), its product with the scale is
+    rounded once: off by at most half a step, 2^-24 of it, and the scale's own product with log2(e) moves a difference D by 2^-23 D.
+    The weight of the second rows, 1 / (1 + 2^-D), then lies between those of D -+ both scores' half steps, and the output between
+    the two means of the values."""
+    d, cap, Bz = 64, 32, 96
+    g = np.random.default_rng([int(top), int(100 * abs(scale))])
+    unit = abs(scale) * np.log2(np.e)
+    z0 = np.float32(2.0 ** np.floor(np.log2(top / unit / 32))) * (1 + g.integers(0, 64, Bz) / 64.0)          # bf16 holds it
+    step = 2.0 ** max(np.floor(np.log2(top / unit)) - 22, 0) / 32                # S of both rows is a multiple of an fp32 step
+    z1 = np.maximum(np.round(g.uniform(1.0, 12.0, Bz) / unit / 32 / step), 1) * step
+    z1 = np.where(inputs.to_grid(z1.astype(np.float32), "bf16") == z1, z1, 4 * step)
+    k = np.zeros((Bz, 1, cap, d), dtype=np.float32)
+    k[..., :32] = (np.sign(scale) * z0)[:, None, None, None]
+    k[:, :, 16:, 32:] = (np.sign(scale) * z1)[:, None, None, None]
+    f = Filled(g, [cap] * Bz, cap, 1, d, 32, k=k)
+    assert np.array_equal(f.k, k.astype(np.float64))
+    S = 32.0 * np.stack([z0, z0 + z1])
+    assert np.array_equal(S.astype(np.float32), S)
+    o = binding.str_kv4_attn(ctx, f.cache, dev(np.ones((Bz, 1, 1, d), dtype=np.float32), dtype), _i32(f.lens), scale).float().cpu().numpy()[:, 0, 0]
+    ctx.check_status()
+    assert np.isfinite(o).all()
+    D, half = unit * 32.0 * z1, 2.0 ** -24 * unit * S.sum(0)
+    lo, hi = (1.0 / (1.0 + np.exp2(np.clip(-(D * (1 + s * 2.0 ** -22) + s * half), -1000, 1000))) for s in (-1, 1))
+    v = f.v[:, 0].reshape(Bz, 2, 16, d)
+    a, b = v.mean(2)[:, 0], v.mean(2)[:, 1]
+    ends = np.stack([a + (b - a) * lo[:, None], a + (b - a) * hi[:, None]])
+    # beside the weights' range: their roundings and sum, the factor of the matrix product, the output's own
+    tol = (64 + cap) * E * np.abs(f.v).max() + (2.0 ** -11 if dtype == "bf16" else 2.0 ** -22) * 15.0 * f.v_scale.max() + HALF[dtype] * np.abs(ends).max(0)
+    assert np.all((o >= ends.min(0) - tol) & (o <= ends.max(0) + tol))
+
+
 def test_attention_scores_that_grow_along_the_row(ctx):
     """Every later row beats all before it: the running maximum moves all the way."""
     d, n, Hkv, Hq = 128, 1000, 1, 4
