@@ -477,7 +477,8 @@ class Kv4Cache:
     """The tensors of a 4-bit key/value cache (layout in ``include/str.h``): codes [Bz,Hkv,cap,d/2] uint8, one int32 word
     (bf16 scale, bf16 zero) per group [Bz,Hkv,cap,d/group], and optionally the original token ids ``pos`` [Bz,cap] int32 and
     the accumulated attention ``weight`` [Bz,Hkv,cap] fp32.  The tensors stay the caller's; how many rows of each sequence
-    are in use is the caller's to keep."""
+    are in use is the caller's to keep.  Every call takes the tensors that the attributes name when it is made: one may be put in
+    another's place (``cache.weight = cache.weight * 0.99``) as long as type, shape and device stay."""
 
     def __init__(self, k_codes, v_codes, k_scales, v_scales, pos=None, weight=None):
         if k_codes.dim() != 4 or k_scales.dim() != 4 or k_scales.shape[3] == 0:
@@ -499,9 +500,15 @@ class Kv4Cache:
         self.k_codes, self.v_codes, self.k_scales, self.v_scales, self.pos, self.weight = k_codes, v_codes, k_scales, v_scales, pos, weight
         self.Bz, self.Hkv, self.cap, self.d, self.group, self.device = Bz, Hkv, cap, d, d // words[3], dev
         self._shape = Kv4Shape(Bz, cap, Hkv, d, self.group)
-        self._ptrs = Kv4CachePtrs(*(t.data_ptr() if t is not None else None for t in (k_codes, v_codes, k_scales, v_scales, pos, weight)))
-        self.shape_ref, self.ptrs_ref = ctypes.addressof(self._shape), ctypes.addressof(self._ptrs)
+        self._ptrs = Kv4CachePtrs()
+        self.shape_ref, self._ptrs_at = ctypes.addressof(self._shape), ctypes.addressof(self._ptrs)
         self.index = dev.index
+
+    @property
+    def ptrs_ref(self):
+        """Address of the C struct of the tensors' addresses, filled in anew: an attribute may name another tensor than it did before."""
+        _marshal().cache(self._ptrs_at, self.shape_ref, self.index, self.k_codes, self.v_codes, self.k_scales, self.v_scales, self.pos, self.weight)
+        return self._ptrs_at
 
     @classmethod
     def empty(cls, ctx, Bz, cap, Hkv, d, group=32, pos=True, weight=True):
@@ -547,7 +554,7 @@ def str_kv4_evict(ctx, cache, lens, keep, n_recent, out, n_evictable=None):
     out._on(ctx)
     if (out.Bz, out.Hkv, out.d, out.group) != (cache.Bz, cache.Hkv, cache.d, cache.group):
         raise ValueError("str_kv4_evict: the two caches have different shapes")
-    return _marshal().evict(ctx.address, ctx.device, cache.shape_ref, cache.ptrs_ref, lens, keep, n_recent, n_evictable, out.cap, out.ptrs_ref)
+    return _marshal().evict(ctx.address, ctx.device, cache.shape_ref, cache.ptrs_ref, lens, keep, n_recent, n_evictable, out._shape.cap, out.ptrs_ref)
 
 
 def str_mamba2_step(ctx, x, dt, A, B, C, state, D=None, state_out=None):

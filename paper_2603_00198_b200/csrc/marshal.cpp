@@ -137,6 +137,25 @@ void dims(const at::Tensor &t, int n, const char *what) {
     throw Refused();
 }
 
+// cache(ptrs, shape, device, k_codes, v_codes, k_scales, v_scales, pos, weight): checks the tensors that a cache's attributes name
+// now and writes their addresses to `ptrs`.  Asked for before every call, as the attributes may be given other tensors, and
+// tensors other memory, between two of them.
+PyObject *cache(PyObject *const *a) {
+    str_kv4_cache *p = address<str_kv4_cache>(a[0]);
+    const str_kv4_shape *s = address<str_kv4_shape>(a[1]);
+    const int device = (int)integer(a[2], 0, 1 << 20, "device");
+    const Shape codes = {s->Bz, s->Hkv, s->cap, s->d / 2}, words = {s->Bz, s->Hkv, s->cap, s->d / s->group};
+    str_kv4_cache c;
+    c.k_codes = arg(a[3], device, codes, at::kByte, "Kv4Cache.k_codes");
+    c.v_codes = arg(a[4], device, codes, at::kByte, "Kv4Cache.v_codes");
+    c.k_scales = arg(a[5], device, words, at::kInt, "Kv4Cache.k_scales");
+    c.v_scales = arg(a[6], device, words, at::kInt, "Kv4Cache.v_scales");
+    c.pos = (int32_t *)optional(a[7], device, {s->Bz, s->cap}, at::kInt, "Kv4Cache.pos");
+    c.weight = (float *)optional(a[8], device, {s->Bz, s->Hkv, s->cap}, at::kFloat, "Kv4Cache.weight");
+    *p = c;
+    Py_RETURN_NONE;
+}
+
 // append(handle, device, shape, cache, k, v, row_start, positions, n_new)
 PyObject *append(PyObject *const *a) {
     const Ctx c(a);
@@ -150,11 +169,11 @@ PyObject *append(PyObject *const *a) {
     void *pk = arg(k, c.device, rows, dt, "k"), *pv = arg(a[5], c.device, rows, dt, "v");
     void *start = arg(a[6], c.device, {s->Bz}, at::kInt, "row_start"), *pos = optional(a[7], c.device, {s->Bz, T}, at::kInt, "positions");
     void *n_new = optional(a[8], c.device, {s->Bz}, at::kInt, "n_new");
-    const str_kv4_cache *cache = address<str_kv4_cache>(a[3]);
+    const str_kv4_cache cache = *address<str_kv4_cache>(a[3]);      // as it is now: another thread may refill it once the lock is free
     int rc;
     {
         Unlocked free;
-        rc = f_append(c.h, s, code, (int)T, pk, pv, (const int32_t *)pos, (const int32_t *)start, (const int32_t *)n_new, cache, stream_of(c.device));
+        rc = f_append(c.h, s, code, (int)T, pk, pv, (const int32_t *)pos, (const int32_t *)start, (const int32_t *)n_new, &cache, stream_of(c.device));
     }
     check(rc, "str_kv4_append");
     Py_RETURN_NONE;
@@ -172,14 +191,14 @@ PyObject *read(PyObject *const *a) {
     const at::ScalarType dt = ((THPDtype *)a[6])->scalar_type;
     const int code = type_code(dt);
     void *start = arg(a[4], c.device, {s->Bz}, at::kInt, "row_start"), *n_rows = optional(a[7], c.device, {s->Bz}, at::kInt, "n_rows");
-    const str_kv4_cache *cache = address<str_kv4_cache>(a[3]);
+    const str_kv4_cache cache = *address<str_kv4_cache>(a[3]);      // as it is now: another thread may refill it once the lock is free
     at::Tensor k, v;
     int rc;
     {
         Unlocked free;
         k = empty({s->Bz, T, s->Hkv, s->d}, dt, c.device);
         v = empty({s->Bz, T, s->Hkv, s->d}, dt, c.device);
-        rc = f_read(c.h, s, code, (int)T, (const int32_t *)start, (const int32_t *)n_rows, cache, k.data_ptr(), v.data_ptr(), stream_of(c.device));
+        rc = f_read(c.h, s, code, (int)T, (const int32_t *)start, (const int32_t *)n_rows, &cache, k.data_ptr(), v.data_ptr(), stream_of(c.device));
     }
     check(rc, "str_kv4_read");
     return Py_BuildValue("NN", THPVariable_Wrap(k), THPVariable_Wrap(v));
@@ -198,7 +217,7 @@ PyObject *attn(PyObject *const *a) {
     const double scale = PyFloat_AsDouble(a[6]);
     if (scale == -1.0 && PyErr_Occurred()) throw Refused();
     void *weight = optional(a[7], c.device, {s->Bz, s->Hkv, s->cap}, at::kFloat, "weight_out");
-    const str_kv4_cache *cache = address<str_kv4_cache>(a[3]);
+    const str_kv4_cache cache = *address<str_kv4_cache>(a[3]);      // as it is now: another thread may refill it once the lock is free
     at::Tensor o, ws;
     int rc;
     {
@@ -206,7 +225,7 @@ PyObject *attn(PyObject *const *a) {
         const size_t need = f_attn_ws(s, (int)Hq, (int)n_q, weight != nullptr);
         o = empty({s->Bz, n_q, Hq, s->d}, code == STR_BF16 ? at::kBFloat16 : at::kFloat, c.device);
         ws = empty({(int64_t)need}, at::kByte, c.device);
-        rc = f_attn(c.h, s, code, (int)Hq, (int)n_q, pq, cache, (const int32_t *)lens, (float)scale, o.data_ptr(), (float *)weight, ws.data_ptr(),
+        rc = f_attn(c.h, s, code, (int)Hq, (int)n_q, pq, &cache, (const int32_t *)lens, (float)scale, o.data_ptr(), (float *)weight, ws.data_ptr(),
                     need, stream_of(c.device));
     }
     check(rc, "str_kv4_attn");
@@ -220,7 +239,7 @@ PyObject *evict(PyObject *const *a) {
     const int64_t keep = integer(a[5], INT32_MIN, INT32_MAX, "keep"), recent = integer(a[6], INT32_MIN, INT32_MAX, "n_recent");
     void *lens = arg(a[4], c.device, {s->Bz}, at::kInt, "lens"), *evictable = optional(a[7], c.device, {s->Bz}, at::kInt, "n_evictable");
     const int64_t cap_out = integer(a[8], 0, INT32_MAX, "cap_out");
-    const str_kv4_cache *cache = address<str_kv4_cache>(a[3]), *out = address<str_kv4_cache>(a[9]);
+    const str_kv4_cache cache = *address<str_kv4_cache>(a[3]), out = *address<str_kv4_cache>(a[9]);
     at::Tensor n, kept, ws;
     int rc;
     {
@@ -229,7 +248,7 @@ PyObject *evict(PyObject *const *a) {
         n = empty({s->Bz}, at::kInt, c.device);
         kept = empty({s->Bz, keep > 0 && keep <= s->cap ? keep : 0}, at::kInt, c.device);         // more than cap rows are refused below
         if (need) ws = empty({(int64_t)need}, at::kByte, c.device);
-        rc = f_evict(c.h, s, cache, (const int32_t *)lens, (int)keep, (int)recent, (const int32_t *)evictable, (int)cap_out, out,
+        rc = f_evict(c.h, s, &cache, (const int32_t *)lens, (int)keep, (int)recent, (const int32_t *)evictable, (int)cap_out, &out,
                      (int32_t *)n.data_ptr(), (int32_t *)kept.data_ptr(), need ? ws.data_ptr() : nullptr, need, stream_of(c.device));
     }
     check(rc, "str_kv4_evict");
@@ -307,7 +326,7 @@ PyObject *setup(PyObject *, PyObject *const *a, Py_ssize_t n) {
 
 #define ENTRY(name, N) {#name, (PyCFunction)(void (*)(void))entry<name, N>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {{"setup", (PyCFunction)(void (*)(void))setup, METH_FASTCALL, nullptr},
-                         ENTRY(append, 9), ENTRY(read, 8), ENTRY(attn, 8), ENTRY(evict, 10), ENTRY(step, 10),
+                         ENTRY(cache, 9), ENTRY(append, 9), ENTRY(read, 8), ENTRY(attn, 8), ENTRY(evict, 10), ENTRY(step, 10),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", "argument marshalling of the decode calls", -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -88,6 +88,61 @@ def test_a_call_before_setup_is_refused():
     assert res.returncode == 0 and res.stdout.split() == ["refused", "refused"], res.stderr[-3000:]
 
 
+class _Fake:
+    """What Kv4Cache looks at in a tensor on a device."""
+
+    def __init__(self, shape, dtype, at):
+        self.shape, self.dtype, self.device, self.at = shape, dtype, torch.device("cuda", 0), at
+
+    def dim(self):
+        return len(self.shape)
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return self.at
+
+
+def test_a_cache_asks_for_the_addresses_of_its_tensors_anew(monkeypatch):
+    """An attribute that names another tensor than before: the next call gets that one's address."""
+
+    class Module:
+        @staticmethod
+        def cache(ptrs, shape, device, *tensors):
+            assert device == 0
+            p = ctypes.cast(ptrs, ctypes.POINTER(binding.Kv4CachePtrs)).contents
+            for (name, _), t in zip(binding.Kv4CachePtrs._fields_, tensors):
+                setattr(p, name, t.data_ptr() if t is not None else None)
+
+    monkeypatch.setattr(binding, "_MARSHAL", Module)
+    codes, words = ((2, 2, 32, 32), torch.uint8), ((2, 2, 32, 2), torch.int32)
+    cache = binding.Kv4Cache(_Fake(*codes, 0x100), _Fake(*codes, 0x200), _Fake(*words, 0x300), _Fake(*words, 0x400),
+                             _Fake((2, 32), torch.int32, 0x500), _Fake((2, 2, 32), torch.float32, 0x600))
+
+    def names():
+        p = ctypes.cast(cache.ptrs_ref, ctypes.POINTER(binding.Kv4CachePtrs)).contents
+        return [getattr(p, n) for n, _ in binding.Kv4CachePtrs._fields_]
+
+    assert names() == [0x100, 0x200, 0x300, 0x400, 0x500, 0x600]
+    cache.weight, cache.pos = _Fake((2, 2, 32), torch.float32, 0x700), None
+    assert names() == [0x100, 0x200, 0x300, 0x400, None, 0x700]
+    cache.k_codes.at = 0x800                                 # the tensor itself was given other memory
+    assert names() == [0x800, 0x200, 0x300, 0x400, None, 0x700]
+
+
+def test_the_tensors_of_a_cache_are_checked_at_every_call():
+    m, sh = binding._marshal(), _Shape()
+    codes, words = torch.zeros(2, 2, 32, 32, dtype=torch.uint8), torch.zeros(2, 2, 32, 2, dtype=torch.int32)
+    with pytest.raises(TypeError, match="Kv4Cache.k_codes: expected a tensor, got NoneType"):
+        m.cache(sh.args[3], sh.args[2], 0, None, codes, words, words, None, None)
+    with pytest.raises(TypeError, match="Kv4Cache.k_codes: expected Byte"):
+        m.cache(sh.args[3], sh.args[2], 0, words, codes, words, words, None, None)
+    with pytest.raises(ValueError, match="Kv4Cache.k_codes: expected a tensor on cuda:0, got cpu"):
+        m.cache(sh.args[3], sh.args[2], 0, codes, codes, words, words, None, None)
+    assert sh.c.k_codes is None                              # nothing is stored before all have been checked
+
+
 @pytest.mark.gpu
 def test_outputs_are_new_tensors_and_threads_may_call_at_once():
     """Four threads, each on its own stream, step their own states: the lock is free during a call, and no two share a buffer."""
@@ -133,3 +188,55 @@ def test_a_refused_eviction_allocates_nothing_for_its_rows():
         with pytest.raises(binding.StrError):
             binding.str_kv4_evict(ctx, cache, lens, keep, 0, out)
     assert torch.cuda.max_memory_allocated() - before < 4096
+
+
+@pytest.mark.gpu
+def test_calls_use_the_tensors_that_a_cache_names_now():
+    """Attributes given other tensors, and a tensor given other memory, between two calls: nothing goes to where they were."""
+    ctx = binding.Context(0)
+    g = torch.Generator(device="cuda").manual_seed(4)
+    rows = lambda: torch.randn(2, 20, 2, 64, device="cuda", generator=g)  # noqa: E731
+    k, v, q = rows(), rows(), torch.randn(2, 1, 4, 64, device="cuda", generator=g)
+    start, lens = torch.zeros(2, dtype=torch.int32, device="cuda"), torch.full((2,), 20, dtype=torch.int32, device="cuda")
+    cache, same = (binding.Kv4Cache.empty(ctx, 2, 32, 2, 64) for _ in range(2))
+    for c in (cache, same):
+        binding.str_kv4_append(ctx, c, k, v, start)
+        binding.str_kv4_attn(ctx, c, q, lens, 0.125, weight_out=c.weight)
+    first = cache.weight
+    kept = first.clone()
+    cache.weight = cache.weight * 0.5                        # a decay written as one would
+    same.weight.mul_(0.5)
+    for c in (cache, same):
+        binding.str_kv4_attn(ctx, c, q, lens, 0.125, weight_out=c.weight)
+    assert torch.equal(cache.weight, same.weight) and torch.equal(first, kept)
+    old, at = cache.v_codes, cache.v_codes.data_ptr()
+    before = old.clone()
+    cache.v_codes = torch.zeros_like(old)
+    binding.str_kv4_append(ctx, cache, k, v, start)
+    binding.str_kv4_append(ctx, same, k, v, start)
+    assert torch.equal(cache.v_codes, same.v_codes) and torch.equal(old, before)
+    moved = torch.zeros_like(cache.k_codes)
+    cache.k_codes.set_(moved)                                # the same tensor object, other memory
+    assert cache.k_codes.data_ptr() == moved.data_ptr() != at
+    binding.str_kv4_append(ctx, cache, k, v, start)
+    assert torch.equal(moved, same.k_codes)
+    out, out_same = (binding.Kv4Cache.empty(ctx, 2, 16, 2, 64) for _ in range(2))
+    out.pos, held = None, out.pos
+    held.fill_(-3)
+    cache.weight, same.weight = (torch.rand(2, 2, 32, device="cuda", generator=g),) * 2
+    assert torch.equal(binding.str_kv4_evict(ctx, cache, lens, 9, 2, out)[1], binding.str_kv4_evict(ctx, same, lens, 9, 2, out_same)[1])
+    assert (held == -3).all() and torch.equal(out.k_codes, out_same.k_codes)
+    for name, bad in (("weight", torch.zeros(2, 2, 16, device="cuda")), ("weight", torch.zeros(2, 2, 32)), ("pos", torch.zeros(2, 32, device="cuda")),
+                      ("k_scales", None), ("v_codes", torch.zeros(2, 2, 64, 32, dtype=torch.uint8, device="cuda")[:, :, ::2])):
+        good = getattr(cache, name)
+        setattr(cache, name, bad)
+        with pytest.raises((TypeError, ValueError), match="Kv4Cache." + name):
+            binding.str_kv4_append(ctx, cache, k, v, start)
+        setattr(cache, name, good)
+    cache.weight.resize_(2, 2, 16)
+    with pytest.raises(ValueError, match="Kv4Cache.weight"):
+        binding.str_kv4_attn(ctx, cache, q, lens, 0.125)
+    cache.weight = None
+    with pytest.raises(binding.StrError):
+        binding.str_kv4_attn(ctx, cache, q, lens, 0.125, weight_out=kept)
+    ctx.check_status()
