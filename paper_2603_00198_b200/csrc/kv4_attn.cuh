@@ -11,8 +11,10 @@
 // matrix instruction lines products up by the nominal exponent and then drops the last six to ten bits: measured, 5e-6 instead
 // of 4e-7 of error.)
 // The other factor is fp16: q scaled by a power of two to just below 2^15 (bf16 values fit exactly; fp32 storage takes two
-// fp16 terms, 22 bits), and p scale 2^(11-E) with E the largest exponent of a value scale so far (one rounding of 2^-11 for
-// bf16 storage, two terms for fp32 storage).
+// fp16 terms, 22 bits), and p scale times a power of two that a warp keeps for each query row and group (one rounding of 2^-11 for
+// bf16 storage, two terms for fp32 storage).  One power for all of a warp's rows was 1 to 8 % faster (8448 rows 9.9 against 10.6 us,
+// 65792 rows 22.8 against 23.3, five tokens over 18 x 16640 rows 269 against 283), but then a huge value took the bits of all others,
+// even one without weight, in another group or seen by another head only.
 // Products are summed in fp32; scales, zeros, the softmax and all sums stay fp32.
 //
 // Layout.  Codes are the A operand (16 rows of it 16 tokens for q.k, 16 elements for the output), the query rows of a
@@ -30,6 +32,8 @@
 #pragma once
 #include <cuda_fp16.h>
 
+#include <stddef.h>
+
 #include <atomic>
 #include <type_traits>
 
@@ -44,10 +48,20 @@ constexpr int WT_THREADS = 256;
 constexpr int JOIN_BATCH = 5;            // parts a warp of the join loads at once: 8 x 5 cover one of 8 key heads spread over the card
 constexpr float M_START = -3.0e38f;      // running maximum before the first row: finite, so that differences stay defined
 constexpr float M_SLACK = 3.0f;          // the running maximum moves only when a score beats it by this (log2): p <= 2^3
+// How far, in powers of two, an fp16 unit may be from the one that rows and maximum ask for: the largest p scale of a column and
+// group is at least 2^(11 - window - lag) of its units, and half the smallest step of fp16 is 2^-25.
+template <int TERMS> constexpr int UNIT_WINDOW = TERMS == 1 ? 12 : 8;
+template <int TERMS> constexpr int UNIT_LAG = TERMS == 1 ? 4 : 3;
+constexpr int UNIT_MAX = 253;            // biased exponent of the largest unit, 2^126: its reciprocal is a normal number
 
 __device__ __forceinline__ float ex2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float rcp(float x) {
+    float y;
+    asm("rcp.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
 __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -116,6 +130,16 @@ struct Stage {
     static constexpr int CODES = AT_TILE * D / 2, WORDS = AT_TILE * (D / GROUP) * 4, BYTES = 2 * CODES + 2 * WORDS;
 };
 
+// What p scale of a column and group is multiplied by to become the fp16 factor (a power of two; the output is kept in units of its
+// reciprocal), for the two columns of a lane.  A unit comes from the scales and weights that its own column and group have met.
+template <int NT, int NGP>
+struct __align__(16) Units {
+    uint32_t limit[4];                   // of group g: words up to this have p scale unit < 2^15 in all columns of the lane
+    float2 of[NT][NGP];
+    float2 change[NT][NGP];              // what they were last multiplied by
+    float2 m[NT];                        // the running maximum when a column's units were last raised
+};
+
 // Neither the scale nor the zero of a word is infinite or NaN.
 __device__ __forceinline__ bool finite_word(uint32_t w) { return (w & 0x7F800000u) != 0x7F800000u && (w & 0x7F80u) != 0x7F80u; }
 
@@ -168,6 +192,7 @@ kv4_attn_kernel(const AttnArgs a) {
     __shared__ uint64_t bars[NW][AT_STAGES];
     __shared__ float warp_m[NW][COLS], warp_l[NW][COLS];
     __shared__ float2 cta_ml[COLS];
+    __shared__ Units<NT, NGP> units[NW][4];                                     // by a lane's c
     __shared__ uint4 q_frag[NT][NG][TERMS][32];                                 // q as the B operand, by lane
     __shared__ float q_top[NT][NG][8];                                          // max |q| of a column's elements of a run
     __shared__ float col_part[NG][COLS], col_mul[COLS];                         // sums of a column's scaled elements by run; what its scores are in
@@ -352,8 +377,22 @@ kv4_attn_kernel(const AttnArgs a) {
                 for (int g = 0; g < NGP; ++g) z[j][g][i] = 0.f;
             }
         }
-        int E = 27;                                                             // biased exponent the value scales are taken relative to
-        uint32_t top_word = ((uint32_t)E << 23) | 0x7FFFFFu;                    // the largest word of a scale with that exponent
+        typedef Units<NT, NGP> Units_;
+        Units_ &mine = units[warp][c];
+        uint32_t units_at;                                                      // its address, kept (worked out anew it costs ten instructions a use)
+        asm volatile("mov.u32 %0, %1;" : "=r"(units_at) : "r"(tc::smem_u32(&mine)));
+        if (r == 0) {
+            const float most = __uint_as_float((uint32_t)UNIT_MAX << 23);
+#pragma unroll
+            for (int g = 0; g < NGP; ++g) mine.limit[g] = 0u;
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+#pragma unroll
+                for (int g = 0; g < NGP; ++g) mine.of[j][g] = make_float2(most, most);
+                mine.m[j] = make_float2(M_START, M_START);
+            }
+        }
+        __syncwarp();
         const int all = len - a.n_q + 1;                                        // rows that every column sees
 
         // One tile.  EDGE: some column may not see some row.
@@ -465,55 +504,146 @@ kv4_attn_kernel(const AttnArgs a) {
                             }
                         }
                 }
-                // value words of this lane's two rows; does the running maximum or exponent move?
-                load_words<NGP>(st + 2 * St::CODES + St::WORDS + ta * (4 * NGR) + half * (4 * NGP), wa);
-                load_words<NGP>(st + 2 * St::CODES + St::WORDS + tb * (4 * NGR) + half * (4 * NGP), wb);
-                uint32_t top = 0u;
+                // value words of this lane's two rows; does the running maximum or a unit move?
+                const uint32_t words_at = st + 2 * St::CODES + St::WORDS + half * (4 * NGP);
+                load_words<NGP>(words_at + ta * (4 * NGR), wa);
+                load_words<NGP>(words_at + tb * (4 * NGR), wb);
+                bool rises = false, beyond = false;
+                uint32_t limit_word[NGP];
+                load_words<NGP>(units_at + (uint32_t)offsetof(Units_, limit), limit_word);
 #pragma unroll
-                for (int g = 0; g < NGP; ++g) top = max(top, max(wa[g], wb[g]));
-                bool grow = top > top_word;
+                for (int g = 0; g < NGP; ++g) beyond |= max(wa[g], wb[g]) > limit_word[g];
 #pragma unroll
                 for (int j = 0; j < NT; ++j)
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) grow |= fmaxf(s[j][i], s[j][i + 2]) > bar[j][i];
-                if (__any_sync(0xffffffffu, grow)) {
-                    uint32_t finite = 0u;                                       // a NaN scale makes its group NaN and sets no exponent
-#pragma unroll
-                    for (int g = 0; g < NGP; ++g) {
-                        const uint32_t w0 = wa[g] & 0x7FFFFFFFu, w1 = wb[g] & 0x7FFFFFFFu;
-                        if (w0 < 0x7F800000u) finite = max(finite, w0);
-                        if (w1 < 0x7F800000u) finite = max(finite, w1);
-                    }
-                    const int e_new = max(E, (int)(__reduce_max_sync(0xffffffffu, finite) >> 23));
-                    const float fe = __uint_as_float((uint32_t)max(127 + E - e_new, 0) << 23);     // 2^(E - e_new); 0 is as good below 2^-126
-                    E = e_new;
-                    top_word = ((uint32_t)E << 23) | 0x7FFFFFu;
+                    for (int i = 0; i < 2; ++i) rises |= fmaxf(s[j][i], s[j][i + 2]) > bar[j][i];
+                if (__any_sync(0xffffffffu, rises || beyond)) {
+                    float2 by[NT][NGP];                                         // what the output is multiplied by
+                    bool scale_output = __any_sync(0xffffffffu, rises);
 #pragma unroll
                     for (int j = 0; j < NT; ++j) {
-                        float f[2];
+                        float f[2] = {1.f, 1.f};
+                        if (scale_output)
 #pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            float t = fmaxf(s[j][i], s[j][i + 2]) * q_mul[j][i];
-                            t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 4));
-                            t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 8));
-                            t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 16));
-                            t = fmaxf(t, m[j][i]);
-                            f[i] = ex2(m[j][i] - t);
-                            m[j][i] = t;
-                            // rounded down twice, so that a score up to the bar lies no more than the slack above t once it has been
-                            // multiplied and rounded (to nearest, scores of 3e7 could lie 8 above); a scale of zero: beyond reach
-                            bar[j][i] = __fdiv_rd(__fadd_rd(t, M_SLACK), q_mul[j][i]);
-                            l[j][i] *= f[i];
+                            for (int i = 0; i < 2; ++i) {
+                                float t = fmaxf(s[j][i], s[j][i + 2]) * q_mul[j][i];
+                                t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 4));
+                                t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 8));
+                                t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 16));
+                                t = fmaxf(t, m[j][i]);
+                                f[i] = ex2(m[j][i] - t);
+                                m[j][i] = t;
+                                beyond |= t - (i ? mine.m[j].y : mine.m[j].x) > (float)UNIT_LAG<TERMS>;
+                                // (t + slack) / q_mul, less what its roundings can add (1.5 2^-23 of the reciprocal and product): a score up to
+                                // the bar lies no more than the slack above t once it has been multiplied and rounded (a quotient to nearest
+                                // let scores of 3e7 lie 8 above); a scale of zero: beyond reach
+                                const float over = __fadd_rd(t, M_SLACK) * rcp(q_mul[j][i]);
+                                bar[j][i] = fmaf(fabsf(over), -4.76837158203125e-07f, over);
+                                l[j][i] *= f[i];
 #pragma unroll
-                            for (int g = 0; g < NGP; ++g) z[j][g][i] *= f[i];
-                        }
+                                for (int g = 0; g < NGP; ++g) z[j][g][i] *= f[i];
+                            }
 #pragma unroll
-                        for (int i = 0; i < 2 * NG; ++i)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) o[j][i][e] *= f[e & 1] * fe;
+                        for (int g = 0; g < NGP; ++g) by[j][g] = make_float2(f[0], f[1]);
                     }
+                    if (__any_sync(0xffffffffu, beyond)) {
+                        // A maximum has risen by 2^up since its column's units were set, so what was added up weighs less by that and the
+                        // units may grow; then these rows hold them down: the largest scale of the sixteen becomes 2^11 .. 2^12, as long as
+                        // it is no more than 2^UNIT_WINDOW times the largest p scale, else that limit does.  Where nothing of that changes
+                        // a unit (scales beyond the limit that draw next to no weight) this ends early.
+                        constexpr int N = 2 * NT * NGP;
+                        float v[N];
+                        int up[NT][2];
+                        beyond = false;
+#pragma unroll
+                        for (int j = 0; j < NT; ++j)
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) {
+                                const float t = m[j][i], rise = fminf(floorf(t - (i ? mine.m[j].y : mine.m[j].x)), 512.f);
+                                const float pa = ex2(__fmul_rn(s[j][i], q_mul[j][i]) - t), pb = ex2(__fmul_rn(s[j][i + 2], q_mul[j][i]) - t);
+                                up[j][i] = (int)rise;
+                                beyond |= rise > (float)UNIT_LAG<TERMS>;
+#pragma unroll
+                                for (int g = 0; g < NGP; ++g) {
+                                    const int n = (j * NGP + g) * 2 + i;
+                                    v[n] = fmaxf(pa * fabsf(kv4_scale(wa[g])), pb * fabsf(kv4_scale(wb[g])));
+                                    beyond |= v[n] * (i ? mine.of[j][g].y : mine.of[j][g].x) >= 4096.f / (1 << UNIT_WINDOW<TERMS>);
+                                }
+                            }
+                        if (__any_sync(0xffffffffu, beyond)) {
+                            // The largest are reduced and scattered over the lanes r: lane r ends up with the unit of index r (modulo their
+                            // number; r and r + 8 of sixteen), in the order of `of`.
+                            scale_output = true;
+#pragma unroll
+                            for (int g = 0; g < NGP; ++g) {
+                                float top = fmaxf(fabsf(kv4_scale(wa[g])), fabsf(kv4_scale(wb[g])));
+                                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
+                                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
+                                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+#pragma unroll
+                                for (int j = 0; j < NT; ++j)
+#pragma unroll
+                                    for (int i = 0; i < 2; ++i) {
+                                        const int n = (j * NGP + g) * 2 + i;
+                                        v[n] = fminf(v[n] * (1 << UNIT_WINDOW<TERMS>), top);
+                                    }
+                            }
+                            if (r == 0)
+#pragma unroll
+                                for (int j = 0; j < NT; ++j) {
+                                    float2 was = mine.m[j];
+                                    was.x = up[j][0] < 512 ? was.x + (float)up[j][0] : m[j][0];
+                                    was.y = up[j][1] < 512 ? was.y + (float)up[j][1] : m[j][1];
+                                    mine.m[j] = was;
+                                }
+#pragma unroll
+                            for (int o = 1, n = N; o < 8; o <<= 1, n = n > 1 ? n / 2 : 1) {
+                                const bool odd = r & o;
+                                if (n == 1) v[0] = fmaxf(v[0], __shfl_xor_sync(0xffffffffu, v[0], 4 * o));
+                                else
+#pragma unroll
+                                    for (int k = 0; k < n / 2; ++k) {
+                                        const float keep = odd ? v[2 * k + 1] : v[2 * k], send = odd ? v[2 * k] : v[2 * k + 1];
+                                        v[k] = fmaxf(keep, __shfl_xor_sync(0xffffffffu, send, 4 * o));
+                                    }
+                            }
+#pragma unroll
+                            for (int k = 0; k < (N > 8 ? N / 8 : 1); ++k) {
+                                const int n = 8 * k + (N < 8 ? r % N : r), j = NT == 1 ? 0 : n / (2 * NGP);
+                                float *unit = (float *)mine.of + n;
+                                int rise = n & 1 ? up[0][1] : up[0][0];
+                                if (NT == 2 && j == 1) rise = n & 1 ? up[NT - 1][1] : up[NT - 1][0];
+                                const int was = (int)(__float_as_uint(*unit) >> 23), now = min(min(was + rise, UNIT_MAX), 265 - (int)(__float_as_uint(v[k]) >> 23));
+                                ((float *)mine.change)[n] = __uint_as_float((uint32_t)max(127 + min(now - was, 127), 0) << 23);
+                                __syncwarp();
+                                *unit = __uint_as_float((uint32_t)now << 23);
+                            }
+                            __syncwarp();
+#pragma unroll
+                            for (int g = 0; g < NGP; ++g) {
+                                float most = 0.f;
+#pragma unroll
+                                for (int j = 0; j < NT; ++j) {
+                                    by[j][g].x *= mine.change[j][g].x;
+                                    by[j][g].y *= mine.change[j][g].y;
+                                    most = fmaxf(most, fmaxf(mine.of[j][g].x, mine.of[j][g].y));
+                                }
+                                if (r == 0) mine.limit[g] = 0x84FFFFFFu - __float_as_uint(most);     // exponent 265 - the largest's, all ones behind
+                            }
+                            __syncwarp();
+                        }
+                    }
+                    if (scale_output)
+#pragma unroll
+                        for (int j = 0; j < NT; ++j)
+#pragma unroll
+                            for (int q = 0; q < NG; ++q)                        // with PACK 2 a lane's values of the other half's groups are not used
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) {
+                                    o[j][2 * q][e] *= e & 1 ? by[j][q / RPG % NGP].y : by[j][q / RPG % NGP].x;
+                                    o[j][2 * q + 1][e] *= e & 1 ? by[j][q / RPG % NGP].y : by[j][q / RPG % NGP].x;
+                                }
                 }
-                const float e_mul = __uint_as_float(0x84800000u - ((uint32_t)E << 23));        // 2^(11 - exponent): 265 - E in the exponent's bits
                 float p[NT][4];
 #pragma unroll
                 for (int j = 0; j < NT; ++j)
@@ -532,15 +662,16 @@ kv4_attn_kernel(const AttnArgs a) {
                 load_words<NV>(vrow + (vb + 8) * (D / 2), v3);
 #pragma unroll
                 for (int g = 0; g < NGP; ++g) {
-                    const float ua = kv4_scale(wa[g]), ub = kv4_scale(wb[g]), sa = ua * e_mul, sb = ub * e_mul;
+                    const float ua = kv4_scale(wa[g]), ub = kv4_scale(wb[g]);
                     const float za = fmaf(8.f, ua, kv4_zero(wa[g])), zb = fmaf(8.f, ub, kv4_zero(wb[g]));
                     uint32_t pb[NT][TERMS][2];
 #pragma unroll
                     for (int j = 0; j < NT; ++j) {
+                        const float2 unit = mine.of[j][g];
                         float w[4];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            w[e] = p[j][e] * (e < 2 ? sa : sb);
+                        for (int e = 0; e < 4; ++e) {                           // p times scale first: scale times unit may be infinite where p is tiny
+                            w[e] = p[j][e] * (e < 2 ? ua : ub) * (e & 1 ? unit.y : unit.x);
                             z[j][g][e & 1] = fmaf(p[j][e], e < 2 ? za : zb, z[j][g][e & 1]);
                         }
                         uint32_t h0[TERMS], h1[TERMS];
@@ -608,7 +739,6 @@ kv4_attn_kernel(const AttnArgs a) {
 
         // the warp's sums over its lanes, its output in true units: [column][element] in its own ring
         float *wo = (float *)ring;
-        const float e_out = __uint_as_float((uint32_t)(E - 11) << 23);          // 2^(exponent - 11)
 #pragma unroll
         for (int j = 0; j < NT; ++j)
 #pragma unroll
@@ -625,6 +755,8 @@ kv4_attn_kernel(const AttnArgs a) {
                 for (int q = 0; q < NG; ++q) {
                     if (PACK == 2 && q / RPG / NGP != half) continue;           // the other half's columns hold these groups
                     const float zq = z[j][q / RPG % NGP][i], f1 = 0.0625f;
+                    const float2 unit = mine.of[j][q / RPG % NGP];
+                    const float e_out = __uint_as_float(0x7F000000u - __float_as_uint(i ? unit.y : unit.x));        // 1 / unit
                     *(float4 *)(wo + cc * D + 32 * q + 4 * r) =
                         make_float4(fmaf(o[j][2 * q][i], e_out, zq), fmaf(o[j][2 * q][i + 2] * f1, e_out, zq),
                                     fmaf(o[j][2 * q + 1][i], e_out, zq), fmaf(o[j][2 * q + 1][i + 2] * f1, e_out, zq));

@@ -319,6 +319,67 @@ def test_attention_of_scores_whose_neighbours_lie_far_apart(ctx, dtype, scale, t
     assert np.all((o >= ends.min(0) - tol) & (o <= ends.max(0) + tol))
 
 
+def _values_of_many_sizes(kind, g, n, cap, d, R):
+    """(q [R, d], k [cap, d], v [cap, d]) of one key head; score units are natural."""
+    q, k, v = g.standard_normal((R, d)), 0.3 * g.standard_normal((cap, d)), g.standard_normal((cap, d))
+    q[:, 0], k[:, 0] = np.sqrt(d), 0.0                                           # k[:, 0] is what it adds to the scores
+    t = np.arange(cap)
+    if kind == "unseen":                                                        # huge values that draw no weight, between others
+        k[[3, 100, 101], 0], v[[3, 100, 101]] = -300.0, v[[3, 100, 101]] * 2.0 ** 45
+    elif kind == "outweighed":                                                  # huge values first, all weight on what follows
+        k[16:, 0], v[:16] = 300.0, v[:16] * 2.0 ** 45
+    elif kind == "heads":                                                       # every other head sees the huge values, the rest do not
+        q[1::2, 0] *= -1.0
+        k[[3, 100], 0], v[[3, 100]] = -300.0, v[[3, 100]] * 2.0 ** 40
+    elif kind == "groups":
+        v *= np.exp2(np.repeat([0.0, -45.0, 30.0, -80.0], 32)[:d])
+    elif kind == "falling":                                                     # weights grow as the values shrink
+        k[:, 0], v = 1.1 * t, v * np.exp2(-t)[:, None]
+    elif kind == "rising":                                                      # and the other way round
+        k[:, 0], v = -0.6 * t, v * np.exp2(t / 2.0 + t % 3)[:, None]
+    elif kind == "constant":                                                    # rows of equal elements: scale 0, with rising scores
+        k[20:, 0], v[20:] = 2.5 * (t[20:, None] - 19)[:, 0], np.float32(0.5)
+    elif kind == "tiny":
+        v *= 2.0 ** -115
+    elif kind == "largest":
+        v *= 2.0 ** 122
+    return q, k, v
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,group,R", [(64, 32, 4), (128, 32, 4), (128, 64, 8), (64, 64, 2), (128, 128, 1), (128, 32, 12)])
+@pytest.mark.parametrize("kind", ["unseen", "outweighed", "heads", "groups", "falling", "rising", "constant", "tiny", "largest"])
+def test_attention_of_values_of_many_sizes(ctx, dtype, d, group, R, kind):
+    """The bound holds for each query row and group by itself: what draws no weight, and what other groups and other heads see, adds
+    nothing to it.  With S = sum p scale and G = sum p max |v| of the row's softmax and the group: rel (as above, of every weight) of
+    the two sums that make up the output, |zero + 8 scale| and |scale (c - 8)| <= 2.2 max |v|; half a step of the fp16 factors (2^-11,
+    or 2^-22 for two) times at most 8; and for factors so small that fp16 holds them with fewer bits half its smallest
+    step, 2^-25, each.  The largest p scale met is 2^11 of a unit when that is set, less a window of 2^12 (two factors: 2^8) that larger
+    scales of other rows have, and the maximum may rise by 2^5 (2^4) before it is set anew: 2^-6 (2^-1) is the least it can be."""
+    n, cap = 200, 208
+    g = np.random.default_rng([d, group, R, len(kind), ord(kind[0])])
+    q, k, v = _values_of_many_sizes(kind, g, n, cap, d, R)
+    f = Filled(g, [n], cap, 1, d, group, k=k.astype(np.float32)[None, None], v=v.astype(np.float32)[None, None])
+    q = inputs.to_grid(q.astype(np.float32)[None, None], dtype)
+    scale = d ** -0.5
+    w_out = torch.zeros(1, 1, cap, device="cuda")
+    o = binding.str_kv4_attn(ctx, f.cache, dev(q, dtype), _i32([n]), scale, weight_out=w_out).float().cpu().numpy()[0, 0]
+    o2 = binding.str_kv4_attn(ctx, f.cache, dev(q, dtype), _i32([n]), scale).float().cpu().numpy()[0, 0]
+    ctx.check_status()
+    assert np.array_equal(o, o2)
+    K, V, sc = f.k[0, 0, :n], f.v[0, 0, :n], f.v_scale[0, 0, :n].astype(np.float64)
+    gmax = np.abs(V).reshape(n, -1, group).max(2)
+    for r in range(R):
+        s = K @ q[0, 0, r].astype(np.float64) * scale
+        p = np.exp(s - s.max())
+        p /= p.sum()
+        rel = 2 * (d + 64) * E * scale * (np.abs(K) @ np.abs(q[0, 0, r]).astype(np.float64)).max() + (32 + n) * E
+        bound = 2.2 * rel * (p @ gmax) + (2.0 ** -11 if dtype == "bf16" else 2.0 ** -22) * 8 * (p @ sc) + n * 2.0 ** (-19 if dtype == "bf16" else -24) * 8 * (p[:, None] * sc).max(0)
+        ref = p @ V
+        bound = np.repeat(bound, group) + HALF[dtype] * np.abs(ref) + 2.0 ** -133                      # bf16 holds multiples of that
+        assert np.all(np.abs(o[r] - ref) <= bound), (r, float((np.abs(o[r] - ref) / bound).max()))
+
+
 def test_attention_scores_that_grow_along_the_row(ctx):
     """Every later row beats all before it: the running maximum moves all the way."""
     d, n, Hkv, Hq = 128, 1000, 1, 4
