@@ -312,7 +312,6 @@ kv4_read_kernel(int cap, int n_out, const int32_t *__restrict__ row_start, const
 extern "C" int str_kv4_append(str_ctx *ctx, const str_kv4_shape *s, int dtype, int T_new, const void *k, const void *v,
                               const int32_t *positions, const int32_t *row_start, const int32_t *n_new,
                               const str_kv4_cache *cache, void *stream) {
-    StrProfScope prof_scope(ctx, STR_CAT_ELEMENTWISE, stream);
     if (!ctx || T_new < 0 || (dtype != STR_F32 && dtype != STR_BF16)) return STR_ERR_INVALID_ARG;
     const int rc = kv4_check_shape(s);
     if (rc != STR_OK) return rc;
@@ -321,6 +320,7 @@ extern "C" int str_kv4_append(str_ctx *ctx, const str_kv4_shape *s, int dtype, i
     if (!k || !v || !row_start || (((uintptr_t)k | (uintptr_t)v) & 15)) return STR_ERR_INVALID_ARG;
     StrDeviceScope dev(ctx);
     if (!dev.ok) return STR_ERR_CUDA;
+    StrProfScope prof_scope(ctx, STR_CAT_ELEMENTWISE, stream);
     const dim3 grid(ceil_div(T_new, KV4_THREADS / (s->d / 8) * KV4_UNROLL), s->Hkv, s->Bz);
 #define KV4_CALL(T, D, G)                                                                                              \
     kv4_append_kernel<T, D, G><<<grid, KV4_THREADS, 0, (cudaStream_t)stream>>>(s->cap, T_new, (const T *)k, (const T *)v, positions, \
@@ -332,7 +332,6 @@ extern "C" int str_kv4_append(str_ctx *ctx, const str_kv4_shape *s, int dtype, i
 
 extern "C" int str_kv4_read(str_ctx *ctx, const str_kv4_shape *s, int dtype, int n_out, const int32_t *row_start,
                             const int32_t *n_rows, const str_kv4_cache *cache, void *k_out, void *v_out, void *stream) {
-    StrProfScope prof_scope(ctx, STR_CAT_ELEMENTWISE, stream);
     if (!ctx || n_out < 0 || (dtype != STR_F32 && dtype != STR_BF16)) return STR_ERR_INVALID_ARG;
     const int rc = kv4_check_shape(s);
     if (rc != STR_OK) return rc;
@@ -341,6 +340,7 @@ extern "C" int str_kv4_read(str_ctx *ctx, const str_kv4_shape *s, int dtype, int
     if (!k_out || !v_out || !row_start || (((uintptr_t)k_out | (uintptr_t)v_out) & 15)) return STR_ERR_INVALID_ARG;
     StrDeviceScope dev(ctx);
     if (!dev.ok) return STR_ERR_CUDA;
+    StrProfScope prof_scope(ctx, STR_CAT_ELEMENTWISE, stream);
     const dim3 grid(ceil_div(n_out, KV4_THREADS / (s->d / 8) * KV4_UNROLL), s->Hkv, s->Bz);
 #define KV4_CALL(T, D, G)                                                                                              \
     kv4_read_kernel<T, D, G><<<grid, KV4_THREADS, 0, (cudaStream_t)stream>>>(s->cap, n_out, row_start, n_rows, *cache, \

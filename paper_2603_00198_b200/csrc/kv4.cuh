@@ -10,7 +10,8 @@
 #pragma once
 #include "common.cuh"
 
-// Makes the context's device current for the launches of one call and puts the caller's back.
+// Makes the context's device current for the launches of one call and puts the caller's back.  Comes before the call's StrProfScope:
+// its events are made on, and recorded on a stream of, the current device.
 struct StrDeviceScope {
     int prev;
     bool ok;

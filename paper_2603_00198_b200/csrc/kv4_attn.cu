@@ -16,7 +16,6 @@ extern "C" size_t str_kv4_attn_workspace_size(const str_kv4_shape *s, int Hq, in
 extern "C" int str_kv4_attn(str_ctx *ctx, const str_kv4_shape *s, int dtype, int Hq, int n_q, const void *q, const str_kv4_cache *cache,
                             const int32_t *lens, float softmax_scale, void *o, float *weight_out, void *workspace,
                             size_t workspace_bytes, void *stream) {
-    StrProfScope prof_scope(ctx, STR_CAT_ATTN_FWD, stream);
     if (!ctx || n_q < 0 || (dtype != STR_F32 && dtype != STR_BF16)) return STR_ERR_INVALID_ARG;
     const int rc = kv4_check_shape(s);
     if (rc != STR_OK) return rc;
@@ -31,6 +30,7 @@ extern "C" int str_kv4_attn(str_ctx *ctx, const str_kv4_shape *s, int dtype, int
     if (workspace_bytes < w.bytes) return STR_ERR_WORKSPACE_TOO_SMALL;
     StrDeviceScope dev(ctx);
     if (!dev.ok) return STR_ERR_CUDA;
+    StrProfScope prof_scope(ctx, STR_CAT_ATTN_FWD, stream);
     const int C = n_q * (Hq / s->Hkv), cols = kv4_attn::unit_columns(s, C);
     const int G = min(ctx->sm_count * (cols <= 8 ? 2 : 1), kv4_attn::AT_MAX_GRID);
     char *base = (char *)workspace;

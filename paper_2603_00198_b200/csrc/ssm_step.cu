@@ -121,7 +121,6 @@ void dispatch_step(const str_ssd_shape *s, const void *x, const float *dt, const
 
 extern "C" int str_mamba2_step(str_ctx *ctx, const str_ssd_shape *s, const void *x, const float *dt, const float *A, const void *B,
                                const void *C, const float *D, const float *state, void *y, float *state_out, void *stream) {
-    StrProfScope prof_scope(ctx, STR_CAT_SSD, stream);
     if (!ctx || !s || !x || !dt || !A || !B || !C || !state || !y || !state_out) return STR_ERR_INVALID_ARG;
     if (s->Bz <= 0 || s->T <= 0 || s->H <= 0 || s->p <= 0 || s->n <= 0 || s->G <= 0 || s->H % s->G != 0 ||
         (s->dtype != STR_F32 && s->dtype != STR_BF16))
@@ -131,6 +130,7 @@ extern "C" int str_mamba2_step(str_ctx *ctx, const str_ssd_shape *s, const void 
     if (s->n > 512 || s->Bz > 65535 || s->H > 65535) return STR_ERR_UNSUPPORTED_SHAPE;
     StrDeviceScope dev(ctx);
     if (!dev.ok) return STR_ERR_CUDA;
+    StrProfScope prof_scope(ctx, STR_CAT_SSD, stream);
     if (s->dtype == STR_BF16) dispatch_step<__nv_bfloat16>(s, x, dt, A, B, C, D, state, state_out, y, (cudaStream_t)stream);
     else dispatch_step<float>(s, x, dt, A, B, C, D, state, state_out, y, (cudaStream_t)stream);
     return str_launch_ok(ctx);
