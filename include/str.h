@@ -378,7 +378,8 @@ typedef struct {
  * value <= the minimum, scale = bf16((max - zero) * fp32(1/15)), code = clamp(rint((x - zero) / scale), 0, 15); a group with a NaN
  * or an infinity (or a range beyond fp32) reads back as NaN.  Stored rows start with weight 0; with `positions`
  * (device [Bz,T_new] int32, or NULL) their ids go to cache->pos.
- * A row outside [0,cap) is not stored, and STR_ERR_INVALID_ARG is recorded for str_check_status (later calls run on).
+ * A row outside [0,cap) is not stored, a count outside [0,T_new] is held to that range, and STR_ERR_INVALID_ARG is recorded for
+ * str_check_status (later calls run on).
  * The rows of one call must not overlap.  Errors: INVALID_ARG, UNSUPPORTED_SHAPE. */
 int str_kv4_append(str_ctx *ctx, const str_kv4_shape *s, int dtype, int T_new, const void *k, const void *v,
                    const int32_t *positions, const int32_t *row_start, const int32_t *n_new, const str_kv4_cache *cache,
@@ -386,7 +387,8 @@ int str_kv4_append(str_ctx *ctx, const str_kv4_shape *s, int dtype, int T_new, c
 
 /* Rows back out, as str_attn_prefill_rows takes keys and values: k_out, v_out device [Bz,n_out,Hkv,d] dtype, token j of
  * sequence b from cache row row_start[b] + j for j < n_rows[b] (NULL: all), zeros behind it.  zero + scale * code is formed
- * in fp32 and rounded to dtype once.  Rows outside [0,cap) give zeros and are recorded as above. */
+ * in fp32 and rounded to dtype once.  Rows outside [0,cap) give zeros, counts outside [0,n_out] are held to that; both are recorded
+ * as above. */
 int str_kv4_read(str_ctx *ctx, const str_kv4_shape *s, int dtype, int n_out, const int32_t *row_start, const int32_t *n_rows,
                  const str_kv4_cache *cache, void *k_out, void *v_out, void *stream);
 

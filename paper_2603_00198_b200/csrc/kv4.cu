@@ -196,7 +196,7 @@ kv4_append_kernel(int cap, int T_new, const T *__restrict__ k, const T *__restri
     constexpr int LPR = D / 8, NG = D / 32, ROWS = KV4_THREADS / LPR;
     const int h = blockIdx.y, b = blockIdx.z, Hkv = gridDim.y;
     const int l = threadIdx.x % LPR, g = l >> 2, c = l & 3;
-    const int n = n_new ? min(n_new[b], T_new) : T_new, start = row_start[b];
+    const int n = kv4_tokens(n_new, b, T_new, status), start = row_start[b];
     const long long src = ((long long)b * T_new * Hkv + h) * D + 8 * l, dst = ((long long)b * Hkv + h) * cap;
     const int t0 = blockIdx.x * (ROWS * KV4_UNROLL) + threadIdx.x / LPR;
     Kv4Raw8<T> raw[2 * KV4_UNROLL];                                             // k, v, k, v .. as stored: widened only when their turn comes
@@ -254,7 +254,7 @@ kv4_read_kernel(int cap, int n_out, const int32_t *__restrict__ row_start, const
     constexpr int LPR = D / 8, NG = D / 32, ROWS = KV4_THREADS / LPR;
     const int h = blockIdx.y, b = blockIdx.z, Hkv = gridDim.y;
     const int l = threadIdx.x % LPR, g = l >> 2, c = l & 3;
-    const int n = n_rows ? n_rows[b] : n_out, start = row_start[b];
+    const int n = kv4_tokens(n_rows, b, n_out, status), start = row_start[b];
     const long long base = ((long long)b * Hkv + h) * cap, out = ((long long)b * n_out * Hkv + h) * D + 8 * l;
     const int t0 = blockIdx.x * (ROWS * KV4_UNROLL) + threadIdx.x / LPR;
     uint32_t ck[KV4_UNROLL], cv[KV4_UNROLL], wk[KV4_UNROLL], wv[KV4_UNROLL];
@@ -263,7 +263,7 @@ kv4_read_kernel(int cap, int n_out, const int32_t *__restrict__ row_start, const
         const int t = t0 + i * ROWS;
         const long long row = (long long)start + t;
         ck[i] = cv[i] = wk[i] = wv[i] = 0u;                                     // reads as zero
-        if (t >= n_out || t >= n) continue;
+        if (t >= n) continue;
         if (row < 0 || row >= cap) {
             kv4_report(status);
             continue;

@@ -195,6 +195,29 @@ def test_append_and_read_outside_the_capacity_are_skipped_and_reported(ctx):
     assert np.array_equal(k[:, :, 0, 0].cpu().numpy(), [[1, 1, 0, 0], [0, 0, 1, 1]])
 
 
+@pytest.mark.parametrize("counts", [[5, 2], [2, -1], [-(1 << 31), (1 << 31) - 1]])
+def test_counts_of_append_and_read_outside_their_range_are_held_to_it_and_reported(ctx, counts):
+    cache = binding.Kv4Cache.empty(ctx, 2, 32, 3, 64, 32)
+    x = dev(np.ones((2, 4, 3, 64), dtype=np.float32))
+    held = [min(max(n, 0), 4) for n in counts]
+    binding.str_kv4_append(ctx, cache, x, x, _i32([3, 8]), n_new=_i32(counts))
+    with pytest.raises(binding.StrError) as e:
+        ctx.check_status()
+    assert e.value.code == -1
+    used = (cache.k_scales[:, :, :, 0] != 0).cpu().numpy()
+    for b, start in enumerate((3, 8)):
+        assert all(np.flatnonzero(used[b, h]).tolist() == list(range(start, start + held[b])) for h in range(3))
+    binding.str_kv4_append(ctx, cache, x, x, _i32([3, 8]), n_new=_i32([4, 0]))
+    binding.str_kv4_append(ctx, cache, x, x, _i32([3, 8]))
+    ctx.check_status()                                              # 0 and T_new are inside
+    k, _ = binding.str_kv4_read(ctx, cache, _i32([3, 8]), 4, torch.float32, n_rows=_i32(counts))
+    with pytest.raises(binding.StrError):
+        ctx.check_status()
+    assert np.array_equal((k[:, :, 1, 0] == 1).sum(1).cpu().numpy(), held) and np.array_equal((k != 0).sum((1, 2, 3)).cpu().numpy(), [64 * 3 * n for n in held])
+    binding.str_kv4_read(ctx, cache, _i32([3, 8]), 4, torch.float32, n_rows=_i32([4, 0]))
+    ctx.check_status()
+
+
 # ---------------------------------------------------------------- attention
 def _attention_reference(f, q, scale):
     """(o, drawn, bound of o without the output rounding, bound of drawn) per sequence."""
