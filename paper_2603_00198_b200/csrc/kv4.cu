@@ -196,7 +196,7 @@ kv4_append_kernel(int cap, int T_new, const T *__restrict__ k, const T *__restri
     constexpr int LPR = D / 8, NG = D / 32, ROWS = KV4_THREADS / LPR;
     const int h = blockIdx.y, b = blockIdx.z, Hkv = gridDim.y;
     const int l = threadIdx.x % LPR, g = l >> 2, c = l & 3;
-    const int n = kv4_tokens(n_new, b, T_new, status), start = row_start[b];
+    const int n = n_new ? min(n_new[b], T_new) : T_new, start = row_start[b];
     const long long src = ((long long)b * T_new * Hkv + h) * D + 8 * l, dst = ((long long)b * Hkv + h) * cap;
     const int t0 = blockIdx.x * (ROWS * KV4_UNROLL) + threadIdx.x / LPR;
     Kv4Raw8<T> raw[2 * KV4_UNROLL];                                             // k, v, k, v .. as stored: widened only when their turn comes
@@ -216,6 +216,7 @@ kv4_append_kernel(int cap, int T_new, const T *__restrict__ k, const T *__restri
         }
         any |= live[i];
     }
+    if (n_new && blockIdx.x == 0 && h == 0 && threadIdx.x == 0 && (n_new[b] < 0 || n_new[b] > T_new)) kv4_report(status);       // behind the loads: in front 3 %
     static_assert(ROWS * KV4_UNROLL <= KV4_THREADS, "one thread a token");
     if (threadIdx.x < ROWS * KV4_UNROLL) {  // weights and positions: one store for all tokens of the block (one a token: +8 %)
         const int t = blockIdx.x * (ROWS * KV4_UNROLL) + threadIdx.x;
@@ -246,6 +247,14 @@ kv4_append_kernel(int cap, int T_new, const T *__restrict__ k, const T *__restri
     }
 }
 
+// Tokens of a sequence: what the caller says (NULL: all `most`), held to [0, most]; a value outside is recorded by its first block.
+__device__ __forceinline__ int tokens(const int32_t *counts, int b, int most, int *status) {
+    if (!counts) return most;
+    const int n = counts[b];
+    if ((n < 0 || n > most) && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) kv4_report(status);
+    return min(max(n, 0), most);
+}
+
 // Grid (token blocks, Hkv, Bz).
 template <typename T, int D, int GROUP>
 __global__ void __launch_bounds__(KV4_THREADS)
@@ -254,7 +263,7 @@ kv4_read_kernel(int cap, int n_out, const int32_t *__restrict__ row_start, const
     constexpr int LPR = D / 8, NG = D / 32, ROWS = KV4_THREADS / LPR;
     const int h = blockIdx.y, b = blockIdx.z, Hkv = gridDim.y;
     const int l = threadIdx.x % LPR, g = l >> 2, c = l & 3;
-    const int n = kv4_tokens(n_rows, b, n_out, status), start = row_start[b];
+    const int n = tokens(n_rows, b, n_out, status), start = row_start[b];
     const long long base = ((long long)b * Hkv + h) * cap, out = ((long long)b * n_out * Hkv + h) * D + 8 * l;
     const int t0 = blockIdx.x * (ROWS * KV4_UNROLL) + threadIdx.x / LPR;
     uint32_t ck[KV4_UNROLL], cv[KV4_UNROLL], wk[KV4_UNROLL], wv[KV4_UNROLL];

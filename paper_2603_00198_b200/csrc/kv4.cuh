@@ -72,15 +72,6 @@ __device__ __forceinline__ void kv4_load8(const T *p, float (&x)[8]) { kv4_widen
 // makes the tensor-core kernels of the context leave at once; a wrong count is no reason for that.)
 __device__ __forceinline__ void kv4_report(int *status) { atomicCAS(status + 1, 0, STR_ERR_INVALID_ARG); }
 
-// Tokens of a sequence that append and read take: what the caller says (NULL: all `most`), held to [0, most]; a value outside is
-// recorded, by the sequence's first block.
-__device__ __forceinline__ int kv4_tokens(const int32_t *counts, int b, int most, int *status) {
-    if (!counts) return most;
-    const int n = counts[b];
-    if ((n < 0 || n > most) && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) kv4_report(status);
-    return min(max(n, 0), most);
-}
-
 // Row count of a sequence as the kernels use it: what the caller says, held to [0, cap]; a value outside is recorded.
 __device__ __forceinline__ int kv4_len(const int32_t *lens, int b, int cap, int *status) {
     const int n = lens[b];
