@@ -396,7 +396,7 @@ int str_kv4_read(str_ctx *ctx, const str_kv4_shape *s, int dtype, int n_out, con
  *   o[i] = sum_t softmax_t(q_i . k_t * softmax_scale) v_t over the rows t <= lens[b] - n_q + i,
  * k, v the values the codes stand for.  q, o device [Bz,n_q,Hq,d] dtype; lens device [Bz] int32, rows in use.  A token with
  * no row to see (an empty sequence; lens[b] < n_q) gives zeros.  A count outside [0,cap] is held to that range and recorded
- * as above.  Meant for few tokens (every 16 query rows of a key head read the cache once); for long
+ * as above.  A softmax_scale that is not finite, or not once multiplied by log2(e), is refused (INVALID_ARG).  Meant for few tokens (every 16 query rows of a key head read the cache once); for long
  * prompts use str_kv4_read and str_attn_prefill_rows.
  *   weight_out  device [Bz,Hkv,cap] fp32 or NULL: weight_out[b,h,t] = cache->weight[b,h,t] + the softmax weights that the
  *               n_q tokens' query heads of key head h put on row t, for t < lens[b]; other rows are left as they are.  May be

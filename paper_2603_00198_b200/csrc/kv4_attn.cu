@@ -1,4 +1,6 @@
 // str_kv4_attn: argument checks, workspace and the choice of kernel (kernels in kv4_attn.cuh, built per storage type).
+#include <cmath>
+
 #include "kv4_attn.cuh"
 
 using kv4_attn::AttnArgs;
@@ -20,6 +22,8 @@ extern "C" int str_kv4_attn(str_ctx *ctx, const str_kv4_shape *s, int dtype, int
     const int rc = kv4_check_shape(s);
     if (rc != STR_OK) return rc;
     if (Hq <= 0 || Hq % s->Hkv != 0 || !kv4_pointers_ok(cache) || !lens || (weight_out && !cache->weight)) return STR_ERR_INVALID_ARG;
+    // (fmaxf in the kernel would make a NaN scale a scale of zero)
+    if (!std::isfinite(softmax_scale * kv4_attn::LOG2E)) return STR_ERR_INVALID_ARG;
     if (n_q == 0) return STR_OK;
     if (!q || !o || ((uintptr_t)q & 15)) return STR_ERR_INVALID_ARG;
     const size_t weight_bytes = (size_t)s->Bz * s->Hkv * s->cap * sizeof(float);
@@ -34,7 +38,7 @@ extern "C" int str_kv4_attn(str_ctx *ctx, const str_kv4_shape *s, int dtype, int
     const int C = n_q * (Hq / s->Hkv), cols = kv4_attn::unit_columns(s, C);
     const int G = min(ctx->sm_count * (cols <= 8 ? 2 : 1), kv4_attn::AT_MAX_GRID);
     char *base = (char *)workspace;
-    AttnArgs a = {s->Bz, s->cap, s->Hkv, Hq, n_q, ceil_div(C, cols), q, lens, softmax_scale * 1.4426950408889634f, *cache, o,
+    AttnArgs a = {s->Bz, s->cap, s->Hkv, Hq, n_q, ceil_div(C, cols), q, lens, softmax_scale * kv4_attn::LOG2E, *cache, o,
                   (float *)(base + w.part), (float2 *)(base + w.part_ml), weight_out ? (float *)(base + w.scores) : nullptr,
                   weight_out ? (float2 *)(base + w.stats) : nullptr, ctx->status_dev};
     cudaStream_t st = (cudaStream_t)stream;

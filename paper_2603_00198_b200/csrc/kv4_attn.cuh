@@ -42,6 +42,7 @@
 
 namespace kv4_attn {
 
+constexpr float LOG2E = 1.4426950408889634f;
 constexpr int AT_TILE = 32;              // rows of a warp's tile
 constexpr int AT_STAGES = 2;             // tiles in flight per warp
 constexpr int WT_THREADS = 256;
