@@ -418,7 +418,7 @@ int str_kv4_attn(str_ctx *ctx, const str_kv4_shape *s, int dtype, int Hq, int n_
  * Their codes, scales, weights and positions are copied bit for bit, in row order, to the rows 0 .. of `out`, a cache of
  * the same Bz, Hkv, d, group and capacity cap_out >= keep; rows of `out` behind them are left as they were.
  *   lens_out device [Bz] int32; kept_idx_out device [Bz,keep] int32, ascending, -1 behind the last.
- * `out` shares no memory with `cache`.  out->weight and out->pos may be NULL (not copied).
+ * What is written (`out`, lens_out, kept_idx_out) shares no memory with what is read, nor with one another.  out->weight and out->pos may be NULL (not copied).
  * Workspace: none for capacities of up to 131072 rows, beyond that size from the query, 256-byte aligned.
  * Errors: INVALID_ARG (keep > cap, keep > cap_out, n_recent > keep, shared buffers), UNSUPPORTED_SHAPE, WORKSPACE_TOO_SMALL. */
 size_t str_kv4_evict_workspace_size(const str_kv4_shape *s, int keep);

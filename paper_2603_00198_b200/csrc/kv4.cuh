@@ -41,7 +41,7 @@ static inline bool kv4_pointers_ok(const str_kv4_cache *c) {
 
 // Do two buffers share memory?
 static inline bool kv4_overlap(const void *a, size_t na, const void *b, size_t nb) {
-    return a && b && (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
+    return a && b && na && nb && (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
 }
 
 __device__ __forceinline__ float kv4_scale(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }

@@ -292,15 +292,22 @@ extern "C" int str_kv4_evict(str_ctx *ctx, const str_kv4_shape *s, const str_kv4
     const int rc = kv4_check_shape(s);
     if (rc != STR_OK) return rc;
     if (!kv4_pointers_ok(cache) || !kv4_pointers_ok(out) || !cache->weight || !lens || !lens_out) return STR_ERR_INVALID_ARG;
-    if ((out->pos && !cache->pos) || lens == lens_out || cap_out <= 0) return STR_ERR_INVALID_ARG;
+    if ((out->pos && !cache->pos) || cap_out <= 0) return STR_ERR_INVALID_ARG;
+    // Every buffer that is written, against every other: rows are read, and counts looked at, while others are written.
     const size_t heads = (size_t)s->Bz * s->Hkv, rows = heads * s->cap, rows_out = heads * cap_out, words = s->d / s->group * 4;
-    if (kv4_overlap(cache->k_codes, rows * (s->d / 2), out->k_codes, rows_out * (s->d / 2)) ||
-        kv4_overlap(cache->v_codes, rows * (s->d / 2), out->v_codes, rows_out * (s->d / 2)) ||
-        kv4_overlap(cache->k_scales, rows * words, out->k_scales, rows_out * words) ||
-        kv4_overlap(cache->v_scales, rows * words, out->v_scales, rows_out * words) ||
-        kv4_overlap(cache->weight, rows * 4, out->weight, rows_out * 4) ||
-        kv4_overlap(cache->pos, (size_t)s->Bz * s->cap * 4, out->pos, (size_t)s->Bz * cap_out * 4))
-        return STR_ERR_INVALID_ARG;
+    const size_t counts = (size_t)s->Bz * sizeof(int32_t);
+    const struct { const void *p; size_t bytes; } read[] = {
+        {cache->k_codes, rows * (s->d / 2)}, {cache->v_codes, rows * (s->d / 2)}, {cache->k_scales, rows * words}, {cache->v_scales, rows * words},
+        {cache->weight, rows * 4}, {cache->pos, (size_t)s->Bz * s->cap * 4}, {lens, counts}, {n_evictable, counts}};
+    const struct { const void *p; size_t bytes; } written[] = {
+        {out->k_codes, rows_out * (s->d / 2)}, {out->v_codes, rows_out * (s->d / 2)}, {out->k_scales, rows_out * words}, {out->v_scales, rows_out * words},
+        {out->weight, rows_out * 4}, {out->pos, (size_t)s->Bz * cap_out * 4}, {lens_out, counts}, {kept_idx_out, keep > 0 ? counts * keep : 0}};
+    for (size_t i = 0; i < sizeof(written) / sizeof(written[0]); ++i) {
+        for (const auto &r : read)
+            if (kv4_overlap(r.p, r.bytes, written[i].p, written[i].bytes)) return STR_ERR_INVALID_ARG;
+        for (size_t j = 0; j < i; ++j)
+            if (kv4_overlap(written[j].p, written[j].bytes, written[i].p, written[i].bytes)) return STR_ERR_INVALID_ARG;
+    }
     if (keep < 0 || keep > s->cap || keep > cap_out || n_recent < 0 || n_recent > keep) return STR_ERR_INVALID_ARG;
     if (cap_out % 16 != 0) return STR_ERR_UNSUPPORTED_SHAPE;
     const bool split = long_rows(s);
