@@ -275,6 +275,17 @@ cudaError_t launch_gather(const str_kv4_shape *s, int cap_out, int keep, bool fi
     return cudaLaunchKernelEx(&cfg, kv4_evict_gather_kernel<D>, s->cap, cap_out, s->d / s->group, keep, fill, kept, lens_out, src, dst);
 }
 
+// Does one of n written buffers share memory with one of m read ones or with another written one?
+struct Buffer { const void *p; size_t bytes; };
+bool any_shared(const Buffer *written, int n, const Buffer *read, int m) {
+    for (int i = 0; i < n; ++i) {
+        for (int j = 0; j < m; ++j)
+            if (kv4_overlap(written[i].p, written[i].bytes, read[j].p, read[j].bytes)) return true;
+        for (int j = 0; j < i; ++j)
+            if (kv4_overlap(written[i].p, written[i].bytes, written[j].p, written[j].bytes)) return true;
+    }
+    return false;
+}
 bool long_rows(const str_kv4_shape *s) { return s->cap > SEL_MAX_ROWS; }
 size_t scores_bytes(const str_kv4_shape *s) { return align_up((size_t)s->Bz * s->cap * sizeof(float), 256); }
 
@@ -293,21 +304,15 @@ extern "C" int str_kv4_evict(str_ctx *ctx, const str_kv4_shape *s, const str_kv4
     if (rc != STR_OK) return rc;
     if (!kv4_pointers_ok(cache) || !kv4_pointers_ok(out) || !cache->weight || !lens || !lens_out) return STR_ERR_INVALID_ARG;
     if ((out->pos && !cache->pos) || cap_out <= 0) return STR_ERR_INVALID_ARG;
-    // Every buffer that is written, against every other: rows are read, and counts looked at, while others are written.
+    // What is written shares no memory with what is read, nor with one another: rows are read, and counts looked at, while others are written.
     const size_t heads = (size_t)s->Bz * s->Hkv, rows = heads * s->cap, rows_out = heads * cap_out, words = s->d / s->group * 4;
     const size_t counts = (size_t)s->Bz * sizeof(int32_t);
-    const struct { const void *p; size_t bytes; } read[] = {
-        {cache->k_codes, rows * (s->d / 2)}, {cache->v_codes, rows * (s->d / 2)}, {cache->k_scales, rows * words}, {cache->v_scales, rows * words},
-        {cache->weight, rows * 4}, {cache->pos, (size_t)s->Bz * s->cap * 4}, {lens, counts}, {n_evictable, counts}};
-    const struct { const void *p; size_t bytes; } written[] = {
-        {out->k_codes, rows_out * (s->d / 2)}, {out->v_codes, rows_out * (s->d / 2)}, {out->k_scales, rows_out * words}, {out->v_scales, rows_out * words},
-        {out->weight, rows_out * 4}, {out->pos, (size_t)s->Bz * cap_out * 4}, {lens_out, counts}, {kept_idx_out, keep > 0 ? counts * keep : 0}};
-    for (size_t i = 0; i < sizeof(written) / sizeof(written[0]); ++i) {
-        for (const auto &r : read)
-            if (kv4_overlap(r.p, r.bytes, written[i].p, written[i].bytes)) return STR_ERR_INVALID_ARG;
-        for (size_t j = 0; j < i; ++j)
-            if (kv4_overlap(written[j].p, written[j].bytes, written[i].p, written[i].bytes)) return STR_ERR_INVALID_ARG;
-    }
+    const Buffer read[] = {{cache->k_codes, rows * (s->d / 2)}, {cache->v_codes, rows * (s->d / 2)}, {cache->k_scales, rows * words},
+                           {cache->v_scales, rows * words}, {cache->weight, rows * 4}, {cache->pos, counts * s->cap}, {lens, counts}, {n_evictable, counts}};
+    const Buffer written[] = {{out->k_codes, rows_out * (s->d / 2)}, {out->v_codes, rows_out * (s->d / 2)}, {out->k_scales, rows_out * words},
+                              {out->v_scales, rows_out * words}, {out->weight, rows_out * 4}, {out->pos, counts * cap_out}, {lens_out, counts},
+                              {kept_idx_out, keep > 0 ? counts * keep : 0}};
+    if (any_shared(written, 6, read, 6)) return STR_ERR_INVALID_ARG;            // the caches
     if (keep < 0 || keep > s->cap || keep > cap_out || n_recent < 0 || n_recent > keep) return STR_ERR_INVALID_ARG;
     if (cap_out % 16 != 0) return STR_ERR_UNSUPPORTED_SHAPE;
     const bool split = long_rows(s);
@@ -315,6 +320,7 @@ extern "C" int str_kv4_evict(str_ctx *ctx, const str_kv4_shape *s, const str_kv4
         if (!kept_idx_out || (split && (!workspace || ((uintptr_t)workspace & 255)))) return STR_ERR_INVALID_ARG;
         if (workspace_bytes < str_kv4_evict_workspace_size(s, keep)) return STR_ERR_WORKSPACE_TOO_SMALL;
     }
+    if (any_shared(written, 8, read, 8)) return STR_ERR_INVALID_ARG;            // and the counts and lists
     cudaStream_t st = (cudaStream_t)stream;
     StrDeviceScope dev(ctx);
     if (!dev.ok) return STR_ERR_CUDA;
