@@ -133,6 +133,8 @@ def _marshal():
             from . import _marshal as m
         except ImportError as e:
             raise ImportError("_marshal.so: %s; run `python -m paper_2603_00198_b200.build`" % e) from e
+        if m.built_for != torch.__version__:
+            raise ImportError("_marshal.so is built for torch %s, this is %s; run `python -m paper_2603_00198_b200.build`" % (m.built_for, torch.__version__))
         L = lib()
         m.setup(_check, torch.OutOfMemoryError, *(ctypes.cast(getattr(L, name), c_void_p).value for name in (
             "str_kv4_append", "str_kv4_read", "str_kv4_attn_workspace_size", "str_kv4_attn", "str_kv4_evict_workspace_size",

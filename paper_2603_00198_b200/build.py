@@ -18,6 +18,7 @@ CSRC = os.path.join(PKG, "csrc")
 OBJ = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libstr.so")
 MARSHAL = os.path.join(PKG, "_marshal.so")
+BUILT_FOR = os.path.join(OBJ, "marshal.torch")
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17",
@@ -41,22 +42,33 @@ def _compile(src, verbose):
     return obj, res.stderr
 
 
+def _built_for():
+    try:
+        with open(BUILT_FOR) as f:
+            return f.read()
+    except OSError:
+        return None
+
+
 def _build_marshal(force):
-    """The extension module links against torch's C++ libraries, which the process has loaded when it imports the module."""
+    """The extension module links against torch's C++ libraries, which the process has loaded when it imports the module.  It is built
+    anew for another torch, whose version is kept in the module (`built_for`, which the binding compares) and beside the objects."""
     import torch
     src = os.path.join(CSRC, "marshal.cpp")
-    if not force and os.path.exists(MARSHAL) and os.path.getmtime(MARSHAL) >= max(os.path.getmtime(src), _deps_mtime()):
+    if not force and os.path.exists(MARSHAL) and os.path.getmtime(MARSHAL) >= max(os.path.getmtime(src), _deps_mtime()) and _built_for() == torch.__version__:
         return
     tdir = os.path.dirname(torch.__file__)
     cuda = os.path.dirname(os.path.dirname(shutil.which("nvcc")))
     incs = [os.path.join(tdir, "include"), os.path.join(tdir, "include", "torch", "csrc", "api", "include"),
             sysconfig.get_paths()["include"], os.path.join(cuda, "include")]
     cmd = ["g++", "-O2", "-std=c++17", "-Wall", "-fPIC", "-shared", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch.compiled_with_cxx11_abi(),
-           "-I" + os.path.join(ROOT, "include")] + [a for i in incs for a in ("-isystem", i)]
+           '-DSTR_BUILT_FOR="%s"' % torch.__version__, "-I" + os.path.join(ROOT, "include")] + [a for i in incs for a in ("-isystem", i)]
     cmd += [src, "-o", MARSHAL, "-L" + os.path.join(tdir, "lib"), "-ltorch_python", "-ltorch_cpu", "-ltorch", "-lc10", "-lc10_cuda"]
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
         raise RuntimeError("g++ failed for %s:\n%s" % (src, res.stderr))
+    with open(BUILT_FOR, "w") as f:
+        f.write(torch.__version__)
 
 
 def build(force=False, verbose=False):

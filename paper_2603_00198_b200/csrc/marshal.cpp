@@ -332,4 +332,8 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", "argument marshalling o
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__marshal(void) { return PyModule_Create(&module); }
+PyMODINIT_FUNC PyInit__marshal(void) {
+    PyObject *m = PyModule_Create(&module);
+    if (m && PyModule_AddStringConstant(m, "built_for", STR_BUILT_FOR) < 0) Py_CLEAR(m);          // the torch whose headers it was built with
+    return m;
+}

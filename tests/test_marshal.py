@@ -143,6 +143,39 @@ def test_the_tensors_of_a_cache_are_checked_at_every_call():
     assert sh.c.k_codes is None                              # nothing is stored before all have been checked
 
 
+def test_a_module_built_for_another_torch_is_refused(monkeypatch):
+    m = binding._marshal()
+    assert m.built_for == torch.__version__
+    monkeypatch.setattr(binding, "_MARSHAL", None)
+    monkeypatch.setattr(torch, "__version__", "0.0.0")
+    with pytest.raises(ImportError, match="built for torch"):
+        binding._marshal()
+
+
+def test_the_module_is_built_anew_for_another_torch(monkeypatch, tmp_path):
+    from paper_2603_00198_b200 import build
+    build.build()
+    commands = []
+
+    def run(cmd, **kw):
+        commands.append(cmd)
+        return subprocess.CompletedProcess(cmd, 0, "", "")
+
+    monkeypatch.setattr(build.subprocess, "run", run)
+    build._build_marshal(False)
+    assert not commands                                      # up to date
+    stamp = tmp_path / "marshal.torch"
+    stamp.write_text("0.0.0")
+    monkeypatch.setattr(build, "BUILT_FOR", str(stamp))
+    build._build_marshal(False)
+    assert len(commands) == 1 and stamp.read_text() == torch.__version__
+    build._build_marshal(False)
+    assert len(commands) == 1
+    stamp.unlink()
+    build._build_marshal(False)
+    assert len(commands) == 2
+
+
 @pytest.mark.gpu
 def test_outputs_are_new_tensors_and_threads_may_call_at_once():
     """Four threads, each on its own stream, step their own states: the lock is free during a call, and no two share a buffer."""
