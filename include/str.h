@@ -12,7 +12,8 @@
  *   - outputs are fully overwritten; inputs are never modified; in and out must not alias.
  *   - dtype is STR_F32 (everything fp32) or STR_BF16 (bf16 storage, fp32 accumulation).
  *   - bounded device-side waits: a kernel that gives up waiting records STR_ERR_TIMEOUT in the
- *     context's device status word and returns; str_check_status() reads it back.
+ *     context's device status and returns; str_check_status() reads it back (and wrong counts, which the
+ *     decode calls record as STR_ERR_INVALID_ARG).
  * Token order inside a sequence follows the paper's setting (Section 3.1): the n_vis visual
  * tokens come first, the n_text text (query) tokens last; text tokens are never dropped.
  */

@@ -176,7 +176,6 @@ class Context:
         if not torch.cuda.is_available():
             raise RuntimeError("libstr needs a CUDA device; there is no CPU path")
         self.device = device
-        self._dev = torch.device("cuda", device)
         torch.cuda.set_device(device)
         self._h = c_void_p()
         _check(lib().str_create(c_int(device), ctypes.byref(self._h)), "str_create")

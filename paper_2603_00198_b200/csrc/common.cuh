@@ -19,7 +19,8 @@ struct str_ctx {
     int device;
     int sm_count;
     int max_smem_optin;
-    int *status_dev;          // device status word: 0 or the first STR_ERR_* a kernel recorded
+    int *status_dev;          // two device status words: 0 or the first STR_ERR_* that a kernel recorded.  [0] makes the kernels of the
+                              // context leave (a wait ran out), [1] does not (wrong counts in device arrays); str_check_status reads both
     void *encode_tiled;       // cuTensorMapEncodeTiled entry point (driver), or nullptr
     long long launches;       // host-side count of kernels launched through this context
     long long tc_calls;       // entry-point calls that took a tensor-core (tcgen05) kernel
