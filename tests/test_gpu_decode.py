@@ -670,6 +670,30 @@ def test_decode_of_a_handed_off_attention_layer(ctx):
     ctx.check_status()
 
 
+@pytest.mark.parametrize("d,group", [(64, 32), (128, 64)])
+def test_a_second_turn_reads_the_cache_back_for_the_prompt_attention(ctx, d, group):
+    """A prompt of 40 tokens behind what two sequences' caches hold: appended, all rows read back, str_attn_prefill_rows for the new
+    rows; the same outputs as str_kv4_attn's, within the bound that each keeps from the oracle on the cached values."""
+    g = np.random.default_rng([77, d])
+    Hq, Hkv, n_new, lens = 6, 2, 40, [203, 203]
+    f = Filled(g, lens, 256, Hkv, d, group)
+    total = [n + n_new for n in lens]
+    k, v = (_rows(g, (2, n_new, Hkv, d), "f32", keys) for keys in (True, False))
+    q = g.standard_normal((2, n_new, Hq, d)).astype(np.float32)
+    binding.str_kv4_append(ctx, f.cache, dev(k), dev(v), _i32(lens))
+    kr, vr = binding.str_kv4_read(ctx, f.cache, _i32([0, 0]), total[0], torch.float32)
+    rows = _i32([np.arange(n, n + n_new) for n in lens])
+    turn = binding.str_attn_prefill_rows(ctx, dev(q), rows, kr, vr, d ** -0.5).cpu().numpy()
+    step = binding.str_kv4_attn(ctx, f.cache, dev(q), _i32(total), d ** -0.5).cpu().numpy()
+    ctx.check_status()
+    kr, vr = (np.swapaxes(t.double().cpu().numpy(), 1, 2) for t in (kr, vr))
+    for b in range(2):
+        ref, _ = decode.kv4_attention(q[b], kr[b], vr[b], d ** -0.5)
+        ds = (d + 64) * E * d ** -0.5 * max((np.abs(kr[b, h]) @ np.abs(q[b].reshape(n_new, Hkv, -1, d)[:, h]).reshape(-1, d).T.astype(np.float64)).max() for h in range(Hkv))
+        bound = (2 * ds + (32 + total[b]) * E + 2 * E) * np.abs(vr[b]).max() + 2.0 ** -22 * 15 * np.ptp(vr[b]) / 15 + E * np.abs(ref)
+        assert np.all(np.abs(turn[b] - ref) <= bound) and np.all(np.abs(step[b] - ref) <= bound)
+
+
 def _decode_args(g, Bz=2, cap=512, Hq=8, Hkv=2, d=64):
     f = Filled(g, [400, 77], cap, Hkv, d, 32)
     mk = lambda *s: dev(inputs.to_grid(g.standard_normal(s), "bf16"), "bf16")  # noqa: E731
