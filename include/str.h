@@ -364,7 +364,8 @@ int str_stack_prefill_host(str_ctx *ctx, const str_stack_desc *d, const void *hi
  * all 16-byte aligned.  Order of the codes in a row (ng = d/32): keys, element 32 g + 8 c + j (c < 4, j < 8) is nibble j of 32-bit word c*ng + g;
  * values, element 32 g + 4 r + i (r < 8, i < 4) is nibble i of 16-bit word r*ng + g.  Nibble 0 is the lowest.
  * Which rows of a sequence are in use is the caller's to keep (`row_start`, `lens` below): the calls read the counts they
- * are given and change none.  Rows that are not in use are never read and may hold anything. */
+ * are given and change none.  Rows that are not in use may hold anything: nothing comes from them (attention fetches rows sixteen at a
+ * time, so up to 15 behind a sequence with it). */
 typedef struct {
     int Bz, cap, Hkv, d, group;
 } str_kv4_shape;
@@ -402,8 +403,12 @@ int str_kv4_read(str_ctx *ctx, const str_kv4_shape *s, int dtype, int n_out, con
  *   weight_out  device [Bz,Hkv,cap] fp32 or NULL: weight_out[b,h,t] = cache->weight[b,h,t] + the softmax weights that the
  *               n_q tokens' query heads of key head h put on row t, for t < lens[b]; other rows are left as they are.  May be
  *               cache->weight itself.  Same bits on every run.
- * q and k may be of any size up to 1e30 (their products are formed relative to the largest element of a query row); q 16-byte
- * aligned, at most 4096 query rows (tokens x heads) per key head.
+ * What is finite in fp32 is computed: q and k of any size up to 1e30 whose scores stay below 1e38, values whose sum over the rows, times
+ * 8, does.  Scores (times log2(e)) are rounded to fp32, so from 2^24 on they are whole numbers.  The elements of a query row are held
+ * to 2^-35 of its largest or better (bf16 elements exactly down to 2^-27 of it, fp32 ones to 2^-22 of themselves).  The factors of the
+ * value product, softmax weight times group scale, are held to 11 bits for bf16 storage and 22 for fp32; weights (weight_out),
+ * maxima and sums are fp32.
+ * q is 16-byte aligned; at most 4096 query rows (tokens x heads) per key head.
  * Workspace: size from the query (want_weights nonzero when weight_out is given: the scores, 4 bytes per query row and
  * cache row), 256-byte aligned; calls that may run at the same time, two captured graphs among them, need their own. */
 size_t str_kv4_attn_workspace_size(const str_kv4_shape *s, int Hq, int n_q, int want_weights);

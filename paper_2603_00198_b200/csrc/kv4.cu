@@ -9,8 +9,9 @@
 // head, so that the cache's rows, which lie head by head, are written and read as whole lines, and every thread has all the
 // loads of its KV4_UNROLL tokens in flight before it uses the first.
 //
-// Every row is read once and written once, so memory is the bound.  16512 rows, 8 heads of 128, group 32, back to back: append of
-// bf16 21.9 us (4.1 TB/s), of fp32 26.9 (5.8); read as bf16 17.1 (5.2), as fp32 28.8 (5.4).  Two tokens a thread, for more warps an
+// Every row is read once and written once, so memory is the floor; the bf16 forms are held up by instruction issue (74 and 70 % of the
+// slots busy, DRAM at 35 and 22 % of its peak, the rest in L2).  16512 rows, 8 heads of 128, group 32, back to back: append of
+// bf16 20.9 us (4.2 TB/s), of fp32 26.0 (6.0); read as bf16 15.3 (5.8), as fp32 29.5 (5.3).  Two tokens a thread, for more warps an
 // SM: with four, 25.0 and 34.4, 19.0 and 39.2 in the steps' first form; with one, 30.5 and 32.9.
 #include "kv4.cuh"
 
@@ -27,7 +28,7 @@ __device__ __forceinline__ void store8(__nv_bfloat16 *p, const float (&x)[8]) {
     }
     *(uint4 *)p = make_uint4(w[0], w[1], w[2], w[3]);
 }
-// 32 bytes a lane in one store where the address allows it: a warp then writes whole lines (28.8 us for the fp32 read above; two
+// 32 bytes a lane in one store where the address allows it: a warp then writes whole lines (29 us for the fp32 read above; two
 // 16-byte stores, each half of every 32-byte sector, 37).
 __device__ __forceinline__ void store8(float *p, const float (&x)[8]) {
     if (((uintptr_t)p & 31) == 0) {

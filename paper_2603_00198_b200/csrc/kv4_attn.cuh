@@ -6,7 +6,8 @@
 //   o_e     = sum_t (p_t scale_t,g) (c_t,e - 8) + sum_t p_t (zero_t,g + 8 scale_t,g)      (g the group of element e)
 // and q . k likewise with c - 8: the codes are centred so that neither sum is the small difference of two large ones.
 // Both code products run on the matrix instruction, on codes turned into fp16 exactly: a byte put into the mantissa of 1024, its
-// low nibble taken off again as c - 8 and what is left is 16 (c - 8) of the high one (codes2: eight instructions for eight codes);
+// low nibble taken off again as c - 8 and what is left is 16 (c - 8) of the high one (codes2: eight instructions for eight codes; that
+// small integers widen for nothing in a mantissa is well known);
 // the powers of two go into q and into the output.  (The nibble as it stands would be the subnormal c 2^-24 for half of that, but the
 // matrix instruction lines products up by the nominal exponent and then drops the last six to ten bits: measured, 5e-6 instead
 // of 4e-7 of error.)

@@ -7,8 +7,8 @@
 // columns, so that both the loads and the sum over n in y are along the lanes; a warp works on RPT rows per group at once,
 // all their loads in flight together.  All arithmetic is fp32; y is rounded to the storage type once.
 //
-// Bound by memory.  64 sequences of the 8B-class layer (537 MB of state in and out): 83.5 us = 6.46 TB/s, 0.99 of the measured
-// copy bandwidth.  Streaming loads and stores (neither alone does it) and blocks of 128 threads are what it takes: 99.8 us with 256
+// Bound by memory.  64 sequences of the 8B-class layer (537 MB of state in and out): 83.0 us = 6.50 TB/s, 0.99 of the measured
+// copy bandwidth, in a CUDA graph; one call after the other 88.4 us, 0.93.  Streaming loads and stores (neither alone does it) and blocks of 128 threads are what it takes: 99.8 us with 256
 // threads and plain accesses, 93.5 with 128 threads.  From 1 to 32 sequences they are never slower, with the states in L2 or
 // not (one sequence 3.2 us either way).
 #include "kv4.cuh"
