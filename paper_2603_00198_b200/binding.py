@@ -178,13 +178,15 @@ class Context:
         self.device = device
         torch.cuda.set_device(device)
         self._h = c_void_p()
+        self.address = 0
         _check(lib().str_create(c_int(device), ctypes.byref(self._h)), "str_create")
+        self.address = self._h.value
         self._ws = None
 
     def close(self):
         if self._h:
             lib().str_destroy(self._h)
-            self._h = c_void_p()
+            self._h, self.address = c_void_p(), 0
 
     def __del__(self):
         try:
@@ -195,10 +197,6 @@ class Context:
     @property
     def handle(self):
         return self._h
-
-    @property
-    def address(self):
-        return self._h.value or 0
 
     def workspace(self, nbytes):
         nbytes = max(int(nbytes), 256)
@@ -505,11 +503,15 @@ class Kv4Cache:
         self.shape_ref, self._ptrs_at = ctypes.addressof(self._shape), ctypes.addressof(self._ptrs)
         self.index = dev.index
 
+    def ptrs_on(self, marshal, device):
+        """Address of the C struct of the tensors' addresses, filled in anew: an attribute may name another tensor than it did before.
+        Refuses tensors that are not on the device."""
+        marshal.cache(self._ptrs_at, self.shape_ref, device, self.k_codes, self.v_codes, self.k_scales, self.v_scales, self.pos, self.weight)
+        return self._ptrs_at
+
     @property
     def ptrs_ref(self):
-        """Address of the C struct of the tensors' addresses, filled in anew: an attribute may name another tensor than it did before."""
-        _marshal().cache(self._ptrs_at, self.shape_ref, self.index, self.k_codes, self.v_codes, self.k_scales, self.v_scales, self.pos, self.weight)
-        return self._ptrs_at
+        return self.ptrs_on(_marshal(), self.index)
 
     @classmethod
     def empty(cls, ctx, Bz, cap, Hkv, d, group=32, pos=True, weight=True):
@@ -523,39 +525,35 @@ class Kv4Cache:
         return cls(*codes, *words, torch.zeros((Bz, cap), dtype=torch.int32, device=dev) if pos else None,
                    torch.zeros(rows, dtype=torch.float32, device=dev) if weight else None)
 
-    def _on(self, ctx):
-        if self.index != ctx.device:
-            raise ValueError("Kv4Cache: the cache is on %s, the context on cuda:%d" % (self.device, ctx.device))
-
 
 def str_kv4_append(ctx, cache, k, v, row_start, positions=None, n_new=None):
     """Quantises k, v [Bz,T,Hkv,d] and stores them in the rows row_start[b] .. of the cache (the first n_new[b] of them)."""
-    cache._on(ctx)
-    _marshal().append(ctx.address, ctx.device, cache.shape_ref, cache.ptrs_ref, k, v, row_start, positions, n_new)
+    m = _marshal()
+    m.append(ctx.address, ctx.device, cache.shape_ref, cache.ptrs_on(m, ctx.device), k, v, row_start, positions, n_new)
 
 
 def str_kv4_read(ctx, cache, row_start, T, dtype, n_rows=None):
     """(k, v) [Bz,T,Hkv,d] of ``dtype`` from the rows row_start[b] .. of the cache; zeros behind the first n_rows[b]."""
-    cache._on(ctx)
-    return _marshal().read(ctx.address, ctx.device, cache.shape_ref, cache.ptrs_ref, row_start, T, dtype, n_rows)
+    m = _marshal()
+    return m.read(ctx.address, ctx.device, cache.shape_ref, cache.ptrs_on(m, ctx.device), row_start, T, dtype, n_rows)
 
 
 def str_kv4_attn(ctx, cache, q, lens, softmax_scale, weight_out=None):
     """Attention of the newest tokens q [Bz,n_q,Hq,d] over the cache, lens[b] rows of which are in use (the tokens' own
     included).  With ``weight_out`` [Bz,Hkv,cap] fp32 (``cache.weight`` itself, or another tensor) it receives cache.weight plus
     the attention weights drawn by each row in use."""
-    cache._on(ctx)
-    return _marshal().attn(ctx.address, ctx.device, cache.shape_ref, cache.ptrs_ref, q, lens, softmax_scale, weight_out)
+    m = _marshal()
+    return m.attn(ctx.address, ctx.device, cache.shape_ref, cache.ptrs_on(m, ctx.device), q, lens, softmax_scale, weight_out)
 
 
 def str_kv4_evict(ctx, cache, lens, keep, n_recent, out, n_evictable=None):
     """Copies the `keep` rows of each sequence with the largest accumulated weight (and the protected newest ones) to the
     cache ``out``.  Returns (lens_out [Bz], kept [Bz,keep]: the rows' old indices, ascending, -1 behind the last)."""
-    cache._on(ctx)
-    out._on(ctx)
     if (out.Bz, out.Hkv, out.d, out.group) != (cache.Bz, cache.Hkv, cache.d, cache.group):
         raise ValueError("str_kv4_evict: the two caches have different shapes")
-    return _marshal().evict(ctx.address, ctx.device, cache.shape_ref, cache.ptrs_ref, lens, keep, n_recent, n_evictable, out._shape.cap, out.ptrs_ref)
+    m = _marshal()
+    return m.evict(ctx.address, ctx.device, cache.shape_ref, cache.ptrs_on(m, ctx.device), lens, keep, n_recent, n_evictable, out._shape.cap,
+                   out.ptrs_on(m, ctx.device))
 
 
 def str_mamba2_step(ctx, x, dt, A, B, C, state, D=None, state_out=None):

@@ -1,7 +1,7 @@
 // _marshal: argument marshalling of the decode calls for the Python binding, which are made once per layer and token: checks of the
 // tensors (type, device, shape, contiguity), outputs and workspace from torch's stream-ordered pool, the current stream of the
 // context's device, and the call of the C entry point.  No arithmetic.  Host time of one call, launches included: append 4.6 us,
-// read 5.1, attention 7.9 (two launches), eviction 7.4 (two), step 4.2; 0.3 of it looks at the tensors of a cache.  Through ctypes it was
+// read 5.1, attention 7.9 (two launches), eviction 7.4 (two), step 4.2; 0.2 of it looks at the tensors of a cache.  Through ctypes it was
 // 1.6 to 2.2 times as much.
 //
 // The entry points are handed over by address (setup), so that the module needs no link to libstr.so.
