@@ -465,6 +465,47 @@ def test_attention_of_many_sequences(ctx, Bz, weights):
     check_attention(ctx, f, q, "bf16", 0.125, weights)
 
 
+@pytest.mark.parametrize("n_q,R", [(512, 8), (1365, 3), (4096, 1)])
+def test_attention_of_as_many_query_rows_as_a_key_head_may_have(ctx, n_q, R):
+    g = np.random.default_rng([n_q, R])
+    f = Filled(g, [n_q + 100, 33, 0], (n_q + 127) // 16 * 16, 1, 64, 32)
+    q = g.standard_normal((3, n_q, R, 64)).astype(np.float32)
+    check_attention(ctx, f, q, "f32", 0.125, True)
+    with pytest.raises(binding.StrError) as e:
+        binding.str_kv4_attn(ctx, f.cache, dev(np.zeros((3, 4097, 1, 64), dtype=np.float32)), _i32(f.lens), 0.125)
+    assert e.value.code == -2
+
+
+def test_decode_calls_on_as_many_sequences_as_a_grid_holds(ctx):
+    """65535 sequences of up to 16 rows."""
+    Bz, d = 65535, 64
+    g = torch.Generator(device="cuda").manual_seed(8)
+    lens = torch.randint(0, 17, (Bz,), generator=g, device="cuda", dtype=torch.int32)
+    cache, out = binding.Kv4Cache.empty(ctx, Bz, 16, 1, d), binding.Kv4Cache.empty(ctx, Bz, 16, 1, d)
+    k, v, q = (torch.randn(Bz, n, 1, d, generator=g, device="cuda") for n in (16, 16, 1))
+    zero = torch.zeros_like(lens)
+    binding.str_kv4_append(ctx, cache, k, v, zero, n_new=lens)
+    kr, vr = binding.str_kv4_read(ctx, cache, zero, 16, torch.float32, n_rows=lens)
+    o = binding.str_kv4_attn(ctx, cache, q, lens, 0.125, weight_out=cache.weight)
+    n, kept = binding.str_kv4_evict(ctx, cache, lens, 4, 1, out)
+    ctx.check_status()
+    pick = np.random.default_rng(8).integers(0, Bz, 300)
+    pick[:2] = 0, Bz - 1
+    w, kept, host = cache.weight.cpu().numpy(), kept.cpu().numpy(), lens.cpu().numpy()
+    for b in pick:
+        m = host[b]
+        qb, kb, vb = (t.cpu().numpy() for t in (q[b], kr[b, :m, 0], vr[b, :m, 0]))
+        ref, drawn = decode.kv4_attention(qb, kb[None], vb[None], 0.125)
+        if m:                                                       # as at the top of the file; read-back rows are off by 2 e, a scale is span / 15
+            rel = 2 * (d + 64) * E * 0.125 * (np.abs(kb) @ np.abs(qb[0, 0])).max() + (32 + m) * E
+            assert np.all(np.abs(o[b].cpu().numpy() - ref) <= (rel + 2 * E) * np.abs(vb).max() + 2.0 ** -22 * 1.1 * np.ptp(vb) + E * np.abs(ref))
+            assert np.all(np.abs(w[b, 0, :m] - drawn[0]) <= (rel + 2 * E) * drawn[0])
+        else:
+            assert not o[b].any()
+        idx = decode.kv4_evict(w[b], m, 4, 1)
+        assert int(n[b]) == len(idx) and np.array_equal(kept[b, :len(idx)], idx) and np.all(kept[b, len(idx):] == -1)
+
+
 def test_attention_weights_in_place_and_the_same_bits_every_time(ctx):
     g = np.random.default_rng(12)
     f = Filled(g, [2000, 0, 517], 2016, 4, 128, 32)
