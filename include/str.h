@@ -441,6 +441,74 @@ int str_kv4_evict(str_ctx *ctx, const str_kv4_shape *s, const str_kv4_cache *cac
 int str_mamba2_step(str_ctx *ctx, const str_ssd_shape *s, const void *x, const float *dt, const float *A, const void *B,
                     const void *C, const float *D, const float *state, void *y, float *state_out, void *stream);
 
+/* ------------------------------------------------------------------------------------------
+ * Packed sequences and continued turns: the layers' operators for sequences of different lengths that lie one after the other in one tensor of
+ * `rows` rows, each of them a whole prompt or the continuation of an earlier one (from a window, a state, earlier keys).
+ * Sequence s has the rows start[s] .. start[s+1]-1 (start: device int32 [n_seq+1], ascending, in [0,rows]); sequences may be empty; rows before the
+ * first and behind the last sequence are nobody's: they are not read into any result, and outputs keep what they held there.  A start that
+ * descends or lies outside is held to the tensor (nothing outside is touched; what is computed is unspecified) and STR_ERR_INVALID_ARG is recorded
+ * for str_check_status.  The calls may be made while another device is current, and may be captured into a CUDA graph.  At most 2^30 rows.
+ * ------------------------------------------------------------------------------------------ */
+
+/* The pre-scan step of str_mamba_conv_split on packed sequences whose convolution starts from a window: zxbcdt device
+ * [rows, 2*d_inner + 2*G*n + H] (its first d_inner columns, the gate, are not read), taps conv_w [d_inner+2Gn, W] fp32 (W 2, 3 or 4), conv_b fp32.
+ *   window      device [n_seq, W-1, d_inner + 2Gn] dtype, oldest first: the x B C columns of the W-1 rows before each sequence's first one, or NULL
+ *               (zeros).
+ *   window_out  the same for what follows (of a sequence with fewer than W-1 rows, rows of `window` among them), or NULL.  Shares no memory with
+ *               `window`.
+ *   x_out [rows,H,p], B_out, C_out [rows,G,n] dtype, dt_out [rows,H] fp32.
+ * Errors: INVALID_ARG, UNSUPPORTED_SHAPE (other W, n_seq > 65535). */
+int str_mamba_conv_packed(str_ctx *ctx, int dtype, int n_seq, int rows, int H, int p, int n, int G, int W, const void *zxbcdt, const float *conv_w,
+                          const float *conv_b, const float *dt_bias, const int32_t *seq_start, const void *window, void *x_out, void *B_out,
+                          void *C_out, float *dt_out, void *window_out, void *stream);
+/* The same for T tokens each of Bz sequences (decoding: what str_mamba2_step takes), zxbcdt [Bz*T, ...]; the window (not NULL) may be updated in
+ * place (window_out == window).  Time grows with T. */
+int str_mamba_conv_step(str_ctx *ctx, int dtype, int Bz, int T, int H, int p, int n, int G, int W, const void *zxbcdt, const float *conv_w,
+                        const float *conv_b, const float *dt_bias, const void *window, void *x_out, void *B_out, void *C_out, float *dt_out,
+                        void *window_out, void *stream);
+
+/* The scan (1) on packed sequences: x, y [rows,H,p], dt [rows,H], B, C [rows,G,n], A, D as in (1); init_state [n_seq,H,p,n] fp32 or NULL (zeros);
+ * final_state the same shape or NULL, may be init_state itself.  An empty sequence's final state is its initial one.
+ * final_state is accurate to fp32 arithmetic whatever the dtype.  Errors: INVALID_ARG, UNSUPPORTED_SHAPE (n > 256, n_seq > 65535),
+ * WORKSPACE_TOO_SMALL. */
+typedef struct {
+    int n_seq, rows, H, p, n, G, dtype;
+} str_ssd_packed_shape;
+size_t str_mamba2_prefill_packed_workspace_size(const str_ssd_packed_shape *s);
+int str_mamba2_prefill_packed(str_ctx *ctx, const str_ssd_packed_shape *s, const void *x, const float *dt, const float *A, const void *B, const void *C,
+                              const float *D, const int32_t *seq_start, const float *init_state, void *y, float *final_state, void *workspace,
+                              size_t workspace_bytes, void *stream);
+
+/* Causal GQA attention of packed sequences, lq queries and lk keys each: query i sees the keys 0 .. lk - lq + i of its sequence, as when the
+ * queries are the newest lq of lk tokens.  A query without any key to see (lk < lq) gives zeros.
+ *   q, o device [rows_q,Hq,d]; k, v device [rows_k,Hkv,d]; q_start, k_start device int32 [n_seq+1]; k_start NULL: the keys' rows are the queries'.
+ * Keys that a query does not see have no influence on it, infinities and NaN among them.  softmax_scale > 0.
+ * Errors: INVALID_ARG, UNSUPPORTED_SHAPE (d > 128, more than 128 query heads per key head, n_seq > 32768), WORKSPACE_TOO_SMALL. */
+typedef struct {
+    int n_seq, rows_q, rows_k, Hq, Hkv, d, dtype;
+} str_attn_packed_shape;
+size_t str_attn_prefill_packed_workspace_size(const str_attn_packed_shape *s);
+int str_attn_prefill_packed(str_ctx *ctx, const str_attn_packed_shape *s, const void *q, const void *k, const void *v, const int32_t *q_start,
+                            const int32_t *k_start, float softmax_scale, void *o, void *workspace, size_t workspace_bytes, void *stream);
+
+/* str_rope_split with the rotary embedding described: of each q and k head the first rot_dim elements (even, <= d, <= 256) are turned, the rest
+ * copied; pair i, angle position * f_i, f_i = theta^(-2i/rot_dim):
+ *   layout   HALF: elements (i, i + rot_dim/2);  INTERLEAVED: (2i, 2i+1)
+ *   scaling  for contexts longer than the trained one: NONE;  LINEAR: f_i / factor;  BANDED: f_i g + (f_i / factor)(1 - g),
+ *            g = clamp((trained_len f_i / 2pi - turns_low) / (turns_high - turns_low), 0, 1): pairs that turn often within trained_len keep their
+ *            frequency, slow ones are stretched, those between are blended
+ *   amplitude  multiplies what is turned (1: a rotation)
+ * qkv device [rows, (Hq+2Hkv)*d]; positions device [rows] int32, any values; q_out [rows,Hq,d], k_out, v_out [rows,Hkv,d].  Angles are formed
+ * in 64 bits.  Outputs share no memory with qkv.  Errors: INVALID_ARG, UNSUPPORTED_SHAPE (rot_dim > 256; odd d with INTERLEAVED). */
+enum { STR_ROPE_HALF = 0, STR_ROPE_INTERLEAVED = 1 };
+enum { STR_ROPE_NONE = 0, STR_ROPE_LINEAR = 1, STR_ROPE_BANDED = 2 };
+typedef struct {
+    int rot_dim, layout, scaling, trained_len;
+    double theta, factor, turns_low, turns_high, amplitude;
+} str_rope_desc;
+int str_rope_split_ex(str_ctx *ctx, const str_rope_desc *r, int dtype, int rows, int Hq, int Hkv, int d, const int32_t *positions, const void *qkv,
+                      void *q_out, void *k_out, void *v_out, void *stream);
+
 /* Optional device timing by kernel category.  While enabled, every leaf entry point records a CUDA
  * event pair around its launches on the caller's stream (str_profile_enable allocates events lazily on
  * first use).  str_profile_collect synchronises on the recorded events, adds the elapsed milliseconds

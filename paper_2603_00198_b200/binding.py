@@ -1,4 +1,4 @@
-"""Thin binding over libstr.so: argument marshalling only (ctypes; the decode calls go through ``csrc/marshal.cpp``).
+"""Thin binding over libstr.so: argument marshalling only (ctypes; the calls for decoding and for packed sequences go through ``csrc/marshal.cpp``).
 
 Every function has the name of the C entry point it calls (see ``include/str.h``) and takes torch
 CUDA tensors, which serve purely as device memory; all arithmetic runs in the library's kernels.
@@ -62,6 +62,19 @@ class Kv4CachePtrs(ctypes.Structure):
     _fields_ = [(k, c_void_p) for k in ("k_codes", "v_codes", "k_scales", "v_scales", "pos", "weight")]
 
 
+class SsdPackedShape(ctypes.Structure):
+    _fields_ = [(k, c_int) for k in ("n_seq", "rows", "H", "p", "n", "G", "dtype")]
+
+
+class AttnPackedShape(ctypes.Structure):
+    _fields_ = [(k, c_int) for k in ("n_seq", "rows_q", "rows_k", "Hq", "Hkv", "d", "dtype")]
+
+
+class RopeDesc(ctypes.Structure):
+    _fields_ = ([(k, c_int) for k in ("rot_dim", "layout", "scaling", "trained_len")]
+                + [(k, ctypes.c_double) for k in ("theta", "factor", "turns_low", "turns_high", "amplitude")])
+
+
 class StackIO(ctypes.Structure):
     _fields_ = [("positions_in", c_void_p), ("idx_map_in", c_void_p), ("mamba_final_states", c_void_p),
                 ("attn_k_out", c_void_p), ("attn_v_out", c_void_p), ("attn_pos_out", c_void_p)]
@@ -86,9 +99,11 @@ EXPORTS = [
     "str_stack_prefill_host",
     "str_kv4_append", "str_kv4_read", "str_kv4_attn_workspace_size", "str_kv4_attn", "str_kv4_evict_workspace_size", "str_kv4_evict",
     "str_mamba2_step",
+    "str_mamba_conv_packed", "str_mamba_conv_step", "str_mamba2_prefill_packed_workspace_size", "str_mamba2_prefill_packed",
+    "str_attn_prefill_packed_workspace_size", "str_attn_prefill_packed", "str_rope_split_ex",
 ]
 
-# Declared argument types of the decode entry points, for direct calls with plain integers as addresses.
+# Declared argument types of the entry points for decoding and for packed sequences, for direct calls with plain integers as addresses.
 _I, _F, _Z, _P = c_int, c_float, c_size_t, c_void_p
 _ARGTYPES = {
     "str_kv4_append": [_P, _P, _I, _I, _P, _P, _P, _P, _P, _P, _P],
@@ -98,6 +113,13 @@ _ARGTYPES = {
     "str_kv4_evict_workspace_size": [_P, _I],
     "str_kv4_evict": [_P, _P, _P, _P, _I, _I, _P, _I, _P, _P, _P, _P, _Z, _P],
     "str_mamba2_step": [_P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P],
+    "str_mamba_conv_packed": [_P] + [_I] * 8 + [_P] * 12,
+    "str_mamba_conv_step": [_P] + [_I] * 8 + [_P] * 11,
+    "str_mamba2_prefill_packed_workspace_size": [_P],
+    "str_mamba2_prefill_packed": [_P] * 13 + [_Z, _P],
+    "str_attn_prefill_packed_workspace_size": [_P],
+    "str_attn_prefill_packed": [_P] * 7 + [_F, _P, _P, _Z, _P],
+    "str_rope_split_ex": [_P, _P] + [_I] * 5 + [_P] * 6,
 }
 
 _LIB = None
@@ -126,7 +148,7 @@ _MARSHAL = None
 
 
 def _marshal():
-    """Load _marshal.so (argument checks, outputs and calls of the decode entry points, ``csrc/marshal.cpp``) once."""
+    """Load _marshal.so (argument checks, outputs and calls of the entry points for decoding and for packed sequences, ``csrc/marshal.cpp``) once."""
     global _MARSHAL
     if _MARSHAL is None:
         try:
@@ -139,6 +161,9 @@ def _marshal():
         m.setup(_check, torch.OutOfMemoryError, *(ctypes.cast(getattr(L, name), c_void_p).value for name in (
             "str_kv4_append", "str_kv4_read", "str_kv4_attn_workspace_size", "str_kv4_attn", "str_kv4_evict_workspace_size",
             "str_kv4_evict", "str_mamba2_step")))
+        m.setup_packed(*(ctypes.cast(getattr(L, name), c_void_p).value for name in (
+            "str_rope_split_ex", "str_mamba_conv_packed", "str_mamba_conv_step", "str_mamba2_prefill_packed_workspace_size", "str_mamba2_prefill_packed",
+            "str_attn_prefill_packed_workspace_size", "str_attn_prefill_packed")))
         _MARSHAL = m
     return _MARSHAL
 
@@ -562,6 +587,56 @@ def str_mamba2_step(ctx, x, dt, A, B, C, state, D=None, state_out=None):
     if state_out is None:
         state_out = state
     return _marshal().step(ctx.address, ctx.device, x, dt, A, B, C, state, D, state_out), state_out
+
+
+class Rope:
+    """A rotary embedding (``str_rope_desc`` in ``include/str.h``): base ``theta``, the first ``rot_dim`` elements of a head in pairs
+    (i, i + rot_dim/2) (``layout`` "half") or (2i, 2i+1) ("interleaved"); ``scaling`` "none", "linear" (frequencies over ``factor``) or
+    "banded" (over ``factor`` for pairs with fewer than turns[0] turns within ``trained_len``, kept for those with more than turns[1], blended between);
+    ``amplitude`` multiplies what is turned."""
+
+    LAYOUTS = {"half": 0, "interleaved": 1}
+    SCALINGS = {"none": 0, "linear": 1, "banded": 2}
+
+    def __init__(self, theta, rot_dim, layout="half", scaling="none", factor=1.0, trained_len=0, turns=(1.0, 32.0), amplitude=1.0):
+        if layout not in self.LAYOUTS or scaling not in self.SCALINGS:
+            raise ValueError("Rope: layout half or interleaved, scaling none, linear or banded, not %s and %s" % (layout, scaling))
+        self._desc = RopeDesc(rot_dim, self.LAYOUTS[layout], self.SCALINGS[scaling], trained_len, theta, factor, turns[0], turns[1], amplitude)
+        self.desc_ref = ctypes.addressof(self._desc)
+
+
+def str_rope_split_ex(ctx, rope, qkv, positions, Hq, Hkv, d):
+    """(q [rows,Hq,d], k, v [rows,Hkv,d]) of qkv [rows,(Hq+2Hkv)*d], q and k turned as the Rope says at positions [rows] int32."""
+    return _marshal().rope(ctx.address, ctx.device, rope.desc_ref, qkv, positions, Hq, Hkv, d)
+
+
+def str_mamba_conv_packed(ctx, zxbcdt, conv_w, conv_b, dt_bias, seq_start, H, p, n, G, window=None, window_out=None, out=None):
+    """The pre-scan step on packed rows zxbcdt [rows, 2*H*p + 2*G*n + H], sequence s in the rows seq_start[s] .. seq_start[s+1]-1, its
+    convolution started from window[s] [W-1, H*p + 2*G*n] (zeros without one); ``window_out`` receives the windows behind the sequences.  Returns
+    (x [rows,H,p], B, C [rows,G,n], dt [rows,H]), ``out`` if such a tuple is given; rows of no sequence are left as they are."""
+    return _marshal().conv_packed(ctx.address, ctx.device, zxbcdt, conv_w, conv_b, dt_bias, H, p, n, G, seq_start, window, window_out,
+                                  *((None,) * 4 if out is None else out))
+
+
+def str_mamba_conv_step(ctx, zxbcdt, conv_w, conv_b, dt_bias, window, Bz, T, H, p, n, G, window_out=None):
+    """The pre-scan step of T tokens each of Bz sequences, zxbcdt [Bz*T, ...]; returns (x [Bz,T,H,p], B, C [Bz,T,G,n], dt [Bz,T,H]).  Without
+    ``window_out`` the window [Bz, W-1, H*p + 2*G*n] is updated in place."""
+    return _marshal().conv_step(ctx.address, ctx.device, zxbcdt, conv_w, conv_b, dt_bias, H, p, n, G, window, Bz, T, window if window_out is None else window_out)
+
+
+def str_mamba2_prefill_packed(ctx, x, dt, A, B, C, seq_start, D=None, init_state=None, final_state=None, out=None):
+    """The scan over packed rows x [rows,H,p], dt [rows,H], B, C [rows,G,n]; sequence s starts from init_state[s] [H,p,n] fp32 (zeros without).
+    Returns y [rows,H,p] (``out`` if given; rows of no sequence are left as they are), with ``final_state`` [n_seq,H,p,n] (init_state
+    itself, or another tensor) written and returned too."""
+    y = _marshal().scan_packed(ctx.address, ctx.device, x, dt, A, B, C, seq_start, D, init_state, final_state, out)
+    return y if final_state is None else (y, final_state)
+
+
+def str_attn_prefill_packed(ctx, q, k, v, q_start, softmax_scale, k_start=None, out=None):
+    """Causal attention of packed sequences: q [rows_q,Hq,d], k, v [rows_k,Hkv,d]; query i of the lq in sequence s sees the first lk - lq + i + 1 of
+    its lk keys.  Without ``k_start`` the keys' rows are the queries'.  Returns o [rows_q,Hq,d], ``out`` if given; rows of no sequence are left
+    as they are."""
+    return _marshal().attn_packed(ctx.address, ctx.device, q, k, v, q_start, k_start, softmax_scale, out)
 
 
 class Stack:

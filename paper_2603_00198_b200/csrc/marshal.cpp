@@ -1,4 +1,5 @@
-// _marshal: argument marshalling of the decode calls for the Python binding, which are made once per layer and token: checks of the
+// _marshal: argument marshalling of the decode calls and of those on packed sequences for the Python binding, which are made once per layer and token
+// or turn: checks of the
 // tensors (type, device, shape, contiguity), outputs and workspace from torch's stream-ordered pool, the current stream of the
 // context's device, and the call of the C entry point.  No arithmetic.  Host time of one call, launches included: append 4.6 us,
 // read 5.1, attention 7.9 (two launches), eviction 7.4 (two), step 4.2; 0.2 of it looks at the tensors of a cache.  Through ctypes it was
@@ -28,6 +29,13 @@ decltype(&str_kv4_attn) f_attn;
 decltype(&str_kv4_evict_workspace_size) f_evict_ws;
 decltype(&str_kv4_evict) f_evict;
 decltype(&str_mamba2_step) f_step;
+decltype(&str_rope_split_ex) f_rope;                 // null until setup_packed() was called, as the ones below
+decltype(&str_mamba_conv_packed) f_conv;
+decltype(&str_mamba_conv_step) f_conv_step;
+decltype(&str_mamba2_prefill_packed_workspace_size) f_scan_ws;
+decltype(&str_mamba2_prefill_packed) f_scan;
+decltype(&str_attn_prefill_packed_workspace_size) f_attn_packed_ws;
+decltype(&str_attn_prefill_packed) f_attn_packed;
 PyObject *on_error;      // binding._check(code, name): raises
 PyObject *out_of_memory; // torch.OutOfMemoryError
 
@@ -282,6 +290,191 @@ PyObject *step(PyObject *const *a) {
     return THPVariable_Wrap(y);
 }
 
+int int32(int64_t v, const char *name) {
+    if (v > INT32_MAX) check(STR_ERR_UNSUPPORTED_SHAPE, name);
+    return (int)v;
+}
+// Sequences that a tensor of starts [n_seq + 1] describes.
+int64_t sequences(const at::Tensor &start, const char *what) {
+    dims(start, 1, what);
+    if (start.size(0) < 2) {
+        PyErr_Format(PyExc_ValueError, "%s: expected n_seq + 1 starts, got %lld", what, (long long)start.size(0));
+        throw Refused();
+    }
+    return start.size(0) - 1;
+}
+// An output: the caller's tensor (checked) or, for None, a new one.
+struct Out {
+    at::Tensor t;
+    void *p = nullptr;
+    bool given = false;
+    Out(PyObject *obj, int device, at::IntArrayRef shape, at::ScalarType dtype, const char *what) {
+        if (obj == Py_None) return;
+        t = tensor(obj, what);
+        p = arg(t, device, shape, dtype, what);
+        given = true;
+    }
+    void make(int device, at::IntArrayRef shape, at::ScalarType dtype) {
+        if (given) return;
+        t = empty(shape, dtype, device);
+        p = t.data_ptr();
+    }
+};
+
+// rope(handle, device, desc, qkv, positions, Hq, Hkv, d) -> (q, k, v)
+PyObject *rope(PyObject *const *a) {
+    const Ctx c(a);
+    const str_rope_desc *desc = address<str_rope_desc>(a[2]);
+    const at::Tensor &qkv = tensor(a[3], "qkv");
+    dims(qkv, 2, "qkv");
+    const int64_t Hq = integer(a[5], 1, 1 << 20, "Hq"), Hkv = integer(a[6], 1, 1 << 20, "Hkv"), d = integer(a[7], 1, 1 << 20, "d");
+    const int rows = int32(qkv.size(0), "str_rope_split_ex");
+    const at::ScalarType dt = qkv.scalar_type();
+    const int code = type_code(dt);
+    void *in = arg(qkv, c.device, {rows, (Hq + 2 * Hkv) * d}, dt, "qkv"), *pos = arg(a[4], c.device, {rows}, at::kInt, "positions");
+    const str_rope_desc r = *desc;                                  // as it is now: another thread may change it once the lock is free
+    at::Tensor q, k, v;
+    int rc;
+    {
+        Unlocked free;
+        q = empty({rows, Hq, d}, dt, c.device);
+        k = empty({rows, Hkv, d}, dt, c.device);
+        v = empty({rows, Hkv, d}, dt, c.device);
+        rc = f_rope(c.h, &r, code, rows, (int)Hq, (int)Hkv, (int)d, (const int32_t *)pos, in, q.data_ptr(), k.data_ptr(), v.data_ptr(), stream_of(c.device));
+    }
+    check(rc, "str_rope_split_ex");
+    return Py_BuildValue("NNN", THPVariable_Wrap(q), THPVariable_Wrap(k), THPVariable_Wrap(v));
+}
+
+// The arguments that both convolution calls share, a[2] ..: zxbcdt, conv_w, conv_b, dt_bias, H, p, n, G.
+struct Conv {
+    int rows, H, p, n, G, W, code;
+    int64_t ch;
+    at::ScalarType dt;
+    void *zx, *w, *b, *dt_bias;
+    Conv(PyObject *const *a, int device, const char *name) {
+        const at::Tensor &z = tensor(a[2], "zxbcdt"), &taps = tensor(a[3], "conv_w");
+        dims(z, 2, "zxbcdt");
+        dims(taps, 2, "conv_w");
+        H = (int)integer(a[6], 1, 1 << 20, "H"), p = (int)integer(a[7], 1, 1 << 20, "p"), n = (int)integer(a[8], 1, 1 << 20, "n"), G = (int)integer(a[9], 1, 1 << 20, "G");
+        rows = int32(z.size(0), name);
+        W = int32(taps.size(1), name);
+        dt = z.scalar_type();
+        code = type_code(dt);
+        const int64_t d_inner = (int64_t)H * p;
+        ch = d_inner + 2 * (int64_t)G * n;
+        zx = arg(z, device, {rows, d_inner + ch + H}, dt, "zxbcdt");
+        w = arg(taps, device, {ch, W}, at::kFloat, "conv_w");
+        b = arg(a[4], device, {ch}, at::kFloat, "conv_b");
+        dt_bias = arg(a[5], device, {H}, at::kFloat, "dt_bias");
+    }
+};
+
+// conv_packed(handle, device, zxbcdt, conv_w, conv_b, dt_bias, H, p, n, G, seq_start, window, window_out, x, B, C, dt) -> (x, B, C, dt)
+PyObject *conv_packed(PyObject *const *a) {
+    const Ctx c(a);
+    const Conv k(a, c.device, "str_mamba_conv_packed");
+    const at::Tensor &start = tensor(a[10], "seq_start");
+    const int n_seq = int32(sequences(start, "seq_start"), "str_mamba_conv_packed");
+    void *st = arg(start, c.device, {(int64_t)n_seq + 1}, at::kInt, "seq_start");
+    const Shape ws = {n_seq, k.W - 1, k.ch}, xs = {k.rows, k.H, k.p}, bs = {k.rows, k.G, k.n}, ds = {k.rows, k.H};
+    void *win = optional(a[11], c.device, ws, k.dt, "window"), *wout = optional(a[12], c.device, ws, k.dt, "window_out");
+    Out x(a[13], c.device, xs, k.dt, "out x"), B(a[14], c.device, bs, k.dt, "out B"), C(a[15], c.device, bs, k.dt, "out C"), dt(a[16], c.device, ds, at::kFloat, "out dt");
+    int rc;
+    {
+        Unlocked free;
+        x.make(c.device, xs, k.dt), B.make(c.device, bs, k.dt), C.make(c.device, bs, k.dt), dt.make(c.device, ds, at::kFloat);
+        rc = f_conv(c.h, k.code, n_seq, k.rows, k.H, k.p, k.n, k.G, k.W, k.zx, (const float *)k.w, (const float *)k.b, (const float *)k.dt_bias,
+                    (const int32_t *)st, win, x.p, B.p, C.p, (float *)dt.p, wout, stream_of(c.device));
+    }
+    check(rc, "str_mamba_conv_packed");
+    return Py_BuildValue("NNNN", THPVariable_Wrap(x.t), THPVariable_Wrap(B.t), THPVariable_Wrap(C.t), THPVariable_Wrap(dt.t));
+}
+
+// conv_step(handle, device, zxbcdt, conv_w, conv_b, dt_bias, H, p, n, G, window, Bz, T, window_out) -> (x, B, C, dt)
+PyObject *conv_step(PyObject *const *a) {
+    const Ctx c(a);
+    const Conv k(a, c.device, "str_mamba_conv_step");
+    const int64_t Bz = integer(a[11], 0, INT32_MAX, "Bz"), T = integer(a[12], 0, INT32_MAX, "T");
+    if (Bz * T != k.rows) {
+        PyErr_Format(PyExc_ValueError, "zxbcdt: expected %lld x %lld rows, got %d", (long long)Bz, (long long)T, k.rows);
+        throw Refused();
+    }
+    const Shape ws = {Bz, k.W - 1, k.ch};
+    void *win = arg(a[10], c.device, ws, k.dt, "window"), *wout = arg(a[13], c.device, ws, k.dt, "window_out");
+    at::Tensor x, B, C, dt;
+    int rc;
+    {
+        Unlocked free;
+        x = empty({Bz, T, k.H, k.p}, k.dt, c.device);
+        B = empty({Bz, T, k.G, k.n}, k.dt, c.device);
+        C = empty({Bz, T, k.G, k.n}, k.dt, c.device);
+        dt = empty({Bz, T, k.H}, at::kFloat, c.device);
+        rc = f_conv_step(c.h, k.code, (int)Bz, (int)T, k.H, k.p, k.n, k.G, k.W, k.zx, (const float *)k.w, (const float *)k.b, (const float *)k.dt_bias, win,
+                         x.data_ptr(), B.data_ptr(), C.data_ptr(), (float *)dt.data_ptr(), wout, stream_of(c.device));
+    }
+    check(rc, "str_mamba_conv_step");
+    return Py_BuildValue("NNNN", THPVariable_Wrap(x), THPVariable_Wrap(B), THPVariable_Wrap(C), THPVariable_Wrap(dt));
+}
+
+// scan_packed(handle, device, x, dt, A, B, C, seq_start, D, init_state, final_state, y) -> y
+PyObject *scan_packed(PyObject *const *a) {
+    const Ctx c(a);
+    const char *name = "str_mamba2_prefill_packed";
+    const at::Tensor &x = tensor(a[2], "x"), &B = tensor(a[5], "B"), &start = tensor(a[7], "seq_start");
+    dims(x, 3, "x");
+    dims(B, 3, "B");
+    const int64_t n_seq = sequences(start, "seq_start"), rows = x.size(0), H = x.size(1), p = x.size(2), G = B.size(1), n = B.size(2);
+    const at::ScalarType t = x.scalar_type();
+    const str_ssd_packed_shape s = {int32(n_seq, name), int32(rows, name), int32(H, name), int32(p, name), int32(n, name), int32(G, name), type_code(t)};
+    const Shape states = {n_seq, H, p, n};
+    void *px = arg(x, c.device, {rows, H, p}, t, "x"), *pdt = arg(a[3], c.device, {rows, H}, at::kFloat, "dt"), *pA = arg(a[4], c.device, {H}, at::kFloat, "A");
+    void *pB = arg(B, c.device, {rows, G, n}, t, "B"), *pC = arg(a[6], c.device, {rows, G, n}, t, "C");
+    void *ps = arg(start, c.device, {n_seq + 1}, at::kInt, "seq_start"), *pD = optional(a[8], c.device, {H}, at::kFloat, "D");
+    void *init = optional(a[9], c.device, states, at::kFloat, "init_state"), *fin = optional(a[10], c.device, states, at::kFloat, "final_state");
+    Out y(a[11], c.device, {rows, H, p}, t, "out");
+    at::Tensor ws;
+    int rc;
+    {
+        Unlocked free;
+        const size_t need = f_scan_ws(&s);
+        y.make(c.device, {rows, H, p}, t);
+        if (need) ws = empty({(int64_t)need}, at::kByte, c.device);
+        rc = f_scan(c.h, &s, px, (const float *)pdt, (const float *)pA, pB, pC, (const float *)pD, (const int32_t *)ps, (const float *)init, y.p, (float *)fin,
+                    need ? ws.data_ptr() : nullptr, need, stream_of(c.device));
+    }
+    check(rc, name);
+    return THPVariable_Wrap(y.t);
+}
+
+// attn_packed(handle, device, q, k, v, q_start, k_start, softmax_scale, o) -> o
+PyObject *attn_packed(PyObject *const *a) {
+    const Ctx c(a);
+    const char *name = "str_attn_prefill_packed";
+    const at::Tensor &q = tensor(a[2], "q"), &k = tensor(a[3], "k"), &start = tensor(a[5], "q_start");
+    dims(q, 3, "q");
+    dims(k, 3, "k");
+    const int64_t n_seq = sequences(start, "q_start"), rows_q = q.size(0), Hq = q.size(1), d = q.size(2), rows_k = k.size(0), Hkv = k.size(1);
+    const at::ScalarType t = q.scalar_type();
+    const str_attn_packed_shape s = {int32(n_seq, name), int32(rows_q, name), int32(rows_k, name), int32(Hq, name), int32(Hkv, name), int32(d, name), type_code(t)};
+    void *pq = arg(q, c.device, {rows_q, Hq, d}, t, "q"), *pk = arg(k, c.device, {rows_k, Hkv, d}, t, "k"), *pv = arg(a[4], c.device, {rows_k, Hkv, d}, t, "v");
+    void *qs = arg(start, c.device, {n_seq + 1}, at::kInt, "q_start"), *ks = optional(a[6], c.device, {n_seq + 1}, at::kInt, "k_start");
+    const double scale = PyFloat_AsDouble(a[7]);
+    if (scale == -1.0 && PyErr_Occurred()) throw Refused();
+    Out o(a[8], c.device, {rows_q, Hq, d}, t, "out");
+    at::Tensor ws;
+    int rc;
+    {
+        Unlocked free;
+        const size_t need = f_attn_packed_ws(&s);
+        o.make(c.device, {rows_q, Hq, d}, t);
+        if (need) ws = empty({(int64_t)need}, at::kByte, c.device);
+        rc = f_attn_packed(c.h, &s, pq, pk, pv, (const int32_t *)qs, (const int32_t *)ks, (float)scale, o.p, need ? ws.data_ptr() : nullptr, need, stream_of(c.device));
+    }
+    check(rc, name);
+    return THPVariable_Wrap(o.t);
+}
+
 // No C++ exception leaves the module: what torch throws (out of memory, say) becomes a Python exception.
 template <PyObject *(*F)(PyObject *const *), int N>
 PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n) {
@@ -324,11 +517,42 @@ PyObject *setup(PyObject *, PyObject *const *a, Py_ssize_t n) {
     Py_RETURN_NONE;
 }
 
+// setup_packed(rope_split_ex, mamba_conv_packed, mamba_conv_step, mamba2_prefill_packed_workspace_size, mamba2_prefill_packed,
+// attn_prefill_packed_workspace_size, attn_prefill_packed): the addresses of the entry points on packed sequences; after setup()
+PyObject *setup_packed(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    if (n != 7) return PyErr_Format(PyExc_TypeError, "expected 7 arguments, got %zd", n);
+    if (!on_error) return PyErr_Format(PyExc_RuntimeError, "setup() has not been called");
+    void *p[7];
+    for (int i = 0; i < 7; ++i) {
+        p[i] = PyLong_AsVoidPtr(a[i]);
+        if (!p[i]) return PyErr_Occurred() ? nullptr : PyErr_Format(PyExc_ValueError, "null entry point");
+    }
+    f_rope = (decltype(f_rope))p[0];
+    f_conv = (decltype(f_conv))p[1];
+    f_conv_step = (decltype(f_conv_step))p[2];
+    f_scan_ws = (decltype(f_scan_ws))p[3];
+    f_scan = (decltype(f_scan))p[4];
+    f_attn_packed_ws = (decltype(f_attn_packed_ws))p[5];
+    f_attn_packed = (decltype(f_attn_packed))p[6];
+    Py_RETURN_NONE;
+}
+
+// The calls on packed sequences: entry(), once their entry points are known.
+template <PyObject *(*F)(PyObject *const *), int N>
+PyObject *entry_packed(PyObject *self, PyObject *const *args, Py_ssize_t n) {
+    if (n == N && !f_rope) return PyErr_Format(PyExc_RuntimeError, "setup_packed() has not been called");
+    return entry<F, N>(self, args, n);
+}
+
 #define ENTRY(name, N) {#name, (PyCFunction)(void (*)(void))entry<name, N>, METH_FASTCALL, nullptr}
+#define ENTRY_PACKED(name, N) {#name, (PyCFunction)(void (*)(void))entry_packed<name, N>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {{"setup", (PyCFunction)(void (*)(void))setup, METH_FASTCALL, nullptr},
                          ENTRY(cache, 9), ENTRY(append, 9), ENTRY(read, 8), ENTRY(attn, 8), ENTRY(evict, 10), ENTRY(step, 10),
+                         {"setup_packed", (PyCFunction)(void (*)(void))setup_packed, METH_FASTCALL, nullptr},
+                         ENTRY_PACKED(rope, 8), ENTRY_PACKED(conv_packed, 17), ENTRY_PACKED(conv_step, 14), ENTRY_PACKED(scan_packed, 12),
+                         ENTRY_PACKED(attn_packed, 9),
                          {nullptr, nullptr, 0, nullptr}};
-PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", "argument marshalling of the decode calls", -1, methods, nullptr, nullptr, nullptr, nullptr};
+PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", "argument marshalling of the decode calls and of those on packed sequences", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
 

@@ -1,0 +1,109 @@
+// Packed sequences: n_seq sequences lie one after the other in a tensor of `rows` rows; start[s] is the first row of sequence s and
+// start[n_seq] the first row behind the last one (device int32, n_seq + 1 entries, ascending).  Rows outside are nobody's.
+//
+// The kernels trust nothing they read there: every start is held to [0, rows], and what follows from it (rows, lengths, indices of
+// sequences) stays inside the tensors for any values at all.  Starts outside that range or descending are recorded as the decode
+// calls record wrong counts.
+#pragma once
+#include "kv4.cuh"
+
+__device__ __forceinline__ int packed_start(const int32_t *start, int i, int rows) { return min(max(__ldg(start + i), 0), rows); }
+
+// Sequence that row t lies in: the last one that starts at or before it (empty ones share their start with the next).  -1 before the
+// first, n_seq behind the last.  All threads of the block call it; one pass over the starts, one barrier.
+__device__ __forceinline__ int packed_sequence_of(const int32_t *start, int n_seq, int t) {
+    int at_or_before = 0;
+    for (int i0 = 0; i0 <= n_seq; i0 += blockDim.x) {
+        const int i = i0 + (int)threadIdx.x;
+        at_or_before += __syncthreads_count(i <= n_seq && __ldg(start + i) <= t);
+    }
+    return at_or_before - 1;
+}
+
+// One block looks all starts over and records what is wrong.
+__device__ __forceinline__ void packed_check(const int32_t *start, int n_seq, int rows, int *status) {
+    for (int i = threadIdx.x; i <= n_seq; i += blockDim.x) {
+        const int v = __ldg(start + i);
+        if (v < 0 || v > rows || (i > 0 && v < __ldg(start + i - 1))) kv4_report(status);
+    }
+}
+
+// ---- the order of attention's query blocks ------------------------------------------------------
+// A query block is `block` consecutive queries of one sequence; it costs as many key tiles as its last query sees.  CTA number r
+// takes the r-th most expensive block of all sequences, so that the long ones start first and the short ones fill the gaps.
+// No list is made: the number of blocks that cost `tiles` or more is a sum over the sequences of a closed form, and a binary search over the
+// cost, then a prefix sum over the sequences, find block r.  Run by one whole warp.
+struct PackedBlock {
+    int seq, first, n;           // sequence, first query within it, queries (0: there is no block r)
+    int q0, lq, k0, lk;          // the sequence's rows
+};
+
+struct PackedAttnSeq {
+    int q0, lq, k0, lk;
+};
+__device__ __forceinline__ PackedAttnSeq packed_attn_seq(const int32_t *q_start, const int32_t *k_start, int s, int rows_q, int rows_k) {
+    PackedAttnSeq r;
+    r.q0 = packed_start(q_start, s, rows_q);
+    r.lq = max(packed_start(q_start, s + 1, rows_q) - r.q0, 0);
+    r.k0 = packed_start(k_start, s, rows_k);
+    r.lk = max(packed_start(k_start, s + 1, rows_k) - r.k0, 0);
+    return r;
+}
+// Blocks of the sequence whose last query sees more than (tiles - 1) * key_tile keys; all of them for tiles <= 0.
+__device__ __forceinline__ int packed_blocks_of_cost(const PackedAttnSeq &q, int block, int key_tile, int tiles) {
+    const int n = (q.lq + block - 1) / block;
+    if (tiles <= 0) return n;
+    const long long below = (long long)(tiles - 1) * key_tile;
+    if (q.lk <= below) return 0;
+    const long long y = below - q.lk + q.lq;             // the last query of a block has to be number y or later
+    return y <= 0 ? n : n - (int)(y / block);
+}
+__device__ __forceinline__ PackedBlock packed_block(const int32_t *q_start, const int32_t *k_start, int n_seq, int rows_q, int rows_k, int block,
+                                                    int key_tile, int r) {
+    const int lane = threadIdx.x & 31;
+    auto blocks = [&](int tiles) {
+        int n = 0;
+        for (int s = lane; s < n_seq; s += 32) n += packed_blocks_of_cost(packed_attn_seq(q_start, k_start, s, rows_q, rows_k), block, key_tile, tiles);
+        return (int)__reduce_add_sync(0xffffffffu, (unsigned)n);
+    };
+    PackedBlock b = {};
+    if (r >= blocks(0)) return b;
+    int lo = 0, hi = (rows_k + key_tile - 1) / key_tile;  // blocks(lo) > r; no block costs more than hi
+    while (lo < hi) {
+        const int mid = lo + (hi - lo + 1) / 2;
+        if (blocks(mid) > r) lo = mid;
+        else hi = mid - 1;
+    }
+    int left = r - blocks(lo + 1);                        // among the blocks that cost exactly lo, in the order of the sequences
+    for (int s0 = 0; s0 < n_seq; s0 += 32) {
+        PackedAttnSeq q = {};
+        int from = 0, n = 0;
+        if (s0 + lane < n_seq) {
+            q = packed_attn_seq(q_start, k_start, s0 + lane, rows_q, rows_k);
+            const int all = (q.lq + block - 1) / block, more = packed_blocks_of_cost(q, block, key_tile, lo + 1);
+            n = packed_blocks_of_cost(q, block, key_tile, lo) - more;
+            from = all - more - n;
+        }
+        int upto = n;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += v;
+        }
+        const unsigned found = __ballot_sync(0xffffffffu, upto > left);
+        if (found) {
+            const int l = __ffs(found) - 1;
+            const int i = from + left - (upto - n);       // meaningful in lane l only
+            b.seq = s0 + l;
+            b.first = __shfl_sync(0xffffffffu, i, l) * block;
+            b.q0 = __shfl_sync(0xffffffffu, q.q0, l);
+            b.lq = __shfl_sync(0xffffffffu, q.lq, l);
+            b.k0 = __shfl_sync(0xffffffffu, q.k0, l);
+            b.lk = __shfl_sync(0xffffffffu, q.lk, l);
+            b.n = min(block, b.lq - b.first);
+            return b;
+        }
+        left -= __shfl_sync(0xffffffffu, upto, 31);
+    }
+    return b;
+}

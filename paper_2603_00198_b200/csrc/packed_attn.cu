@@ -1,0 +1,209 @@
+// str_attn_prefill_packed: causal attention with grouped heads over packed sequences; query i of a sequence with lq queries and lk keys
+// sees its keys 0 .. lk - lq + i.  The entry point, and the kernel in fp32 arithmetic: every type, head sizes up to 128.
+//
+// One pass over the keys with the running maximum and sum of the softmax.  The 128 rows of a block are (query, head) pairs: the queries of a
+// key head's group lie in one block, so that its keys and values are fetched once for all of them.
+#include <math.h>
+
+#include "dispatch.cuh"
+#include "packed.cuh"
+
+namespace {
+
+constexpr int BR = 128, BC = 64, THREADS = 256, LDP = BC + 4;
+
+// DP: head size padded to 64 or 128.  Thread (ty, tx) of 16 x 16: rows ty + 16 a (a < 8), keys tx + 16 j (j < 4), columns 4 tx + 64 c ...
+template <typename T, int DP>
+__global__ void __launch_bounds__(THREADS)
+attn_packed_simt_kernel(int n_seq, int rows_q, int rows_k, int Hq, int Hkv, int d, float scale_log2, const int32_t *__restrict__ q_start,
+                        const int32_t *__restrict__ k_start, const T *__restrict__ q, const T *__restrict__ k, const T *__restrict__ v, T *__restrict__ o,
+                        int *status) {
+    constexpr int LD = DP + 4, DC = DP / 64;
+    extern __shared__ float4 smem4[];
+    float *Qs = (float *)smem4, *Ks = Qs + BR * LD, *Vs = Ks + BC * LD, *Ps = Vs + BC * DP;
+    __shared__ PackedBlock blk;
+    const int tid = threadIdx.x, ty = tid / 16, tx = tid % 16;
+    const int kv = blockIdx.x % Hkv, group = Hq / Hkv, per = BR / group;  // queries per block
+    if (blockIdx.x == 0) {
+        packed_check(q_start, n_seq, rows_q, status);
+        packed_check(k_start, n_seq, rows_k, status);
+    }
+    if (tid < 32) {
+        const PackedBlock b = packed_block(q_start, k_start, n_seq, rows_q, rows_k, per, BC, blockIdx.x / Hkv);
+        if (tid == 0) blk = b;
+    }
+    __syncthreads();
+    const PackedBlock b = blk;
+    if (b.n <= 0) return;
+    const int first_limit = b.lk - b.lq + b.first;                       // last key that the block's first query sees
+    const int seen = max(first_limit + b.n, 0);                          // keys that its last query sees
+    for (int e = tid; e < BR * DP; e += THREADS) {
+        const int r = e / DP, c = e % DP, t = r / group;
+        Qs[r * LD + c] = t < b.n && c < d ? ldf(q + ((size_t)(b.q0 + b.first + t) * Hq + kv * group + r % group) * d + c) : 0.f;
+    }
+    int limit[8];
+    float mx[8], sm[8], acc[8][DC * 4];
+#pragma unroll
+    for (int a = 0; a < 8; ++a) {
+        limit[a] = first_limit + min((ty + 16 * a) / group, b.n - 1);
+        mx[a] = -INFINITY;
+        sm[a] = 0.f;
+#pragma unroll
+        for (int c = 0; c < DC * 4; ++c) acc[a][c] = 0.f;
+    }
+    for (int c0 = 0; c0 < seen; c0 += BC) {
+        __syncthreads();
+        bool odd = false;                                                // a value that is not finite
+        for (int e = tid; e < BC * DP; e += THREADS) {
+            const int r = e / DP, c = e % DP;
+            const size_t at = ((size_t)(b.k0 + c0 + r) * Hkv + kv) * d + c;
+            const bool in = c0 + r < seen && c < d;
+            const float vv = in ? ldf(v + at) : 0.f;
+            Ks[r * LD + c] = in ? ldf(k + at) : 0.f;
+            Vs[r * DP + c] = vv;
+            odd |= !isfinite(vv);
+        }
+        // Weights of hidden keys are zero, and zero times a value that is not finite is not: a tile that some rows see in part only, with such a
+        // value in it, takes the sum that leaves hidden keys out.
+        const bool careful = __syncthreads_or(odd && c0 + BC - 1 > first_limit);
+        float s[8][4] = {};
+#pragma unroll 2
+        for (int c = 0; c < DP; c += 4) {
+            float4 kk[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) kk[j] = *(const float4 *)(Ks + (tx + 16 * j) * LD + c);
+#pragma unroll
+            for (int a = 0; a < 8; ++a) {
+                const float4 qq = *(const float4 *)(Qs + (ty + 16 * a) * LD + c);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    s[a][j] = fmaf(qq.x, kk[j].x, s[a][j]);
+                    s[a][j] = fmaf(qq.y, kk[j].y, s[a][j]);
+                    s[a][j] = fmaf(qq.z, kk[j].z, s[a][j]);
+                    s[a][j] = fmaf(qq.w, kk[j].w, s[a][j]);
+                }
+            }
+        }
+#pragma unroll
+        for (int a = 0; a < 8; ++a) {
+            float top = -INFINITY;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                s[a][j] = c0 + tx + 16 * j <= limit[a] ? s[a][j] * scale_log2 : -INFINITY;
+                top = fmaxf(top, s[a][j]);
+            }
+#pragma unroll
+            for (int off = 8; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+            const float nm = fmaxf(mx[a], top), at = nm == -INFINITY ? 0.f : nm;
+            const float f = exp2f(mx[a] - at);
+            float sum = 0.f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float p = exp2f(s[a][j] - at);
+                Ps[(ty + 16 * a) * LDP + tx + 16 * j] = p;
+                sum += p;
+            }
+#pragma unroll
+            for (int off = 8; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+            sm[a] = fmaf(sm[a], f, sum);
+            mx[a] = nm;
+#pragma unroll
+            for (int c = 0; c < DC * 4; ++c) acc[a][c] *= f;
+        }
+        __syncwarp();                                                    // a row's weights are written and read by the same half warp
+        if (!careful) {
+#pragma unroll 2
+            for (int j = 0; j < BC; j += 4) {
+                float4 vv[4][DC];
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int c = 0; c < DC; ++c) vv[i][c] = *(const float4 *)(Vs + (j + i) * DP + 4 * tx + 64 * c);
+#pragma unroll
+                for (int a = 0; a < 8; ++a) {
+                    const float4 p4 = *(const float4 *)(Ps + (ty + 16 * a) * LDP + j);
+                    const float p[4] = {p4.x, p4.y, p4.z, p4.w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int c = 0; c < DC; ++c) {
+                            acc[a][4 * c] = fmaf(p[i], vv[i][c].x, acc[a][4 * c]);
+                            acc[a][4 * c + 1] = fmaf(p[i], vv[i][c].y, acc[a][4 * c + 1]);
+                            acc[a][4 * c + 2] = fmaf(p[i], vv[i][c].z, acc[a][4 * c + 2]);
+                            acc[a][4 * c + 3] = fmaf(p[i], vv[i][c].w, acc[a][4 * c + 3]);
+                        }
+                }
+            }
+        } else {
+#pragma unroll 1
+            for (int j = 0; j < BC; ++j)
+#pragma unroll
+                for (int a = 0; a < 8; ++a)
+                    if (c0 + j <= limit[a]) {
+                        const float p = Ps[(ty + 16 * a) * LDP + j];
+#pragma unroll
+                        for (int c = 0; c < DC * 4; ++c) acc[a][c] = fmaf(p, Vs[j * DP + 4 * tx + 64 * (c / 4) + c % 4], acc[a][c]);
+                    }
+        }
+    }
+#pragma unroll
+    for (int a = 0; a < 8; ++a) {
+        const int r = ty + 16 * a, t = r / group;
+        if (t >= b.n) continue;
+        const float inv = limit[a] >= 0 ? 1.0f / sm[a] : 0.f;
+        T *dst = o + ((size_t)(b.q0 + b.first + t) * Hq + kv * group + r % group) * d;
+#pragma unroll
+        for (int c = 0; c < DC * 4; ++c) {
+            const int col = 4 * tx + 64 * (c / 4) + c % 4;
+            if (col < d) stf(dst + col, limit[a] >= 0 ? acc[a][c] * inv : 0.f);
+        }
+    }
+}
+
+template <typename T, int DP>
+int launch(str_ctx *ctx, const str_attn_packed_shape *s, const void *q, const void *k, const void *v, const int32_t *q_start, const int32_t *k_start,
+           float scale, void *o, cudaStream_t st) {
+    constexpr size_t smem = sizeof(float) * ((size_t)(BR + BC) * (DP + 4) + BC * DP + BR * LDP);
+    STR_CUDA_OK(cudaFuncSetAttribute(attn_packed_simt_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    const int per = BR / (s->Hq / s->Hkv);
+    attn_packed_simt_kernel<T, DP><<<(s->rows_q / per + s->n_seq) * s->Hkv, THREADS, smem, st>>>(
+        s->n_seq, s->rows_q, s->rows_k, s->Hq, s->Hkv, s->d, scale * 1.4426950408889634f, q_start, k_start, (const T *)q, (const T *)k, (const T *)v,
+        (T *)o, ctx->status_dev);
+    return str_launch_ok(ctx);
+}
+
+}  // namespace
+
+extern "C" size_t str_attn_prefill_packed_workspace_size(const str_attn_packed_shape *) { return 0; }
+
+extern "C" int str_attn_prefill_packed(str_ctx *ctx, const str_attn_packed_shape *s, const void *q, const void *k, const void *v, const int32_t *q_start,
+                                       const int32_t *k_start, float softmax_scale, void *o, void *workspace, size_t workspace_bytes, void *stream) {
+    (void)workspace;
+    if (!ctx || !s || !q_start) return STR_ERR_INVALID_ARG;
+    if (s->n_seq <= 0 || s->rows_q < 0 || s->rows_k < 0 || s->Hq <= 0 || s->Hkv <= 0 || s->Hq % s->Hkv != 0 || s->d <= 0 ||
+        (s->dtype != STR_F32 && s->dtype != STR_BF16) || !(softmax_scale > 0.f) || !isfinite(softmax_scale * 1.4426950408889634f))
+        return STR_ERR_INVALID_ARG;
+    if (!k_start) {
+        if (s->rows_q != s->rows_k) return STR_ERR_INVALID_ARG;
+        k_start = q_start;
+    }
+    if (s->rows_q == 0) return STR_OK;
+    if (!q || !o || (s->rows_k > 0 && (!k || !v))) return STR_ERR_INVALID_ARG;
+    const int group = s->Hq / s->Hkv;
+    if (s->d > 128 || group > BR || s->n_seq > 32768 || s->rows_q > (1 << 30) || s->rows_k > (1 << 30) ||
+        ((long long)s->rows_q / (BR / group) + s->n_seq) * s->Hkv > INT32_MAX)
+        return STR_ERR_UNSUPPORTED_SHAPE;
+    const size_t es = dtype_size(s->dtype), qb = es * s->rows_q * s->Hq * s->d, kb = es * s->rows_k * s->Hkv * s->d;
+    if (kv4_overlap(q, qb, o, qb) || kv4_overlap(k, kb, o, qb) || kv4_overlap(v, kb, o, qb)) return STR_ERR_INVALID_ARG;
+    if (workspace_bytes < str_attn_prefill_packed_workspace_size(s)) return STR_ERR_WORKSPACE_TOO_SMALL;
+    StrDeviceScope dev(ctx);
+    if (!dev.ok) return STR_ERR_CUDA;
+    StrProfScope prof_scope(ctx, STR_CAT_ATTN_FWD, stream);
+    cudaStream_t st = (cudaStream_t)stream;
+    ++ctx->fallback_calls;
+    if (s->dtype == STR_BF16)
+        return s->d <= 64 ? launch<__nv_bfloat16, 64>(ctx, s, q, k, v, q_start, k_start, softmax_scale, o, st)
+                          : launch<__nv_bfloat16, 128>(ctx, s, q, k, v, q_start, k_start, softmax_scale, o, st);
+    return s->d <= 64 ? launch<float, 64>(ctx, s, q, k, v, q_start, k_start, softmax_scale, o, st)
+                      : launch<float, 128>(ctx, s, q, k, v, q_start, k_start, softmax_scale, o, st);
+}

@@ -1,0 +1,282 @@
+// str_mamba_conv_packed, str_mamba_conv_step: the Mamba block's pre-scan step with a window of earlier inputs,
+//   u_t = bias + sum_j w_j in_{t-W+1+j},   x | B | C = SiLU(u),   dt = softplus(raw + dt_bias),
+// where inputs before the sequence's first row come from its window (the last W - 1 inputs of what went before; zeros without one), and
+// the last W - 1 inputs go out as the next window.
+//
+// Bound by memory: every column of x | B | C | dt in once and out once.
+#include "packed.cuh"
+
+#define STR_DTYPE_OK(dt) ((dt) == STR_F32 || (dt) == STR_BF16)
+
+namespace {
+
+constexpr int THREADS = 256, TT = 32, UNROLL = 8;        // rows a block walks, rows whose loads are in flight together
+
+struct ConvDims {
+    int d_inner, gn, H, ch, ld;                           // ch = d_inner + 2 gn channels behind the d_inner columns of the gate
+};
+
+// VEC consecutive elements as they are stored.
+template <typename T, int VEC> struct alignas(VEC * sizeof(T)) Pack { T v[VEC]; };
+template <int VEC, typename T>
+__device__ __forceinline__ Pack<T, VEC> load_pack(const T *p) {
+    Pack<T, VEC> r;
+    if constexpr (VEC * sizeof(T) == 16) *(uint4 *)&r = __ldg((const uint4 *)p);
+    else if constexpr (VEC * sizeof(T) == 8) *(uint2 *)&r = __ldg((const uint2 *)p);
+    else
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) r.v[i] = p[i];
+    return r;
+}
+template <int VEC, typename T>
+__device__ __forceinline__ void store_pack(T *p, const Pack<T, VEC> &r) {
+    if constexpr (VEC * sizeof(T) == 16) *(uint4 *)p = *(const uint4 *)&r;
+    else if constexpr (VEC * sizeof(T) == 8) *(uint2 *)p = *(const uint2 *)&r;
+    else
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) p[i] = r.v[i];
+}
+template <typename T, int VEC>
+__device__ __forceinline__ Pack<T, VEC> zero_pack() {
+    Pack<T, VEC> r;
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) stf(&r.v[i], 0.f);
+    return r;
+}
+
+__device__ __forceinline__ float act(float u, const __nv_bfloat16 *) { return silu_fast(u); }
+__device__ __forceinline__ float act(float u, const float *) { return silu_f(u); }
+
+// Where a channel's outputs go: x, B or C, each [rows, width].
+template <typename T>
+__device__ __forceinline__ T *out_column(const ConvDims &c, int ch0, T *x, T *B, T *C, int &width) {
+    if (ch0 < c.d_inner) { width = c.d_inner; return x + ch0; }
+    width = c.gn;
+    return ch0 < c.d_inner + c.gn ? B + (ch0 - c.d_inner) : C + (ch0 - c.d_inner - c.gn);
+}
+
+template <typename T, int VEC, int W>
+struct Taps {
+    float w[VEC][W], bias[VEC];
+    __device__ __forceinline__ Taps(const float *conv_w, const float *conv_b, int ch0) {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+#pragma unroll
+            for (int j = 0; j < W; ++j) w[i][j] = __ldg(conv_w + (size_t)(ch0 + i) * W + j);
+            bias[i] = __ldg(conv_b + ch0 + i);
+        }
+    }
+    // Output row from the W - 1 rows before it (oldest first) and its own; moves the history on.
+    __device__ __forceinline__ Pack<T, VEC> apply(Pack<T, VEC> (&hist)[W - 1], const Pack<T, VEC> &cur) const {
+        Pack<T, VEC> o;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            float u = bias[i];
+#pragma unroll
+            for (int j = 0; j < W - 1; ++j) u = fmaf(w[i][j], ldf(&hist[j].v[i]), u);
+            u = fmaf(w[i][W - 1], ldf(&cur.v[i]), u);
+            stf(&o.v[i], act(u, (const T *)nullptr));
+        }
+#pragma unroll
+        for (int j = 0; j + 1 < W - 1; ++j) hist[j] = hist[j + 1];
+        hist[W - 2] = cur;
+        return o;
+    }
+};
+
+// Blocks (i, j): rows [TT i, TT i + TT) of the packed tensor, channels of column block j; the last j takes the dt columns.  Behind the row
+// tiles one block i per sequence copies its window, column block by column block.
+template <typename T, int VEC, int W>
+__global__ void __launch_bounds__(THREADS)
+conv_packed_kernel(ConvDims c, int n_seq, int rows, int tiles, const T *__restrict__ zx, const float *__restrict__ conv_w,
+                   const float *__restrict__ conv_b, const float *__restrict__ dt_bias, const int32_t *__restrict__ start,
+                   const T *__restrict__ window, T *__restrict__ x, T *__restrict__ B, T *__restrict__ C, float *__restrict__ dt,
+                   T *__restrict__ window_out, int *status) {
+    const bool dt_block = blockIdx.y == gridDim.y - 1;
+    const int ch0 = (blockIdx.y * THREADS + threadIdx.x) * VEC;
+    const T *src = zx + c.d_inner + ch0;                  // + row * ld
+    if ((int)blockIdx.x >= tiles) {
+        const int s = blockIdx.x - tiles;
+        if (dt_block) {
+            if (s == 0) packed_check(start, n_seq, rows, status);
+            return;
+        }
+        if (!window_out || ch0 >= c.ch) return;
+        const int s0 = packed_start(start, s, rows), T_s = max(packed_start(start, s + 1, rows) - s0, 0);
+#pragma unroll
+        for (int j = 0; j < W - 1; ++j) {
+            const int r = T_s - (W - 1) + j;              // row of the sequence, or (negative) of the window behind it
+            Pack<T, VEC> v = zero_pack<T, VEC>();
+            if (r >= 0) v = load_pack<VEC>(src + (size_t)(s0 + r) * c.ld);
+            else if (window) v = load_pack<VEC>(window + ((size_t)s * (W - 1) + r + W - 1) * c.ch + ch0);
+            store_pack<VEC>(window_out + ((size_t)s * (W - 1) + j) * c.ch + ch0, v);
+        }
+        return;
+    }
+    const int t0 = blockIdx.x * TT, t1 = min(rows, t0 + TT);
+    int s = packed_sequence_of(start, n_seq, t0);
+    if (dt_block) {
+        for (int e = threadIdx.x; e < (t1 - t0) * c.H; e += THREADS) {
+            const int t = t0 + e / c.H, h = e % c.H;
+            int st = s;
+            while (st < n_seq && __ldg(start + st + 1) <= t) ++st;
+            if (st >= 0 && st < n_seq) dt[(size_t)t * c.H + h] = softplus_f(ldf(zx + (size_t)t * c.ld + c.d_inner + c.ch + h) + dt_bias[h]);
+        }
+        return;
+    }
+    if (ch0 >= c.ch) return;
+    const Taps<T, VEC, W> taps(conv_w, conv_b, ch0);
+    int width;
+    T *dst = out_column(c, ch0, x, B, C, width);
+    Pack<T, VEC> hist[W - 1];
+    auto history = [&](int t) {                           // the W - 1 inputs before row t of sequence s
+        const int s0 = s >= 0 && s < n_seq ? min(packed_start(start, s, rows), t) : t;
+#pragma unroll
+        for (int j = 0; j < W - 1; ++j) {
+            const int r = t - (W - 1) + j;
+            hist[j] = zero_pack<T, VEC>();
+            if (s < 0 || s >= n_seq) continue;
+            if (r >= s0) hist[j] = load_pack<VEC>(src + (size_t)r * c.ld);
+            else if (window) hist[j] = load_pack<VEC>(window + ((size_t)s * (W - 1) + (r - s0 + W - 1)) * c.ch + ch0);
+        }
+    };
+    history(t0);
+    int next = s < n_seq ? __ldg(start + s + 1) : rows;   // where the next sequence begins
+#pragma unroll 1
+    for (int tb = t0; tb < t1; tb += UNROLL) {
+        Pack<T, VEC> raw[UNROLL];
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) raw[u] = tb + u < t1 ? load_pack<VEC>(src + (size_t)(tb + u) * c.ld) : zero_pack<T, VEC>();
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) {
+            const int t = tb + u;
+            if (t < t1) {
+                if (t >= next && s < n_seq) {
+                    while (s < n_seq && __ldg(start + s + 1) <= t) ++s;
+                    next = s < n_seq ? __ldg(start + s + 1) : rows;
+                    history(t);
+                }
+                const Pack<T, VEC> o = taps.apply(hist, raw[u]);
+                if (s >= 0 && s < n_seq) store_pack<VEC>(dst + (size_t)t * width, o);
+            }
+        }
+    }
+}
+
+// A few tokens per sequence: a thread takes VEC channels of one sequence, window in registers.  The window may be written where it was read.
+template <typename T, int VEC, int W>
+__global__ void __launch_bounds__(THREADS)
+conv_step_kernel(ConvDims c, int T_new, const T *__restrict__ zx, const float *__restrict__ conv_w, const float *__restrict__ conv_b,
+                 const float *__restrict__ dt_bias, const T *window, T *__restrict__ x, T *__restrict__ B, T *__restrict__ C,
+                 float *__restrict__ dt, T *window_out) {
+    const int b = blockIdx.x;
+    const size_t row0 = (size_t)b * T_new;
+    if (blockIdx.y == gridDim.y - 1) {
+        for (int e = threadIdx.x; e < T_new * c.H; e += THREADS) {
+            const int t = e / c.H, h = e % c.H;
+            dt[(row0 + t) * c.H + h] = softplus_f(ldf(zx + (row0 + t) * c.ld + c.d_inner + c.ch + h) + dt_bias[h]);
+        }
+        return;
+    }
+    const int ch0 = (blockIdx.y * THREADS + threadIdx.x) * VEC;
+    if (ch0 >= c.ch) return;
+    Pack<T, VEC> hist[W - 1];
+#pragma unroll
+    for (int j = 0; j < W - 1; ++j) hist[j] = load_pack<VEC>(window + ((size_t)b * (W - 1) + j) * c.ch + ch0);
+    const Taps<T, VEC, W> taps(conv_w, conv_b, ch0);
+    int width;
+    T *dst = out_column(c, ch0, x, B, C, width);
+    for (int t = 0; t < T_new; ++t) store_pack<VEC>(dst + (row0 + t) * width, taps.apply(hist, load_pack<VEC>(zx + (row0 + t) * c.ld + c.d_inner + ch0)));
+#pragma unroll
+    for (int j = 0; j < W - 1; ++j) store_pack<VEC>(window_out + ((size_t)b * (W - 1) + j) * c.ch + ch0, hist[j]);
+}
+
+// What both entry points are given.
+struct ConvCall {
+    ConvDims c;
+    int n_seq, rows;                                      // conv_step: sequences and tokens per sequence
+    const void *zx, *window;
+    const float *conv_w, *conv_b, *dt_bias;
+    const int32_t *start;
+    void *x, *B, *C, *window_out;
+    float *dt;
+    int *status;
+};
+
+template <typename T, int VEC, int W>
+void launch(const ConvCall &k, bool step, cudaStream_t st) {
+    const int cols = ceil_div(ceil_div(k.c.ch, VEC), THREADS) + 1;
+    if (step) {
+        conv_step_kernel<T, VEC, W><<<dim3(k.n_seq, cols), THREADS, 0, st>>>(k.c, k.rows, (const T *)k.zx, k.conv_w, k.conv_b, k.dt_bias,
+                                                                             (const T *)k.window, (T *)k.x, (T *)k.B, (T *)k.C, k.dt, (T *)k.window_out);
+    } else {
+        const int tiles = ceil_div(k.rows, TT);
+        conv_packed_kernel<T, VEC, W><<<dim3(tiles + k.n_seq, cols), THREADS, 0, st>>>(
+            k.c, k.n_seq, k.rows, tiles, (const T *)k.zx, k.conv_w, k.conv_b, k.dt_bias, k.start, (const T *)k.window, (T *)k.x, (T *)k.B, (T *)k.C, k.dt,
+            (T *)k.window_out, k.status);
+    }
+}
+template <typename T, int VEC>
+void dispatch_width(const ConvCall &k, int W, bool step, cudaStream_t st) {
+    if (W == 2) launch<T, VEC, 2>(k, step, st);
+    else if (W == 3) launch<T, VEC, 3>(k, step, st);
+    else launch<T, VEC, 4>(k, step, st);
+}
+// Four channels a thread where rows, columns and pointers allow vector accesses, else one.
+template <typename T>
+void dispatch_vec(const ConvCall &k, int W, bool step, cudaStream_t st) {
+    constexpr int VEC = 4;
+    const uintptr_t at = (uintptr_t)k.zx | (uintptr_t)k.window | (uintptr_t)k.window_out | (uintptr_t)k.x | (uintptr_t)k.B | (uintptr_t)k.C;
+    if (k.c.d_inner % VEC == 0 && k.c.gn % VEC == 0 && k.c.ld % VEC == 0 && at % (VEC * sizeof(T)) == 0) dispatch_width<T, VEC>(k, W, step, st);
+    else dispatch_width<T, 1>(k, W, step, st);
+}
+
+int check_dims(int dtype, int H, int p, int n, int G, int W, ConvDims *c) {
+    if (H <= 0 || p <= 0 || n <= 0 || G <= 0 || H % G != 0 || W <= 0 || !STR_DTYPE_OK(dtype)) return STR_ERR_INVALID_ARG;
+    const long long d_inner = (long long)H * p, gn = (long long)G * n, ld = 2 * d_inner + 2 * gn + H;
+    if (W < 2 || W > 4 || d_inner > (1 << 24) || gn > (1 << 24)) return STR_ERR_UNSUPPORTED_SHAPE;
+    *c = {(int)d_inner, (int)gn, H, (int)(d_inner + 2 * gn), (int)ld};
+    return STR_OK;
+}
+
+}  // namespace
+
+extern "C" int str_mamba_conv_packed(str_ctx *ctx, int dtype, int n_seq, int rows, int H, int p, int n, int G, int W, const void *zxbcdt,
+                                     const float *conv_w, const float *conv_b, const float *dt_bias, const int32_t *seq_start, const void *window,
+                                     void *x_out, void *B_out, void *C_out, float *dt_out, void *window_out, void *stream) {
+    ConvDims c;
+    if (!ctx || !conv_w || !conv_b || !dt_bias || !seq_start || n_seq <= 0 || rows < 0) return STR_ERR_INVALID_ARG;
+    if (rows > 0 && (!zxbcdt || !x_out || !B_out || !C_out || !dt_out)) return STR_ERR_INVALID_ARG;
+    const int rc = check_dims(dtype, H, p, n, G, W, &c);
+    if (rc != STR_OK) return rc;
+    if (n_seq > 65535 || rows > (1 << 30)) return STR_ERR_UNSUPPORTED_SHAPE;
+    const size_t es = dtype_size(dtype), wb = (size_t)n_seq * (W - 1) * c.ch * es;
+    if (kv4_overlap(window, wb, window_out, wb)) return STR_ERR_INVALID_ARG;
+    StrDeviceScope dev(ctx);
+    if (!dev.ok) return STR_ERR_CUDA;
+    StrProfScope prof_scope(ctx, STR_CAT_ELEMENTWISE, stream);
+    const ConvCall k = {c, n_seq, rows, zxbcdt, window, conv_w, conv_b, dt_bias, seq_start, x_out, B_out, C_out, window_out, dt_out, ctx->status_dev};
+    if (dtype == STR_BF16) dispatch_vec<__nv_bfloat16>(k, W, false, (cudaStream_t)stream);
+    else dispatch_vec<float>(k, W, false, (cudaStream_t)stream);
+    return str_launch_ok(ctx);
+}
+
+extern "C" int str_mamba_conv_step(str_ctx *ctx, int dtype, int Bz, int T, int H, int p, int n, int G, int W, const void *zxbcdt,
+                                   const float *conv_w, const float *conv_b, const float *dt_bias, const void *window, void *x_out, void *B_out,
+                                   void *C_out, float *dt_out, void *window_out, void *stream) {
+    ConvDims c;
+    if (!ctx || !zxbcdt || !conv_w || !conv_b || !dt_bias || !window || !x_out || !B_out || !C_out || !dt_out || !window_out || Bz <= 0 || T <= 0)
+        return STR_ERR_INVALID_ARG;
+    const int rc = check_dims(dtype, H, p, n, G, W, &c);
+    if (rc != STR_OK) return rc;
+    if ((long long)Bz * T > (1 << 30)) return STR_ERR_UNSUPPORTED_SHAPE;
+    const size_t es = dtype_size(dtype), wb = (size_t)Bz * (W - 1) * c.ch * es;
+    if (window != window_out && kv4_overlap(window, wb, window_out, wb)) return STR_ERR_INVALID_ARG;
+    StrDeviceScope dev(ctx);
+    if (!dev.ok) return STR_ERR_CUDA;
+    StrProfScope prof_scope(ctx, STR_CAT_ELEMENTWISE, stream);
+    const ConvCall k = {c, Bz, T, zxbcdt, window, conv_w, conv_b, dt_bias, nullptr, x_out, B_out, C_out, window_out, dt_out, ctx->status_dev};
+    if (dtype == STR_BF16) dispatch_vec<__nv_bfloat16>(k, W, true, (cudaStream_t)stream);
+    else dispatch_vec<float>(k, W, true, (cudaStream_t)stream);
+    return str_launch_ok(ctx);
+}

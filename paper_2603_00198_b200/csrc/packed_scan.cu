@@ -1,0 +1,138 @@
+// str_mamba2_prefill_packed: the Mamba-2 recurrence over packed sequences, each from a state of its own,
+//   S <- exp(dt A_h) S + (dt x) b^T,   y = S c + D_h x.
+// The entry point, and the kernel that runs the recurrence token by token in fp32: every type and shape.
+//
+// A row of the state (one of p) lies across four lanes, NV vectors of four columns each; a block holds the rows of one head of one
+// sequence in registers from the first token to the last.  Tokens come through shared memory TB at a time.  Per token and head that is
+// p n (one multiplication and two fused ones): as many operations as the chunked form in fp32 needs, without its two roundings more, and a
+// state that never leaves the registers.
+#include "dispatch.cuh"
+#include "packed.cuh"
+
+namespace {
+
+constexpr int LPR = 4, TB = 32, MAX_THREADS = 256;        // lanes per row, tokens per turn
+
+template <typename T, int NV>
+__global__ void __launch_bounds__(MAX_THREADS)
+scan_packed_kernel(int n_seq, int rows, int H, int p, int n, int G, const T *__restrict__ x, const float *__restrict__ dt, const float *__restrict__ A,
+                   const T *__restrict__ B, const T *__restrict__ C, const float *__restrict__ Dskip, const int32_t *__restrict__ start,
+                   const float *state, T *__restrict__ y, float *final_state, int *status) {
+    constexpr int NP = NV * 4 * LPR;                      // columns, padded
+    extern __shared__ float4 smem4[];
+    float *bs = (float *)smem4, *cs = bs + TB * NP, *xs = cs + TB * NP;
+    const int R = blockDim.x / LPR;                       // rows of the state per block
+    float *ys = xs + TB * R, *dts = ys + TB * R, *decay = dts + TB;
+    const int h = blockIdx.y, s = blockIdx.z, g = h / (H / G);
+    const int i0 = blockIdx.x * R, r = threadIdx.x / LPR, l = threadIdx.x % LPR;
+    if (blockIdx.x == 0 && h == 0 && s == 0) packed_check(start, n_seq, rows, status);
+    const int t0 = packed_start(start, s, rows), t1 = packed_start(start, s + 1, rows);
+    if (t1 <= t0 && (!final_state || (state == final_state))) return;
+    const size_t base = (((size_t)s * H + h) * p + i0 + r) * n;
+    float S[NV][4];
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int col = (v * LPR + l) * 4 + i;
+            S[v][i] = state && i0 + r < p && col < n ? state[base + col] : 0.f;
+        }
+    const float Ah = A[h], Dh = Dskip ? Dskip[h] : 0.f;
+    for (int tb = t0; tb < t1; tb += TB) {
+        const int m = min(TB, t1 - tb);
+        __syncthreads();
+        for (int e = threadIdx.x; e < m * NP; e += blockDim.x) {
+            const int t = e / NP, col = e % NP;
+            const size_t at = ((size_t)(tb + t) * G + g) * n + col;
+            bs[e] = col < n ? ldf(B + at) : 0.f;
+            cs[e] = col < n ? ldf(C + at) : 0.f;
+        }
+        for (int e = threadIdx.x; e < m * R; e += blockDim.x) {
+            const int t = e / R, i = e % R;
+            xs[e] = i0 + i < p ? ldf(x + ((size_t)(tb + t) * H + h) * p + i0 + i) : 0.f;
+        }
+        if (threadIdx.x < m) {
+            const float d = dt[(size_t)(tb + threadIdx.x) * H + h];
+            dts[threadIdx.x] = d;
+            decay[threadIdx.x] = expf(d * Ah);
+        }
+        __syncthreads();
+#pragma unroll 2
+        for (int t = 0; t < m; ++t) {
+            const float xv = xs[t * R + r], dx = dts[t] * xv, a = decay[t];
+            float acc[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                const float4 b = *(const float4 *)(bs + t * NP + (v * LPR + l) * 4), c = *(const float4 *)(cs + t * NP + (v * LPR + l) * 4);
+                S[v][0] = fmaf(a, S[v][0], dx * b.x); acc[0] = fmaf(S[v][0], c.x, acc[0]);
+                S[v][1] = fmaf(a, S[v][1], dx * b.y); acc[1] = fmaf(S[v][1], c.y, acc[1]);
+                S[v][2] = fmaf(a, S[v][2], dx * b.z); acc[2] = fmaf(S[v][2], c.z, acc[2]);
+                S[v][3] = fmaf(a, S[v][3], dx * b.w); acc[3] = fmaf(S[v][3], c.w, acc[3]);
+            }
+            float sum = (acc[0] + acc[1]) + (acc[2] + acc[3]);
+#pragma unroll
+            for (int o = 1; o < LPR; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            if (l == 0) ys[t * R + r] = fmaf(Dh, xv, sum);
+        }
+        __syncthreads();
+        for (int e = threadIdx.x; e < m * R; e += blockDim.x) {
+            const int t = e / R, i = e % R;
+            if (i0 + i < p) stf(y + ((size_t)(tb + t) * H + h) * p + i0 + i, ys[e]);
+        }
+    }
+    if (!final_state) return;
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int col = (v * LPR + l) * 4 + i;
+            if (i0 + r < p && col < n) final_state[base + col] = S[v][i];
+        }
+}
+
+template <typename T, int NV>
+int launch(str_ctx *ctx, const str_ssd_packed_shape *s, const void *x, const float *dt, const float *A, const void *B, const void *C, const float *D,
+           const int32_t *start, const float *state, void *y, float *final_state, cudaStream_t st) {
+    const int warps = s->p >= 64 ? 8 : (s->p * LPR + 31) / 32, threads = 32 * warps, R = threads / LPR;
+    const size_t smem = sizeof(float) * ((size_t)TB * (2 * NV * 4 * LPR + 2 * R) + 2 * TB);
+    if (smem > 48 * 1024) STR_CUDA_OK(cudaFuncSetAttribute(scan_packed_kernel<T, NV>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    scan_packed_kernel<T, NV><<<dim3(ceil_div(s->p, R), s->H, s->n_seq), threads, smem, st>>>(
+        s->n_seq, s->rows, s->H, s->p, s->n, s->G, (const T *)x, dt, A, (const T *)B, (const T *)C, D, start, state, (T *)y, final_state, ctx->status_dev);
+    return str_launch_ok(ctx);
+}
+template <typename T>
+int dispatch(str_ctx *ctx, const str_ssd_packed_shape *s, const void *x, const float *dt, const float *A, const void *B, const void *C, const float *D,
+             const int32_t *start, const float *state, void *y, float *final_state, cudaStream_t st) {
+    const int need = ceil_div(s->n, 4 * LPR);
+#define SCAN(NV) launch<T, NV>(ctx, s, x, dt, A, B, C, D, start, state, y, final_state, st)
+    return need <= 1 ? SCAN(1) : need <= 2 ? SCAN(2) : need <= 4 ? SCAN(4) : need <= 8 ? SCAN(8) : SCAN(16);
+#undef SCAN
+}
+
+}  // namespace
+
+extern "C" size_t str_mamba2_prefill_packed_workspace_size(const str_ssd_packed_shape *) { return 0; }
+
+extern "C" int str_mamba2_prefill_packed(str_ctx *ctx, const str_ssd_packed_shape *s, const void *x, const float *dt, const float *A, const void *B,
+                                         const void *C, const float *D, const int32_t *seq_start, const float *init_state, void *y,
+                                         float *final_state, void *workspace, size_t workspace_bytes, void *stream) {
+    (void)workspace;
+    if (!ctx || !s || !A || !seq_start) return STR_ERR_INVALID_ARG;
+    if (s->n_seq <= 0 || s->rows < 0 || s->H <= 0 || s->p <= 0 || s->n <= 0 || s->G <= 0 || s->H % s->G != 0 ||
+        (s->dtype != STR_F32 && s->dtype != STR_BF16))
+        return STR_ERR_INVALID_ARG;
+    if (s->rows > 0 && (!x || !dt || !B || !C || !y)) return STR_ERR_INVALID_ARG;
+    if (s->n > 256 || s->n_seq > 65535 || s->H > 65535 || s->rows > (1 << 30) || s->p > (1 << 20)) return STR_ERR_UNSUPPORTED_SHAPE;
+    const size_t state_bytes = (size_t)s->n_seq * s->H * s->p * s->n * sizeof(float), es = dtype_size(s->dtype);
+    const size_t xb = (size_t)s->rows * s->H * s->p * es, bb = (size_t)s->rows * s->G * s->n * es;
+    if (final_state != init_state && kv4_overlap(init_state, state_bytes, final_state, state_bytes)) return STR_ERR_INVALID_ARG;
+    if (kv4_overlap(x, xb, y, xb) || kv4_overlap(B, bb, y, xb) || kv4_overlap(C, bb, y, xb)) return STR_ERR_INVALID_ARG;
+    if (workspace_bytes < str_mamba2_prefill_packed_workspace_size(s)) return STR_ERR_WORKSPACE_TOO_SMALL;
+    StrDeviceScope dev(ctx);
+    if (!dev.ok) return STR_ERR_CUDA;
+    StrProfScope prof_scope(ctx, STR_CAT_SSD, stream);
+    cudaStream_t st = (cudaStream_t)stream;
+    ++ctx->fallback_calls;
+    if (s->dtype == STR_BF16) return dispatch<__nv_bfloat16>(ctx, s, x, dt, A, B, C, D, seq_start, init_state, y, final_state, st);
+    return dispatch<float>(ctx, s, x, dt, A, B, C, D, seq_start, init_state, y, final_state, st);
+}

@@ -1,0 +1,168 @@
+"""What the entry points on packed sequences refuse on the host, before anything touches CUDA: through the C ABI with addresses that nothing may
+follow, and through the module that marshals them with host tensors."""
+import ctypes
+import os
+import subprocess
+import sys
+
+import pytest
+import torch
+
+from paper_2603_00198_b200 import binding
+
+INVALID, UNSUPPORTED, NO_DEVICE = -1, -2, -4
+no_device = pytest.mark.skipif(torch.cuda.is_available(), reason="the addresses are not real")
+
+
+class Call:
+    def __init__(self):
+        self.ctx = ctypes.create_string_buffer(4096)
+        self.next = 1 << 20
+
+    def buffer(self):
+        self.next += 1 << 34
+        return self.next
+
+    def _args(self, names, given):
+        a = {n: self.buffer() for n in names}
+        a.update({n: given.pop(n) for n in list(given) if n in a})
+        assert not given, given
+        return a
+
+    def conv(self, step=False, dtype=1, n_seq=3, rows=50, H=4, p=16, n=8, G=2, W=4, ctx=True, **at):
+        a = self._args(("zx", "w", "b", "bias", "start", "window", "x", "B", "C", "dt", "wout"), at)
+        f = binding.lib().str_mamba_conv_step if step else binding.lib().str_mamba_conv_packed
+        ptrs = [a[k] for k in ("zx", "w", "b", "bias")] + ([] if step else [a["start"]]) + [a[k] for k in ("window", "x", "B", "C", "dt", "wout")]
+        return f(ctypes.addressof(self.ctx) if ctx else None, dtype, n_seq, rows, H, p, n, G, W, *ptrs, None)
+
+    def scan(self, n_seq=3, rows=50, H=4, p=16, n=8, G=2, dtype=1, **at):
+        a = self._args(("x", "dt", "A", "B", "C", "D", "start", "init", "y", "final"), at)
+        s = binding.SsdPackedShape(n_seq, rows, H, p, n, G, dtype)
+        return binding.lib().str_mamba2_prefill_packed(ctypes.addressof(self.ctx), ctypes.addressof(s), *(a[k] for k in ("x", "dt", "A", "B", "C", "D", "start", "init", "y", "final")),
+                                                       None, 0, None)
+
+    def attn(self, n_seq=3, rows_q=50, rows_k=50, Hq=4, Hkv=2, d=64, dtype=1, scale=0.1, **at):
+        a = self._args(("q", "k", "v", "qs", "ks", "o"), at)
+        s = binding.AttnPackedShape(n_seq, rows_q, rows_k, Hq, Hkv, d, dtype)
+        need = binding.lib().str_attn_prefill_packed_workspace_size(ctypes.addressof(s))
+        return binding.lib().str_attn_prefill_packed(ctypes.addressof(self.ctx), ctypes.addressof(s), *(a[k] for k in ("q", "k", "v", "qs", "ks")), scale, a["o"],
+                                                     self.buffer() if need else None, need, None)
+
+    def rope(self, rows=9, Hq=4, Hkv=2, d=64, dtype=1, at=None, **desc):
+        a = self._args(("pos", "qkv", "q", "k", "v"), dict(at or {}))
+        r = dict(rot_dim=32, layout=0, scaling=0, trained_len=100, theta=1e4, factor=2.0, turns_low=1.0, turns_high=32.0, amplitude=1.0)
+        r.update(desc)
+        s = binding.RopeDesc(**r)
+        return binding.lib().str_rope_split_ex(ctypes.addressof(self.ctx), ctypes.addressof(s), dtype, rows, Hq, Hkv, d, *(a[k] for k in ("pos", "qkv", "q", "k", "v")), None)
+
+
+@no_device
+@pytest.mark.parametrize("step", [False, True])
+def test_convolution(step):
+    assert Call().conv(step) == NO_DEVICE
+    for bad in (dict(n_seq=0), dict(rows=-1), dict(H=0), dict(p=0), dict(n=0), dict(G=0), dict(G=3), dict(W=0), dict(dtype=2), dict(ctx=False), dict(w=None), dict(b=None),
+                dict(bias=None), dict(zx=None), dict(x=None), dict(B=None), dict(C=None), dict(dt=None)):
+        assert Call().conv(step, **bad) == INVALID, bad
+    for bad in (dict(W=1), dict(W=5)):
+        assert Call().conv(step, **bad) == UNSUPPORTED, bad
+    size = 3 * 3 * 96 * 2                                   # bytes of the windows
+    assert Call().conv(step, window=1 << 40, wout=(1 << 40) + size - 2) == INVALID
+    assert Call().conv(step, window=1 << 40, wout=(1 << 40) + size) == NO_DEVICE
+    assert Call().conv(step, window=1 << 40, wout=1 << 40) == (NO_DEVICE if step else INVALID)
+    if step:
+        assert Call().conv(step, window=None) == INVALID and Call().conv(step, wout=None) == INVALID and Call().conv(step, rows=0) == INVALID
+    else:
+        assert Call().conv(window=None) == NO_DEVICE and Call().conv(wout=None) == NO_DEVICE and Call().conv(start=None) == INVALID
+        assert Call().conv(rows=0, zx=None, x=None, B=None, C=None, dt=None) == NO_DEVICE
+        assert Call().conv(n_seq=65536) == UNSUPPORTED and Call().conv(rows=(1 << 30) + 1) == UNSUPPORTED
+
+
+@no_device
+def test_scan():
+    assert Call().scan() == NO_DEVICE
+    for bad in (dict(n_seq=0), dict(rows=-1), dict(H=0), dict(p=0), dict(n=0), dict(G=0), dict(G=3), dict(dtype=3), dict(x=None), dict(dt=None), dict(A=None), dict(B=None),
+                dict(C=None), dict(start=None), dict(y=None)):
+        assert Call().scan(**bad) == INVALID, bad
+    for bad in (dict(n=257), dict(n_seq=65536), dict(rows=(1 << 30) + 1)):
+        assert Call().scan(**bad) == UNSUPPORTED, bad
+    for free in (dict(D=None), dict(init=None), dict(final=None), dict(rows=0, x=None, dt=None, B=None, C=None, y=None)):
+        assert Call().scan(**free) == NO_DEVICE, free
+    at, size = 1 << 40, 3 * 4 * 16 * 8 * 4
+    assert Call().scan(init=at, final=at) == NO_DEVICE and Call().scan(init=at, final=at + 4) == INVALID and Call().scan(init=at, final=at + size) == NO_DEVICE
+    for name in ("x", "B", "C"):
+        assert Call().scan(**{name: at, "y": at}) == INVALID, name
+
+
+@no_device
+def test_attention():
+    assert Call().attn() == NO_DEVICE
+    for bad in (dict(n_seq=0), dict(rows_q=-1), dict(rows_k=-1), dict(Hq=0), dict(Hkv=0), dict(Hq=3), dict(d=0), dict(dtype=2), dict(q=None), dict(k=None), dict(v=None),
+                dict(o=None), dict(qs=None), dict(ks=None, rows_k=49)):
+        assert Call().attn(**bad) == INVALID, bad
+    for scale in (0.0, -1.0, float("nan"), float("inf"), 3.0e38):
+        assert Call().attn(scale=scale) == INVALID, scale
+    for bad in (dict(d=129), dict(Hq=129, Hkv=1), dict(n_seq=32769), dict(rows_q=(1 << 30) + 1), dict(rows_k=(1 << 30) + 1)):
+        assert Call().attn(**bad) == UNSUPPORTED, bad
+    assert Call().attn(ks=None) == NO_DEVICE and Call().attn(rows_k=0, k=None, v=None) == NO_DEVICE
+    assert Call().attn(rows_q=0) == 0
+    at = 1 << 40
+    for name in ("q", "k", "v"):
+        assert Call().attn(**{name: at, "o": at}) == INVALID, name
+
+
+@no_device
+def test_rotary():
+    assert Call().rope() == NO_DEVICE
+    for bad in (dict(rot_dim=0), dict(rot_dim=33), dict(rot_dim=66), dict(layout=2), dict(scaling=3), dict(theta=0.0), dict(theta=float("nan")), dict(amplitude=float("inf")),
+                dict(scaling=1, factor=0.0), dict(scaling=2, factor=-1.0), dict(scaling=2, trained_len=0), dict(scaling=2, turns_low=32.0), dict(scaling=2, turns_high=float("nan")),
+                dict(rows=-1), dict(Hq=0), dict(Hkv=0), dict(d=0), dict(dtype=2), dict(at=dict(pos=None)), dict(at=dict(qkv=None)), dict(at=dict(v=None)),
+                dict(at=dict(qkv=1 << 40, q=1 << 40)), dict(at=dict(qkv=1 << 40, v=(1 << 40) + 64))):
+        assert Call().rope(**bad) == INVALID, bad
+    assert Call().rope(d=300, rot_dim=258) == UNSUPPORTED and Call().rope(d=65, layout=1) == UNSUPPORTED and Call().rope(d=65) == NO_DEVICE
+    assert Call().rope(rows=0, at=dict(pos=None, qkv=None, q=None, k=None, v=None)) == 0
+
+
+def test_the_description_of_a_rotary_embedding_is_checked():
+    with pytest.raises(ValueError, match="layout"):
+        binding.Rope(1e4, 64, "neox")
+    with pytest.raises(ValueError, match="scaling"):
+        binding.Rope(1e4, 64, scaling="dynamic")
+
+
+def test_tensors_are_checked():
+    m, i32 = binding._marshal(), lambda *s: torch.zeros(s, dtype=torch.int32)
+    for f, n in ((m.rope, 8), (m.conv_packed, 17), (m.conv_step, 14), (m.scan_packed, 12), (m.attn_packed, 9)):
+        with pytest.raises(TypeError, match="arguments"):
+            f(1, 2)
+    q, w = torch.zeros(5, 2, 64), torch.zeros(2 * 16 + 2 * 8, 4)
+    r = binding.Rope(1e4, 64)
+    with pytest.raises(ValueError, match="expected a tensor on cuda:0, got cpu"):
+        m.attn_packed(0, 0, q, q, q, i32(2), None, 0.1, None)
+    with pytest.raises(ValueError, match="q_start: expected n_seq"):
+        m.attn_packed(0, 0, q, q, q, i32(1), None, 0.1, None)
+    with pytest.raises(ValueError, match="q: expected 3 dimensions"):
+        m.attn_packed(0, 0, q[0], q, q, i32(2), None, 0.1, None)
+    with pytest.raises(TypeError, match="unsupported dtype"):
+        m.attn_packed(0, 0, q.half(), q, q, i32(2), None, 0.1, None)
+    with pytest.raises(ValueError, match="expected a tensor on cuda:0, got cpu"):
+        m.rope(0, 0, r.desc_ref, torch.zeros(3, 4 * 64), i32(3), 2, 1, 64)
+    with pytest.raises(ValueError, match="Hq: 0 is out of range"):
+        m.rope(0, 0, r.desc_ref, torch.zeros(3, 4 * 64), i32(3), 0, 1, 64)
+    zx = torch.zeros(6, 2 * 32 + 2 * 8 + 2)
+    with pytest.raises(ValueError, match="expected a tensor on cuda:0, got cpu"):
+        m.conv_packed(0, 0, zx, w, w[:, 0], w[:2, 0], 2, 16, 8, 1, i32(2), None, None, None, None, None, None)
+    with pytest.raises(ValueError, match="expected a tensor on cuda:0, got cpu"):
+        m.conv_step(0, 0, zx, w, w[:, 0], w[:2, 0], 2, 16, 8, 1, zx, 2, 3, zx)
+    with pytest.raises(ValueError, match="expected a tensor on cuda:0, got cpu"):
+        m.scan_packed(0, 0, q, q, q, q, q, i32(2), None, None, None, None)
+
+
+def test_a_call_before_setup_is_refused():
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    code = ("import torch\nfrom paper_2603_00198_b200 import _marshal as m\n"
+            "for f in (lambda: m.rope(*[0] * 8), lambda: m.setup_packed(*[0] * 7)):\n"
+            "    try:\n        f()\n    except RuntimeError as e:\n        assert 'setup' in str(e)\n        print('refused')\n"
+            "m.setup(print, 0, *[1] * 7)\n"
+            "try:\n    m.setup_packed(*[0] * 7)\nexcept ValueError:\n    print('refused')\n")
+    res = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
+    assert res.returncode == 0 and res.stdout.split() == ["refused"] * 3, res.stderr[-3000:]
