@@ -95,3 +95,7 @@ int str_gated_rmsnorm_gather(str_ctx *ctx, int dtype, int Bz, int T_in, int n_vi
 int str_mamba_conv_split_rows(str_ctx *ctx, int dtype, int Bz, int T, int H, int p, int n, int G, int W, bool has_z,
                               const void *zxbcdt, const float *conv_w, const float *conv_b, const float *dt_bias,
                               void *x_out, void *B_out, void *C_out, float *dt_out, void *stream);
+// Packed sequences on the tensor cores (bf16).
+bool str_attn_packed_tc_supported(const str_attn_packed_shape *s, const void *q, const void *k, const void *v, const void *o);
+int str_attn_packed_tc(str_ctx *ctx, const str_attn_packed_shape *s, const void *q, const void *k, const void *v, const int32_t *q_start,
+                       const int32_t *k_start, float scale, void *o, cudaStream_t st);

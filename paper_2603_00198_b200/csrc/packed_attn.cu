@@ -200,6 +200,8 @@ extern "C" int str_attn_prefill_packed(str_ctx *ctx, const str_attn_packed_shape
     if (!dev.ok) return STR_ERR_CUDA;
     StrProfScope prof_scope(ctx, STR_CAT_ATTN_FWD, stream);
     cudaStream_t st = (cudaStream_t)stream;
+    if (!str_force_simt() && str_attn_packed_tc_supported(s, q, k, v, o))
+        return ++ctx->tc_calls, str_attn_packed_tc(ctx, s, q, k, v, q_start, k_start, softmax_scale, o, st);
     ++ctx->fallback_calls;
     if (s->dtype == STR_BF16)
         return s->d <= 64 ? launch<__nv_bfloat16, 64>(ctx, s, q, k, v, q_start, k_start, softmax_scale, o, st)

@@ -1,0 +1,404 @@
+// Causal attention of packed sequences on tcgen05 tensor cores (bf16 in/out, fp32 accumulate, head sizes up to 128 that are multiples of 8).
+//
+// Rows are (query, head) pairs: the 128 rows of a tile are 128 / R consecutive queries of one sequence for the R query heads of one key head, so
+// that a key tile is fetched once for all of them and a turn of a few queries still fills the tile.  A CTA owns two such tiles that take turns on
+// the tensor pipe; the softmax of one overlaps the products of the other.  Per key tile j of 128 keys and row tile i:
+//   S_i  = Q_i K_j^T                 both operands K-major in shared memory (TMA, 128-byte swizzle, columns beyond d read as zero)
+//   P_i  = exp2(c S_i - c m_i)       one thread per row; running maximum m_i and sum l_i in fp32; P_i is narrowed to bf16 (relative error 2^-8 of each
+//                                    weight at most, random in sign: what the tensor pipe takes) over the first 64 columns of S_i, and is the A
+//                                    operand of
+//   O_i += P_i V_j                   A from tensor memory, V MN-major; issued half by half, as soon as 64 keys' weights are there
+//   out  = O_i / l_i
+// O_i is rescaled only when a row's maximum grows by more than 2^8: until then the stale maximum stays in use, which divides out through l_i.
+//
+// What a row does not see must not reach it.  Hidden scores are replaced before the maximum, so anything may stand there.  Hidden values meet weights of
+// zero in the product, and zero times infinity or NaN is NaN: rows of V behind the sequence are zeroed in shared memory, and the tiles that some
+// row of the CTA sees in part only are looked through for values that are not finite.  A CTA that found one computes its rows anew, row by row
+// (attn_row): right, slow and rare.
+//
+// Tensor memory (512 columns): S_0 | S_1 | O_0 | O_1, 128 columns each.
+// Warps: 0-3 softmax of tile 0, 4-7 softmax of tile 1 (warp w may touch TMEM lanes 32 (w % 4)...), 8 TMA producer (Q once, then a 2-slot ring for K and
+// one for V), 9 MMA issuer, 10 the guard that zeroes and looks through tiles of V.
+// Every mbarrier wait is bounded; a give-up records STR_ERR_TIMEOUT and the CTA tears down.
+#include "dispatch.cuh"
+#include "packed.cuh"
+#include "tc_common.cuh"
+
+namespace {
+
+constexpr int BQ = 128, BKV = 128, TILE_16K = 16384;      // rows x 64 bf16
+enum { B_Q = 0, B_KF, B_KE = B_KF + 2, B_VF = B_KE + 2, B_VR = B_VF + 2, B_VE = B_VR + 2, B_SF = B_VE + 2, B_PA = B_SF + 2, B_PB = B_PA + 2, B_OF = B_PB + 2,
+       B_COUNT = B_OF + 2 };
+constexpr int NUM_WARPS = 11, NUM_THREADS = NUM_WARPS * 32;
+constexpr uint32_t TM_S = 0, TM_O = 256;
+constexpr float RESCALE_THRESHOLD = 8.0f;                 // in log2 units
+
+template <int HD> struct Smem {
+    static constexpr int TILE = HD / 64 * TILE_16K;       // one tile of Q, K or V
+    static constexpr int Q = 0, K = 2 * TILE, V = 4 * TILE, MISC = 6 * TILE;
+    static constexpr size_t BYTES = (size_t)MISC + B_COUNT * 8 + 32 + sizeof(PackedBlock);
+};
+
+// One row's output in fp32 arithmetic, by one warp: a lane takes a key for the scores and every 32nd column for the values.
+__device__ __noinline__ void attn_row(const __nv_bfloat16 *q, const __nv_bfloat16 *k, const __nv_bfloat16 *v, __nv_bfloat16 *o, size_t ld, int keys, int d,
+                                      float scale_log2) {
+    const int lane = threadIdx.x & 31;
+    float m = -INFINITY, l = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int j0 = 0; j0 < keys; j0 += 32) {
+        float s = -INFINITY;
+        if (j0 + lane < keys) {
+            s = 0.f;
+            for (int c = 0; c < d; ++c) s = fmaf(ldf(q + c), ldf(k + (size_t)(j0 + lane) * ld + c), s);
+            s *= scale_log2;
+        }
+        const float nm = fmaxf(m, warp_max(s)), at = nm == -INFINITY ? 0.f : nm;
+        const float f = exp2f(m - at), p = exp2f(s - at);
+        l = fmaf(l, f, warp_sum(p));
+        m = nm;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[i] *= f;
+        for (int j = 0; j < min(32, keys - j0); ++j) {
+            const float pj = __shfl_sync(0xffffffffu, p, j);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (lane + 32 * i < d) acc[i] = fmaf(pj, ldf(v + (size_t)(j0 + j) * ld + lane + 32 * i), acc[i]);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (lane + 32 * i < d) stf(o + lane + 32 * i, keys > 0 ? acc[i] / l : 0.f);
+}
+
+template <int HD>
+__global__ void __launch_bounds__(NUM_THREADS, 1)
+attn_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
+                      int n_seq, int rows_q, int rows_k, int Hq, int Hkv, int d, float scale_log2, const int32_t *__restrict__ q_start,
+                      const int32_t *__restrict__ k_start, const __nv_bfloat16 *__restrict__ q, const __nv_bfloat16 *__restrict__ k,
+                      const __nv_bfloat16 *__restrict__ v, __nv_bfloat16 *__restrict__ out, int *status) {
+    typedef Smem<HD> SM;
+    constexpr int HALVES = HD / 64;
+    extern __shared__ __align__(1024) uint8_t smem[];
+    uint64_t *bars = (uint64_t *)(smem + SM::MISC);
+    uint32_t *tmem_slot = (uint32_t *)(bars + B_COUNT);
+    volatile int *abort_flag = (volatile int *)(tmem_slot + 1);       // [2]
+    volatile int *found = abort_flag + 2;                             // a hidden value that is not finite
+    PackedBlock *blk = (PackedBlock *)(tmem_slot + 4);
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int group = Hq / Hkv, TQ = BQ / group;                      // queries per tile
+    const int kv = blockIdx.x % Hkv;
+
+    if ((tc::smem_u32(smem) & 1023u) != 0) {
+        if (threadIdx.x == 0) atomicCAS(status, 0, STR_ERR_CUDA);
+        return;
+    }
+    if (tc::cta_should_leave(status)) return;     // an earlier CTA failed: the whole CTA leaves at once
+    if (blockIdx.x == 0) {
+        packed_check(q_start, n_seq, rows_q, status);
+        packed_check(k_start, n_seq, rows_k, status);
+    }
+    if (warp == 0) {
+        const PackedBlock b = packed_block(q_start, k_start, n_seq, rows_q, rows_k, 2 * TQ, BKV, blockIdx.x / Hkv);
+        if (lane == 0) *blk = b;
+    }
+    if (threadIdx.x == 32) {
+        tc::mbar_init(bars + B_Q, 1);
+        for (int s = 0; s < 2; ++s) {
+            tc::mbar_init(bars + B_KF + s, 1); tc::mbar_init(bars + B_KE + s, 1);
+            tc::mbar_init(bars + B_VF + s, 1); tc::mbar_init(bars + B_VR + s, 1); tc::mbar_init(bars + B_VE + s, 2);
+            tc::mbar_init(bars + B_SF + s, 1); tc::mbar_init(bars + B_PA + s, 4); tc::mbar_init(bars + B_PB + s, 4);
+            tc::mbar_init(bars + B_OF + s, 1);
+        }
+        abort_flag[0] = 0; abort_flag[1] = 0; found[0] = 0;
+        tc::fence_mbar_init();
+        tc::prefetch_tmap(&tmap_q); tc::prefetch_tmap(&tmap_k); tc::prefetch_tmap(&tmap_v);
+    }
+    __syncthreads();
+    const PackedBlock b = *blk;
+    if (b.n <= 0) return;                                             // more CTAs than blocks of queries
+    if (warp == 9) { tc::tmem_alloc(tmem_slot, 512); tc::tmem_relinquish(); }
+    tc::tc_fence_before();
+    __syncthreads();
+    tc::tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+
+    // Query number t of the block sees the keys 0 .. first_limit + t.
+    const int first_limit = b.lk - b.lq + b.first;
+    const int n0 = (max(first_limit + min(b.n, TQ), 0) + BKV - 1) / BKV;              // key tiles of row tile 0
+    const int n1 = b.n > TQ ? (max(first_limit + b.n, 0) + BKV - 1) / BKV : 0;        // of row tile 1; not fewer unless it is empty
+    const int nt = max(n0, n1);
+
+    if (warp == 8) {
+        // ------------------------------------------------------------------ TMA producer
+        if (lane == 0 && nt > 0) {
+            bool ok = true;
+            tc::mbar_arrive_expect_tx(bars + B_Q, (uint32_t)(2 * HALVES * TQ * group) * 128u);
+            for (int i = 0; i < 2; ++i)
+                for (int hf = 0; hf < HALVES; ++hf)
+                    tc::tma_load_3d(smem + SM::Q + i * SM::TILE + hf * TILE_16K, &tmap_q, bars + B_Q, hf * 64, kv * group, b.q0 + b.first + i * TQ);
+            int issued_k = 0, issued_v = 0;
+            for (int j = 0; j < nt; ++j) {
+                const int s = j & 1;
+                const uint32_t ph = ((j >> 1) & 1) ^ 1;
+                if (!tc::mbar_wait(bars + B_KE + s, ph, abort_flag)) { ok = false; break; }
+                tc::mbar_arrive_expect_tx(bars + B_KF + s, SM::TILE);
+                for (int hf = 0; hf < HALVES; ++hf)
+                    tc::tma_load_3d(smem + SM::K + s * SM::TILE + hf * TILE_16K, &tmap_k, bars + B_KF + s, hf * 64, kv, b.k0 + j * BKV);
+                ++issued_k;
+                if (!tc::mbar_wait(bars + B_VE + s, ph, abort_flag)) { ok = false; break; }
+                tc::mbar_arrive_expect_tx(bars + B_VF + s, SM::TILE);
+                for (int hf = 0; hf < HALVES; ++hf)
+                    tc::tma_load_3d(smem + SM::V + s * SM::TILE + hf * TILE_16K, &tmap_v, bars + B_VF + s, hf * 64, kv, b.k0 + j * BKV);
+                ++issued_v;
+            }
+            if (!ok) {
+                atomicCAS(status, 0, STR_ERR_TIMEOUT);
+                // let copies already issued land before the CTA's shared memory goes away
+                tc::mbar_wait(bars + B_Q, 0, abort_flag + 1);
+                for (int back = 1; back <= 2 && back <= issued_k; ++back) {
+                    const int j = issued_k - back;
+                    tc::mbar_wait(bars + B_KF + (j & 1), (j >> 1) & 1, abort_flag + 1);
+                }
+                for (int back = 1; back <= 2 && back <= issued_v; ++back) {
+                    const int j = issued_v - back;
+                    tc::mbar_wait(bars + B_VF + (j & 1), (j >> 1) & 1, abort_flag + 1);
+                }
+            }
+        }
+    } else if (warp == 9) {
+        // ------------------------------------------------------------------ MMA issuer (one elected thread for the whole loop, see tc_common.cuh)
+        if (tc::elect_one() && nt > 0) {
+            const uint32_t id_s = tc::make_idesc_bf16(BQ, BKV, 0, 0);     // Q (K-major) x K (K-major)
+            const uint32_t id_o = tc::make_idesc_bf16(BQ, HD, 0, 1);      // P (tensor memory) x V (MN-major)
+            const uint32_t sbase = tc::smem_u32(smem);
+            auto issue_s = [&](int i, int slot) {
+                const uint64_t qd = tc::desc_kmajor_sw128(sbase + SM::Q + (uint32_t)i * SM::TILE, 0);
+                const uint64_t kd = tc::desc_kmajor_sw128(sbase + SM::K + (uint32_t)slot * SM::TILE, 0);
+                if constexpr (HD == 128) tc::mma8_ss<tc::StepKMajor2x64, tc::StepKMajor2x64>(tmem + TM_S + (uint32_t)i * 128, qd, kd, id_s, false);
+                else tc::mma4_ss<tc::StepKMajor64, tc::StepKMajor64>(tmem + TM_S + (uint32_t)i * 128, qd, kd, id_s, false);
+                tc::mma_commit(bars + B_SF + i);
+            };
+            auto issue_pv = [&](int i, int slot, int half, bool first) {
+                const uint64_t vd = tc::make_smem_desc(sbase + SM::V + (uint32_t)slot * SM::TILE + (uint32_t)half * 8192u, TILE_16K, 1024, tc::SWZ_128B);
+                tc::mma4_ts<tc::StepTmem8, tc::StepMNMajor>(tmem + TM_O + (uint32_t)i * 128, tmem + TM_S + (uint32_t)i * 128 + (uint32_t)half * 32, vd, id_o, !first);
+            };
+            bool ok = tc::mbar_wait(bars + B_Q, 0, abort_flag) && tc::mbar_wait(bars + B_KF, 0, abort_flag);
+            if (ok) {
+                tc::tc_fence_after();
+                if (n0 > 0) issue_s(0, 0);
+                if (n1 > 0) issue_s(1, 0);
+                tc::mma_commit(bars + B_KE);
+            }
+            for (int j = 0; j < nt && ok; ++j) {
+                const int s = j & 1, ns = (j + 1) & 1;
+                if (!tc::mbar_wait(bars + B_VF + s, (j >> 1) & 1, abort_flag) || !tc::mbar_wait(bars + B_VR + s, (j >> 1) & 1, abort_flag)) { ok = false; break; }
+                if (j < n0) {
+                    if (!tc::mbar_wait(bars + B_PA, j & 1, abort_flag)) { ok = false; break; }
+                    tc::tc_fence_after();
+                    issue_pv(0, s, 0, j == 0);
+                    if (!tc::mbar_wait(bars + B_PB, j & 1, abort_flag)) { ok = false; break; }
+                    tc::tc_fence_after();
+                    issue_pv(0, s, 1, false);
+                    if (j == n0 - 1) tc::mma_commit(bars + B_OF);
+                }
+                if (j + 1 < nt) {
+                    if (!tc::mbar_wait(bars + B_KF + ns, ((j + 1) >> 1) & 1, abort_flag)) { ok = false; break; }
+                    tc::tc_fence_after();
+                    if (j + 1 < n0) issue_s(0, ns);
+                }
+                if (j < n1) {
+                    if (!tc::mbar_wait(bars + B_PA + 1, j & 1, abort_flag)) { ok = false; break; }
+                    tc::tc_fence_after();
+                    issue_pv(1, s, 0, j == 0);
+                    if (!tc::mbar_wait(bars + B_PB + 1, j & 1, abort_flag)) { ok = false; break; }
+                    tc::tc_fence_after();
+                    issue_pv(1, s, 1, false);
+                    if (j == n1 - 1) tc::mma_commit(bars + B_OF + 1);
+                }
+                tc::mma_commit(bars + B_VE + s);
+                if (j + 1 < nt) {
+                    if (j + 1 < n1) issue_s(1, ns);
+                    tc::mma_commit(bars + B_KE + ns);
+                }
+            }
+            if (!ok) atomicCAS(status, 0, STR_ERR_TIMEOUT);
+        }
+        __syncwarp();
+    } else if (warp == 10) {
+        // ------------------------------------------------------------------ guard over the tiles of V
+        bool ok = true;
+        for (int j = 0; j < nt; ++j) {
+            const int s = j & 1;
+            if (!tc::mbar_wait(bars + B_VF + s, (j >> 1) & 1, abort_flag)) { ok = false; break; }
+            uint8_t *tile = smem + SM::V + s * SM::TILE;
+            const int valid = min(b.lk - j * BKV, BKV);               // rows of the tile that are the sequence's
+            if (valid < BKV) {
+                for (int e = valid * 8 + lane; e < BKV * 8; e += 32)
+#pragma unroll
+                    for (int hf = 0; hf < HALVES; ++hf) *(uint4 *)(tile + hf * TILE_16K + e * 16) = make_uint4(0u, 0u, 0u, 0u);
+                tc::fence_proxy_async();
+                __syncwarp();
+            }
+            if (lane == 0) tc::mbar_arrive(bars + B_VR + s);
+            if (j * BKV + BKV - 1 > first_limit) {                    // hidden in part: zero times what is finite stays zero
+                const __nv_bfloat162 zero = __float2bfloat162_rn(0.f);
+                __nv_bfloat162 sum = zero;
+#pragma unroll 4
+                for (int e = lane; e < BKV * 8 * HALVES; e += 32) {
+                    const uint4 w = *(const uint4 *)(tile + e * 16);
+                    const __nv_bfloat162 *x = reinterpret_cast<const __nv_bfloat162 *>(&w);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) sum = __hfma2(x[i], zero, sum);
+                }
+                if (__low2float(sum) != 0.f || __high2float(sum) != 0.f) found[0] = 1;       // NaN
+                __syncwarp();
+            }
+            if (lane == 0) tc::mbar_arrive(bars + B_VE + s);
+        }
+        if (!ok && lane == 0) atomicCAS(status, 0, STR_ERR_TIMEOUT);
+    } else {
+        // ------------------------------------------------------------------ softmax warps
+        const int i = warp >> 2, quad = warp & 3;
+        const int row = quad * 32 + lane, t = i * TQ + row / group;   // row of the tile, query of the block
+        const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
+        const uint32_t tS = tmem + lane_base + TM_S + (uint32_t)i * 128;
+        const uint32_t tO = tmem + lane_base + TM_O + (uint32_t)i * 128;
+        const int ni = i == 0 ? n0 : n1;
+        const bool live = row < TQ * group && t < b.n;
+        const int limit = first_limit + min(t, b.n - 1);              // this row sees the keys 0 .. limit
+        const float2 scale2 = make_float2(scale_log2, scale_log2);
+        float m = -INFINITY, l = 0.f;
+        bool ok = true;
+        for (int j = 0; j < ni; ++j) {
+            if (!tc::mbar_wait(bars + B_SF + i, j & 1, abort_flag)) { ok = false; break; }
+            tc::tc_fence_after();
+            uint32_t w[4][32];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) tc::tmem_ld32(tS + c * 32, w[c]);
+            tc::tmem_ld_wait();
+            if (__any_sync(0xffffffffu, j * BKV + BKV - 1 > limit)) { // some row of this warp ends inside (or before) this tile
+                const int lim = limit - j * BKV;
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+#pragma unroll
+                    for (int e = 0; e < 32; ++e)
+                        if (c * 32 + e > lim) w[c][e] = 0xFF800000u;  // -infinity
+            }
+            float top[4] = {m, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+            for (int e = 0; e < 32; e += 2)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) top[c] = tc::max3(top[c], __uint_as_float(w[c][e]), __uint_as_float(w[c][e + 1]));
+            const float m_new = fmaxf(tc::max3(top[0], top[1], top[2]), top[3]);
+            // A row raises its maximum only when it has grown by more than the threshold: a decision of the row alone.  From minus infinity
+            // (nothing seen yet) any score is growth.
+            const bool grow = (m_new - m) * scale_log2 > RESCALE_THRESHOLD;
+            if (j == 0) {
+                m = m_new;
+            } else if (__any_sync(0xffffffffu, grow)) {
+                // S_j complete implies the previous P V product of this tile is complete: O is stable.  The whole warp
+                // runs the (warp-collective) accumulator update; rows that keep their maximum multiply by exactly 1.
+                const float f = grow ? tc::ex2((m - m_new) * scale_log2) : 1.0f;
+                if (grow) { l *= f; m = m_new; }
+#pragma unroll 1
+                for (int c = 0; c < HD / 32; ++c) {
+                    uint32_t o[32];
+                    tc::tmem_ld32(tO + c * 32, o);
+                    tc::tmem_ld_wait();
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                    tc::tmem_st32(tO + c * 32, o);
+                }
+                tc::tmem_st_wait();
+            }
+            const float mc = m == -INFINITY ? 0.f : m * scale_log2;
+            const float2 nmc2 = make_float2(-mc, -mc);
+            float2 sum = make_float2(0.f, 0.f);
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf) {
+                uint32_t pk[32];
+#pragma unroll
+                for (int e = 0; e < 32; ++e) {
+                    const int cc = 2 * hf + (e >> 4), ee = (2 * e) & 31;
+                    const float2 a = __ffma2_rn(make_float2(__uint_as_float(w[cc][ee]), __uint_as_float(w[cc][ee + 1])), scale2, nmc2);
+                    const float2 p = make_float2(tc::ex2(a.x), tc::ex2(a.y));
+                    sum = __fadd2_rn(sum, p);
+                    pk[e] = tc::pack_bf16x2(p.x, p.y);
+                }
+                tc::tmem_st32(tS + hf * 32, pk);
+                tc::tmem_st_wait();
+                tc::tc_fence_before();
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(bars + (hf == 0 ? B_PA : B_PB) + i);
+            }
+            l += sum.x + sum.y;
+        }
+        if (ok && ni > 0) ok = tc::mbar_wait(bars + B_OF + i, 0, abort_flag);
+        if (ok) {
+            tc::tc_fence_after();
+            const bool sees = limit >= 0;
+            const float inv = sees ? 1.0f / l : 0.f;
+            __nv_bfloat16 *dst = out + ((size_t)(b.q0 + b.first + t) * Hq + kv * group + row % group) * d;
+#pragma unroll 1
+            for (int c = 0; c < HD / 32; ++c) {
+                uint32_t o[32];
+                if (ni > 0) {
+                    tc::tmem_ld32(tO + c * 32, o);
+                    tc::tmem_ld_wait();
+                }
+                if (live) {
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        if (c * 32 + g * 8 >= d) break;
+                        uint32_t r[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            r[e] = sees ? tc::pack_bf16x2(__uint_as_float(o[8 * g + 2 * e]) * inv, __uint_as_float(o[8 * g + 2 * e + 1]) * inv) : 0u;
+                        *reinterpret_cast<uint4 *>(dst + c * 32 + g * 8) = make_uint4(r[0], r[1], r[2], r[3]);
+                    }
+                }
+            }
+        } else if (lane == 0) {
+            atomicCAS(status, 0, STR_ERR_TIMEOUT);
+        }
+    }
+    tc::tc_fence_before();
+    __syncthreads();
+    if (warp == 9) { tc::tc_fence_after(); tc::tmem_dealloc(tmem, 512); }
+    if (found[0] == 0) return;
+    for (int r = warp; r < b.n * group; r += NUM_WARPS) {
+        const int t = r / group;
+        const size_t at = ((size_t)(b.q0 + b.first + t) * Hq + kv * group + r % group) * d, keys = ((size_t)b.k0 * Hkv + kv) * d;
+        attn_row(q + at, k + keys, v + keys, out + at, (size_t)Hkv * d, max(first_limit + t + 1, 0), d, scale_log2);
+    }
+}
+
+template <int HD>
+int launch(str_ctx *ctx, const str_attn_packed_shape *s, const void *q, const void *k, const void *v, const int32_t *q_start, const int32_t *k_start,
+           float scale, void *o, cudaStream_t st) {
+    const int group = s->Hq / s->Hkv, TQ = BQ / group;
+    CUtensorMap tq, tk, tv;
+    int rc = str_make_tmap_heads_bf16_sw128(ctx, &tq, q, s->d, s->Hq, s->rows_q, group, TQ);
+    if (rc == STR_OK) rc = str_make_tmap_heads_bf16_sw128(ctx, &tk, k, s->d, s->Hkv, s->rows_k, 1, BKV);
+    if (rc == STR_OK) rc = str_make_tmap_heads_bf16_sw128(ctx, &tv, v, s->d, s->Hkv, s->rows_k, 1, BKV);
+    if (rc != STR_OK) return rc;
+    rc = str_ensure_smem(ctx, HD == 64 ? STR_SMEM_ATTN_PACKED_64 : STR_SMEM_ATTN_PACKED_128, attn_packed_tc_kernel<HD>, Smem<HD>::BYTES);
+    if (rc != STR_OK) return rc;
+    const int blocks = s->rows_q / (2 * TQ) + s->n_seq;               // at least as many as there are blocks of queries
+    attn_packed_tc_kernel<HD><<<blocks * s->Hkv, NUM_THREADS, Smem<HD>::BYTES, st>>>(
+        tq, tk, tv, s->n_seq, s->rows_q, s->rows_k, s->Hq, s->Hkv, s->d, scale * 1.4426950408889634f, q_start, k_start, (const __nv_bfloat16 *)q,
+        (const __nv_bfloat16 *)k, (const __nv_bfloat16 *)v, (__nv_bfloat16 *)o, ctx->status_dev);
+    return str_launch_ok(ctx);
+}
+
+}  // namespace
+
+bool str_attn_packed_tc_supported(const str_attn_packed_shape *s, const void *q, const void *k, const void *v, const void *o) {
+    if (s->dtype != STR_BF16 || s->d > 128 || s->d % 8 != 0 || s->rows_k == 0 || s->Hq / s->Hkv > BQ) return false;
+    return (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)o) & 15) == 0;
+}
+
+int str_attn_packed_tc(str_ctx *ctx, const str_attn_packed_shape *s, const void *q, const void *k, const void *v, const int32_t *q_start,
+                       const int32_t *k_start, float scale, void *o, cudaStream_t st) {
+    return s->d <= 64 ? launch<64>(ctx, s, q, k, v, q_start, k_start, scale, o, st) : launch<128>(ctx, s, q, k, v, q_start, k_start, scale, o, st);
+}

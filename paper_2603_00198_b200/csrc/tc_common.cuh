@@ -239,6 +239,19 @@ __device__ __forceinline__ void mma4_ss(uint32_t d_tmem, uint64_t a0, uint64_t b
           "n"(SA::at(1)), "n"(SB::at(1)), "n"(SA::at(2)), "n"(SB::at(2)), "n"(SA::at(3)), "n"(SB::at(3))
         : "memory");
 }
+// Four K-slices, A (bf16) in tensor memory, B in shared memory.
+template <class SA, class SB>
+__device__ __forceinline__ void mma4_ts(uint32_t d_tmem, uint32_t a_tmem0, uint64_t b0, uint32_t idesc, bool acc_first) {
+    asm volatile(
+        "{\n\t.reg .pred pf, pt;\n\t.reg .b64 b;\n\t.reg .b32 at;\n\t"
+        "setp.ne.b32 pf, %4, 0;\n\tsetp.eq.u32 pt, 0, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, pf;\n\t"
+        STR_MMA_TAIL_TS(1, 5, 6) STR_MMA_TAIL_TS(2, 7, 8) STR_MMA_TAIL_TS(3, 9, 10)
+        "}"
+        ::"r"(d_tmem), "r"(a_tmem0), "l"(b0), "r"(idesc), "r"((uint32_t)acc_first),
+          "n"(SA::at(1)), "n"(SB::at(1)), "n"(SA::at(2)), "n"(SB::at(2)), "n"(SA::at(3)), "n"(SB::at(3))
+        : "memory");
+}
 #undef STR_MMA_TAIL_SS
 #undef STR_MMA_TAIL_TS
 
@@ -388,6 +401,12 @@ __device__ __forceinline__ float ex2(float x) {
     return y;
 }
 
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+
 // log2(x) on the special-function unit (log2(0) = -inf).
 __device__ __forceinline__ float lg2(float x) {
     float y;
@@ -433,6 +452,25 @@ static inline int str_make_tmap_3d_bf16_sw128(str_ctx *ctx, CUtensorMap *map, co
     cuuint64_t dims[3] = {inner, rows, outer};
     cuuint64_t strides[2] = {inner * 2, inner * rows * 2};
     cuuint32_t box[3] = {64, box_rows, 1};
+    cuuint32_t estr[3] = {1, 1, 1};
+    CUresult r = ((encode_fn)ctx->encode_tiled)(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(base), dims,
+                                                strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                                                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                                                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? STR_OK : STR_ERR_CUDA;
+}
+
+// bf16 tensor [rows][heads][d] (contiguous), box [box_rows][box_heads][64] with 128-byte swizzle.  Columns beyond d read as zero, so heads whose size
+// is not a multiple of 64 are padded on the way.
+static inline int str_make_tmap_heads_bf16_sw128(str_ctx *ctx, CUtensorMap *map, const void *base, uint64_t d, uint64_t heads, uint64_t rows,
+                                                 uint32_t box_heads, uint32_t box_rows) {
+    typedef CUresult (*encode_fn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
+                                  const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+    if (!ctx->encode_tiled) return STR_ERR_CUDA;
+    cuuint64_t dims[3] = {d, heads, rows};
+    cuuint64_t strides[2] = {d * 2, d * heads * 2};
+    cuuint32_t box[3] = {64, box_heads, box_rows};
     cuuint32_t estr[3] = {1, 1, 1};
     CUresult r = ((encode_fn)ctx->encode_tiled)(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(base), dims,
                                                 strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
