@@ -132,6 +132,8 @@ extern "C" int str_mamba2_prefill_packed(str_ctx *ctx, const str_ssd_packed_shap
     if (!dev.ok) return STR_ERR_CUDA;
     StrProfScope prof_scope(ctx, STR_CAT_SSD, stream);
     cudaStream_t st = (cudaStream_t)stream;
+    if (!str_force_simt() && str_scan_packed_tc_supported(s, x, B, C, y))
+        return ++ctx->tc_calls, str_scan_packed_tc(ctx, s, x, dt, A, B, C, D, seq_start, init_state, y, final_state, st);
     ++ctx->fallback_calls;
     if (s->dtype == STR_BF16) return dispatch<__nv_bfloat16>(ctx, s, x, dt, A, B, C, D, seq_start, init_state, y, final_state, st);
     return dispatch<float>(ctx, s, x, dt, A, B, C, D, seq_start, init_state, y, final_state, st);
