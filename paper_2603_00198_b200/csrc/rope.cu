@@ -54,7 +54,7 @@ rope_split_ex_kernel(const __grid_constant__ RopeTable tab, int rows, int Hq, in
     __syncthreads();
     const int turned = HALF ? pairs / VEC : rot / VEC, per_head = turned + (d - rot) / VEC;
     const int heads = (Hq + Hkv) * per_head, units = heads + Hkv * d / VEC;
-    for (int e = threadIdx.x; e < units; e += THREADS) {
+    for (int e = threadIdx.x; e < units; e += blockDim.x) {
         int head = 0, u = turned, at;                     // at: column of the unit's (first) vector
         T *dst;
         int width;                                        // elements of a row of dst
