@@ -1,8 +1,9 @@
 // str_attn_prefill_packed: causal attention with grouped heads over packed sequences; query i of a sequence with lq queries and lk keys
 // sees its keys 0 .. lk - lq + i.  The entry point, and the kernel in fp32 arithmetic: every type, head sizes up to 128.
 //
-// One pass over the keys with the running maximum and sum of the softmax.  The 128 rows of a block are (query, head) pairs: the queries of a
-// key head's group lie in one block, so that its keys and values are fetched once for all of them.
+// One pass over the keys with the running maximum and sum of the softmax.  The BR rows of a block are (query, head) pairs: the queries of a
+// key head's group lie in one block, so that its keys and values are fetched once for all of them.  Bound by fp32 arithmetic: both products
+// are formed two elements an instruction, from 16-byte pieces of shared memory.
 #include <math.h>
 
 #include "dispatch.cuh"
@@ -10,15 +11,27 @@
 
 namespace {
 
-constexpr int BR = 128, BC = 64, THREADS = 256, LDP = BC + 4;
+constexpr int MAX_ROWS = 128, BC = 64, LDP = BC + 4;
 
-// DP: head size padded to 64 or 128.  Thread (ty, tx) of 16 x 16: rows ty + 16 a (a < 8), keys tx + 16 j (j < 4), columns 4 tx + 64 c ...
-template <typename T, int DP>
-__global__ void __launch_bounds__(THREADS)
+// Four columns of a row, the first `in` of which exist.
+__device__ __forceinline__ float4 raw4(const float *p) { return __ldg((const float4 *)p); }
+__device__ __forceinline__ float4 raw4(const __nv_bfloat16 *p) {
+    const uint2 w = __ldg((const uint2 *)p);
+    return make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xFFFF0000u), __uint_as_float(w.y << 16), __uint_as_float(w.y & 0xFFFF0000u));
+}
+template <typename T>
+__device__ __forceinline__ float4 load4(const T *p, int in, bool vec) {
+    if (vec && in >= 4) return raw4(p);
+    return make_float4(in > 0 ? ldf(p) : 0.f, in > 1 ? ldf(p + 1) : 0.f, in > 2 ? ldf(p + 2) : 0.f, in > 3 ? ldf(p + 3) : 0.f);
+}
+
+// DP: head size padded to 64 or 128.  Thread (ty, tx) of BR/8 x 16: rows ty + BR/8 a (a < 8), keys tx + 16 j (j < 4), columns 4 tx + 64 c ...
+template <typename T, int DP, int BR>
+__global__ void __launch_bounds__(2 * BR)
 attn_packed_simt_kernel(int n_seq, int rows_q, int rows_k, int Hq, int Hkv, int d, float scale_log2, const int32_t *__restrict__ q_start,
                         const int32_t *__restrict__ k_start, const T *__restrict__ q, const T *__restrict__ k, const T *__restrict__ v, T *__restrict__ o,
                         int *status) {
-    constexpr int LD = DP + 4, DC = DP / 64;
+    constexpr int LD = DP + 4, DC = DP / 64, THREADS = 2 * BR, RS = BR / 8;
     extern __shared__ float4 smem4[];
     float *Qs = (float *)smem4, *Ks = Qs + BR * LD, *Vs = Ks + BC * LD, *Ps = Vs + BC * DP;
     __shared__ PackedBlock blk;
@@ -37,36 +50,44 @@ attn_packed_simt_kernel(int n_seq, int rows_q, int rows_k, int Hq, int Hkv, int 
     if (b.n <= 0) return;
     const int first_limit = b.lk - b.lq + b.first;                       // last key that the block's first query sees
     const int seen = max(first_limit + b.n, 0);                          // keys that its last query sees
-    for (int e = tid; e < BR * DP; e += THREADS) {
-        const int r = e / DP, c = e % DP, t = r / group;
-        Qs[r * LD + c] = t < b.n && c < d ? ldf(q + ((size_t)(b.q0 + b.first + t) * Hq + kv * group + r % group) * d + c) : 0.f;
+    // Rows whose columns come in fours are read so.
+    const bool vec = d % 4 == 0 && (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v) & 15) == 0;
+    for (int e = tid; e < BR * (DP / 4); e += THREADS) {
+        const int r = e / (DP / 4), c = e % (DP / 4) * 4, t = r / group;
+        *(float4 *)(Qs + r * LD + c) = load4(q + ((size_t)(b.q0 + b.first + t) * Hq + kv * group + r % group) * d + c, t < b.n ? d - c : 0, vec);
     }
     int limit[8];
-    float mx[8], sm[8], acc[8][DC * 4];
+    float mx[8], sm[8];
+    float2 acc[8][DC * 2];
 #pragma unroll
     for (int a = 0; a < 8; ++a) {
-        limit[a] = first_limit + min((ty + 16 * a) / group, b.n - 1);
+        limit[a] = first_limit + min((ty + RS * a) / group, b.n - 1);
         mx[a] = -INFINITY;
         sm[a] = 0.f;
 #pragma unroll
-        for (int c = 0; c < DC * 4; ++c) acc[a][c] = 0.f;
+        for (int c = 0; c < DC * 2; ++c) acc[a][c] = make_float2(0.f, 0.f);
     }
     for (int c0 = 0; c0 < seen; c0 += BC) {
         __syncthreads();
         bool odd = false;                                                // a value that is not finite
-        for (int e = tid; e < BC * DP; e += THREADS) {
-            const int r = e / DP, c = e % DP;
+#pragma unroll 4
+        for (int e = tid; e < BC * (DP / 4); e += THREADS) {
+            const int r = e / (DP / 4), c = e % (DP / 4) * 4;
             const size_t at = ((size_t)(b.k0 + c0 + r) * Hkv + kv) * d + c;
-            const bool in = c0 + r < seen && c < d;
-            const float vv = in ? ldf(v + at) : 0.f;
-            Ks[r * LD + c] = in ? ldf(k + at) : 0.f;
-            Vs[r * DP + c] = vv;
-            odd |= !isfinite(vv);
+            const int in = c0 + r < seen ? d - c : 0;                    // columns from c on
+            const float4 kk = load4(k + at, in, vec), vv = load4(v + at, in, vec);
+            *(float4 *)(Ks + r * LD + c) = kk;
+            *(float4 *)(Vs + r * DP + c) = vv;
+            odd |= !(isfinite(vv.x) && isfinite(vv.y) && isfinite(vv.z) && isfinite(vv.w));
         }
         // Weights of hidden keys are zero, and zero times a value that is not finite is not: a tile that some rows see in part only, with such a
         // value in it, takes the sum that leaves hidden keys out.
         const bool careful = __syncthreads_or(odd && c0 + BC - 1 > first_limit);
-        float s[8][4] = {};
+        float2 s2[8][4];                                                 // even and odd columns' sums
+#pragma unroll
+        for (int a = 0; a < 8; ++a)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s2[a][j] = make_float2(0.f, 0.f);
 #pragma unroll 2
         for (int c = 0; c < DP; c += 4) {
             float4 kk[4];
@@ -74,16 +95,19 @@ attn_packed_simt_kernel(int n_seq, int rows_q, int rows_k, int Hq, int Hkv, int 
             for (int j = 0; j < 4; ++j) kk[j] = *(const float4 *)(Ks + (tx + 16 * j) * LD + c);
 #pragma unroll
             for (int a = 0; a < 8; ++a) {
-                const float4 qq = *(const float4 *)(Qs + (ty + 16 * a) * LD + c);
+                const float4 qq = *(const float4 *)(Qs + (ty + RS * a) * LD + c);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    s[a][j] = fmaf(qq.x, kk[j].x, s[a][j]);
-                    s[a][j] = fmaf(qq.y, kk[j].y, s[a][j]);
-                    s[a][j] = fmaf(qq.z, kk[j].z, s[a][j]);
-                    s[a][j] = fmaf(qq.w, kk[j].w, s[a][j]);
+                    s2[a][j] = __ffma2_rn(make_float2(qq.x, qq.y), make_float2(kk[j].x, kk[j].y), s2[a][j]);
+                    s2[a][j] = __ffma2_rn(make_float2(qq.z, qq.w), make_float2(kk[j].z, kk[j].w), s2[a][j]);
                 }
             }
         }
+        float s[8][4];
+#pragma unroll
+        for (int a = 0; a < 8; ++a)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s[a][j] = s2[a][j].x + s2[a][j].y;
 #pragma unroll
         for (int a = 0; a < 8; ++a) {
             float top = -INFINITY;
@@ -100,7 +124,7 @@ attn_packed_simt_kernel(int n_seq, int rows_q, int rows_k, int Hq, int Hkv, int 
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const float p = exp2f(s[a][j] - at);
-                Ps[(ty + 16 * a) * LDP + tx + 16 * j] = p;
+                Ps[(ty + RS * a) * LDP + tx + 16 * j] = p;
                 sum += p;
             }
 #pragma unroll
@@ -108,7 +132,7 @@ attn_packed_simt_kernel(int n_seq, int rows_q, int rows_k, int Hq, int Hkv, int 
             sm[a] = fmaf(sm[a], f, sum);
             mx[a] = nm;
 #pragma unroll
-            for (int c = 0; c < DC * 4; ++c) acc[a][c] *= f;
+            for (int c = 0; c < DC * 2; ++c) acc[a][c] = __fmul2_rn(acc[a][c], make_float2(f, f));
         }
         __syncwarp();                                                    // a row's weights are written and read by the same half warp
         if (!careful) {
@@ -121,16 +145,14 @@ attn_packed_simt_kernel(int n_seq, int rows_q, int rows_k, int Hq, int Hkv, int 
                     for (int c = 0; c < DC; ++c) vv[i][c] = *(const float4 *)(Vs + (j + i) * DP + 4 * tx + 64 * c);
 #pragma unroll
                 for (int a = 0; a < 8; ++a) {
-                    const float4 p4 = *(const float4 *)(Ps + (ty + 16 * a) * LDP + j);
+                    const float4 p4 = *(const float4 *)(Ps + (ty + RS * a) * LDP + j);
                     const float p[4] = {p4.x, p4.y, p4.z, p4.w};
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
 #pragma unroll
                         for (int c = 0; c < DC; ++c) {
-                            acc[a][4 * c] = fmaf(p[i], vv[i][c].x, acc[a][4 * c]);
-                            acc[a][4 * c + 1] = fmaf(p[i], vv[i][c].y, acc[a][4 * c + 1]);
-                            acc[a][4 * c + 2] = fmaf(p[i], vv[i][c].z, acc[a][4 * c + 2]);
-                            acc[a][4 * c + 3] = fmaf(p[i], vv[i][c].w, acc[a][4 * c + 3]);
+                            acc[a][2 * c] = __ffma2_rn(make_float2(p[i], p[i]), make_float2(vv[i][c].x, vv[i][c].y), acc[a][2 * c]);
+                            acc[a][2 * c + 1] = __ffma2_rn(make_float2(p[i], p[i]), make_float2(vv[i][c].z, vv[i][c].w), acc[a][2 * c + 1]);
                         }
                 }
             }
@@ -140,36 +162,49 @@ attn_packed_simt_kernel(int n_seq, int rows_q, int rows_k, int Hq, int Hkv, int 
 #pragma unroll
                 for (int a = 0; a < 8; ++a)
                     if (c0 + j <= limit[a]) {
-                        const float p = Ps[(ty + 16 * a) * LDP + j];
+                        const float p = Ps[(ty + RS * a) * LDP + j];
 #pragma unroll
-                        for (int c = 0; c < DC * 4; ++c) acc[a][c] = fmaf(p, Vs[j * DP + 4 * tx + 64 * (c / 4) + c % 4], acc[a][c]);
+                        for (int c = 0; c < DC * 2; ++c) {
+                            const float *vv = Vs + j * DP + 4 * tx + 64 * (c / 2) + 2 * (c % 2);
+                            acc[a][c] = __ffma2_rn(make_float2(p, p), make_float2(vv[0], vv[1]), acc[a][c]);
+                        }
                     }
         }
     }
 #pragma unroll
     for (int a = 0; a < 8; ++a) {
-        const int r = ty + 16 * a, t = r / group;
+        const int r = ty + RS * a, t = r / group;
         if (t >= b.n) continue;
         const float inv = limit[a] >= 0 ? 1.0f / sm[a] : 0.f;
         T *dst = o + ((size_t)(b.q0 + b.first + t) * Hq + kv * group + r % group) * d;
 #pragma unroll
         for (int c = 0; c < DC * 4; ++c) {
             const int col = 4 * tx + 64 * (c / 4) + c % 4;
-            if (col < d) stf(dst + col, limit[a] >= 0 ? acc[a][c] * inv : 0.f);
+            if (col < d) stf(dst + col, limit[a] >= 0 ? (c % 2 ? acc[a][c / 2].y : acc[a][c / 2].x) * inv : 0.f);
         }
     }
 }
 
-template <typename T, int DP>
+template <typename T, int DP, int BR>
 int launch(str_ctx *ctx, const str_attn_packed_shape *s, const void *q, const void *k, const void *v, const int32_t *q_start, const int32_t *k_start,
            float scale, void *o, cudaStream_t st) {
     constexpr size_t smem = sizeof(float) * ((size_t)(BR + BC) * (DP + 4) + BC * DP + BR * LDP);
-    STR_CUDA_OK(cudaFuncSetAttribute(attn_packed_simt_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    STR_CUDA_OK(cudaFuncSetAttribute(attn_packed_simt_kernel<T, DP, BR>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     const int per = BR / (s->Hq / s->Hkv);
-    attn_packed_simt_kernel<T, DP><<<(s->rows_q / per + s->n_seq) * s->Hkv, THREADS, smem, st>>>(
+    attn_packed_simt_kernel<T, DP, BR><<<(s->rows_q / per + s->n_seq) * s->Hkv, 2 * BR, smem, st>>>(
         s->n_seq, s->rows_q, s->rows_k, s->Hq, s->Hkv, s->d, scale * 1.4426950408889634f, q_start, k_start, (const T *)q, (const T *)k, (const T *)v,
         (T *)o, ctx->status_dev);
     return str_launch_ok(ctx);
+}
+
+// Small heads: blocks of 64 rows, three of which fit an SM; blocks of 128 where a group needs them or the head is wide (one block fits, and has to
+// bring its warps along).
+template <typename T>
+int dispatch(str_ctx *ctx, const str_attn_packed_shape *s, const void *q, const void *k, const void *v, const int32_t *q_start, const int32_t *k_start,
+             float scale, void *o, cudaStream_t st) {
+    if (s->d > 64) return launch<T, 128, 128>(ctx, s, q, k, v, q_start, k_start, scale, o, st);
+    if (s->Hq / s->Hkv > 64) return launch<T, 64, 128>(ctx, s, q, k, v, q_start, k_start, scale, o, st);
+    return launch<T, 64, 64>(ctx, s, q, k, v, q_start, k_start, scale, o, st);
 }
 
 }  // namespace
@@ -190,8 +225,8 @@ extern "C" int str_attn_prefill_packed(str_ctx *ctx, const str_attn_packed_shape
     if (s->rows_q == 0) return STR_OK;
     if (!q || !o || (s->rows_k > 0 && (!k || !v))) return STR_ERR_INVALID_ARG;
     const int group = s->Hq / s->Hkv;
-    if (s->d > 128 || group > BR || s->n_seq > 32768 || s->rows_q > (1 << 30) || s->rows_k > (1 << 30) ||
-        ((long long)s->rows_q / (BR / group) + s->n_seq) * s->Hkv > INT32_MAX)
+    if (s->d > 128 || group > MAX_ROWS || s->n_seq > 32768 || s->rows_q > (1 << 30) || s->rows_k > (1 << 30) ||
+        ((long long)s->rows_q * group + s->n_seq) * s->Hkv > INT32_MAX)
         return STR_ERR_UNSUPPORTED_SHAPE;
     const size_t es = dtype_size(s->dtype), qb = es * s->rows_q * s->Hq * s->d, kb = es * s->rows_k * s->Hkv * s->d;
     if (kv4_overlap(q, qb, o, qb) || kv4_overlap(k, kb, o, qb) || kv4_overlap(v, kb, o, qb)) return STR_ERR_INVALID_ARG;
@@ -203,9 +238,6 @@ extern "C" int str_attn_prefill_packed(str_ctx *ctx, const str_attn_packed_shape
     if (!str_force_simt() && str_attn_packed_tc_supported(s, q, k, v, o))
         return ++ctx->tc_calls, str_attn_packed_tc(ctx, s, q, k, v, q_start, k_start, softmax_scale, o, st);
     ++ctx->fallback_calls;
-    if (s->dtype == STR_BF16)
-        return s->d <= 64 ? launch<__nv_bfloat16, 64>(ctx, s, q, k, v, q_start, k_start, softmax_scale, o, st)
-                          : launch<__nv_bfloat16, 128>(ctx, s, q, k, v, q_start, k_start, softmax_scale, o, st);
-    return s->d <= 64 ? launch<float, 64>(ctx, s, q, k, v, q_start, k_start, softmax_scale, o, st)
-                      : launch<float, 128>(ctx, s, q, k, v, q_start, k_start, softmax_scale, o, st);
+    return s->dtype == STR_BF16 ? dispatch<__nv_bfloat16>(ctx, s, q, k, v, q_start, k_start, softmax_scale, o, st)
+                                : dispatch<float>(ctx, s, q, k, v, q_start, k_start, softmax_scale, o, st);
 }

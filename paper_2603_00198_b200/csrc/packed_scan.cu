@@ -3,15 +3,16 @@
 // The entry point, and the kernel that runs the recurrence token by token in fp32: every type and shape.
 //
 // A row of the state (one of p) lies across four lanes, NV vectors of four columns each; a block holds the rows of one head of one
-// sequence in registers from the first token to the last.  Tokens come through shared memory TB at a time.  Per token and head that is
-// p n (one multiplication and two fused ones): as many operations as the chunked form in fp32 needs, without its two roundings more, and a
-// state that never leaves the registers.
+// sequence in registers from the first token to the last.  Tokens come through shared memory TB at a time; the next ones are already on their way to
+// registers.  A lane leaves its part of y in shared memory, and the four parts are added when the tokens' outputs are written: no shuffles between
+// tokens, whose chain is then one fused operation a token.  Per token and head that is p n (one multiplication and two fused ones): as many
+// operations as the chunked form in fp32 needs, without its two roundings more, and a state that never leaves the registers.
 #include "dispatch.cuh"
 #include "packed.cuh"
 
 namespace {
 
-constexpr int LPR = 4, TB = 32, MAX_THREADS = 256;        // lanes per row, tokens per turn
+constexpr int LPR = 4, TB = 16, MAX_THREADS = 256;        // lanes per row, tokens per turn
 
 template <typename T, int NV>
 __global__ void __launch_bounds__(MAX_THREADS)
@@ -21,45 +22,78 @@ scan_packed_kernel(int n_seq, int rows, int H, int p, int n, int G, const T *__r
     constexpr int NP = NV * 4 * LPR;                      // columns, padded
     extern __shared__ float4 smem4[];
     float *bs = (float *)smem4, *cs = bs + TB * NP, *xs = cs + TB * NP;
-    const int R = blockDim.x / LPR;                       // rows of the state per block
-    float *ys = xs + TB * R, *dts = ys + TB * R, *decay = dts + TB;
+    const int threads = blockDim.x, R = threads / LPR;    // rows of the state per block
+    float *ys = xs + TB * R, *dts = ys + TB * R * LPR, *decay = dts + TB;
     const int h = blockIdx.y, s = blockIdx.z, g = h / (H / G);
-    const int i0 = blockIdx.x * R, r = threadIdx.x / LPR, l = threadIdx.x % LPR;
+    const int tid = threadIdx.x, i0 = blockIdx.x * R, r = tid / LPR, l = tid % LPR;
     if (blockIdx.x == 0 && h == 0 && s == 0) packed_check(start, n_seq, rows, status);
     const int t0 = packed_start(start, s, rows), t1 = packed_start(start, s + 1, rows);
     if (t1 <= t0 && (!final_state || (state == final_state))) return;
     const size_t base = (((size_t)s * H + h) * p + i0 + r) * n;
-    float S[NV][4];
+    // Four columns at a time where a row has whole vectors of them.
+    const bool vec = n % 4 == 0 && (((uintptr_t)state | (uintptr_t)final_state) & 15) == 0;
+    alignas(16) float S[NV][4];
 #pragma unroll
-    for (int v = 0; v < NV; ++v)
+    for (int v = 0; v < NV; ++v) {
+        const int col = (v * LPR + l) * 4;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int col = (v * LPR + l) * 4 + i;
-            S[v][i] = state && i0 + r < p && col < n ? state[base + col] : 0.f;
+        for (int i = 0; i < 4; ++i) S[v][i] = 0.f;
+        if (state && i0 + r < p && col < n) {
+            if (vec) *(float4 *)S[v] = *(const float4 *)(state + base + col);
+            else
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (col + i < n) S[v][i] = state[base + col + i];
         }
+    }
     const float Ah = A[h], Dh = Dskip ? Dskip[h] : 0.f;
+    // What the thread carries of the next TB tokens: element e = tid + k threads of [TB][NP] and of [TB][R].  A block has at least 2 NP threads' worth of rows
+    // or takes more elements a thread: at most BC of b and c, and TB / LPR of x.
+    constexpr int BC = TB * NP / 32 < 16 ? TB * NP / 32 : 16;
+    T bq[BC], cq[BC], xq[TB / LPR];
+    float dq = 0.f;
+    const int per = (TB * NP + threads - 1) / threads;
+    auto fetch = [&](int tb) {
+        const int m = min(TB, t1 - tb);
+#pragma unroll
+        for (int k = 0; k < BC; ++k) {
+            const int e = tid + k * threads, t = e / NP, col = e % NP;
+            stf(&bq[k], 0.f);
+            stf(&cq[k], 0.f);
+            if (k < per && t < m && col < n) {
+                const size_t at = ((size_t)(tb + t) * G + g) * n + col;
+                bq[k] = B[at];
+                cq[k] = C[at];
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < TB / LPR; ++k) {
+            const int e = tid + k * threads, t = e / R, i = e % R;
+            stf(&xq[k], 0.f);
+            if (t < m && i0 + i < p) xq[k] = x[((size_t)(tb + t) * H + h) * p + i0 + i];
+        }
+        if (tid < m) dq = dt[(size_t)(tb + tid) * H + h];
+    };
+    if (t0 < t1) fetch(t0);
     for (int tb = t0; tb < t1; tb += TB) {
         const int m = min(TB, t1 - tb);
-        __syncthreads();
-        for (int e = threadIdx.x; e < m * NP; e += blockDim.x) {
-            const int t = e / NP, col = e % NP;
-            const size_t at = ((size_t)(tb + t) * G + g) * n + col;
-            bs[e] = col < n ? ldf(B + at) : 0.f;
-            cs[e] = col < n ? ldf(C + at) : 0.f;
-        }
-        for (int e = threadIdx.x; e < m * R; e += blockDim.x) {
-            const int t = e / R, i = e % R;
-            xs[e] = i0 + i < p ? ldf(x + ((size_t)(tb + t) * H + h) * p + i0 + i) : 0.f;
-        }
-        if (threadIdx.x < m) {
-            const float d = dt[(size_t)(tb + threadIdx.x) * H + h];
-            dts[threadIdx.x] = d;
-            decay[threadIdx.x] = expf(d * Ah);
+#pragma unroll
+        for (int k = 0; k < BC; ++k)
+            if (k < per && tid + k * threads < TB * NP) {
+                bs[tid + k * threads] = ldf(&bq[k]);
+                cs[tid + k * threads] = ldf(&cq[k]);
+            }
+#pragma unroll
+        for (int k = 0; k < TB / LPR; ++k) xs[tid + k * threads] = ldf(&xq[k]);
+        if (tid < m) {
+            dts[tid] = dq;
+            decay[tid] = expf(dq * Ah);
         }
         __syncthreads();
-#pragma unroll 2
+        if (tb + TB < t1) fetch(tb + TB);
+#pragma unroll (NV >= 8 ? 2 : 4)
         for (int t = 0; t < m; ++t) {
-            const float xv = xs[t * R + r], dx = dts[t] * xv, a = decay[t];
+            const float dx = dts[t] * xs[t * R + r], a = decay[t];
             float acc[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
@@ -69,32 +103,36 @@ scan_packed_kernel(int n_seq, int rows, int H, int p, int n, int G, const T *__r
                 S[v][2] = fmaf(a, S[v][2], dx * b.z); acc[2] = fmaf(S[v][2], c.z, acc[2]);
                 S[v][3] = fmaf(a, S[v][3], dx * b.w); acc[3] = fmaf(S[v][3], c.w, acc[3]);
             }
-            float sum = (acc[0] + acc[1]) + (acc[2] + acc[3]);
-#pragma unroll
-            for (int o = 1; o < LPR; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-            if (l == 0) ys[t * R + r] = fmaf(Dh, xv, sum);
+            ys[t * threads + tid] = (acc[0] + acc[1]) + (acc[2] + acc[3]);
         }
         __syncthreads();
-        for (int e = threadIdx.x; e < m * R; e += blockDim.x) {
+        for (int e = tid; e < m * R; e += threads) {
             const int t = e / R, i = e % R;
-            if (i0 + i < p) stf(y + ((size_t)(tb + t) * H + h) * p + i0 + i, ys[e]);
+            const float4 part = *(const float4 *)(ys + e * LPR);
+            if (i0 + i < p) stf(y + ((size_t)(tb + t) * H + h) * p + i0 + i, fmaf(Dh, xs[e], (part.x + part.y) + (part.z + part.w)));
         }
+        __syncthreads();
     }
-    if (!final_state) return;
+    if (!final_state || i0 + r >= p) return;
 #pragma unroll
-    for (int v = 0; v < NV; ++v)
+    for (int v = 0; v < NV; ++v) {
+        const int col = (v * LPR + l) * 4;
+        if (vec && col < n) *(float4 *)(final_state + base + col) = *(const float4 *)S[v];
+        if (!vec)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int col = (v * LPR + l) * 4 + i;
-            if (i0 + r < p && col < n) final_state[base + col] = S[v][i];
-        }
+            for (int i = 0; i < 4; ++i)
+                if (col + i < n) final_state[base + col + i] = S[v][i];
+    }
 }
 
 template <typename T, int NV>
 int launch(str_ctx *ctx, const str_ssd_packed_shape *s, const void *x, const float *dt, const float *A, const void *B, const void *C, const float *D,
            const int32_t *start, const float *state, void *y, float *final_state, cudaStream_t st) {
-    const int warps = s->p >= 64 ? 8 : (s->p * LPR + 31) / 32, threads = 32 * warps, R = threads / LPR;
-    const size_t smem = sizeof(float) * ((size_t)TB * (2 * NV * 4 * LPR + 2 * R) + 2 * TB);
+    // As many warps as the head has rows for, and enough that a thread carries no more than sixteen elements of b and c.
+    int warps = s->p >= 64 ? 8 : (s->p * LPR + 31) / 32;
+    if (warps < NV / 2) warps = NV / 2;
+    const int threads = 32 * warps, R = threads / LPR;
+    const size_t smem = sizeof(float) * ((size_t)TB * (2 * NV * 4 * LPR + R + R * LPR) + 2 * TB);
     if (smem > 48 * 1024) STR_CUDA_OK(cudaFuncSetAttribute(scan_packed_kernel<T, NV>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     scan_packed_kernel<T, NV><<<dim3(ceil_div(s->p, R), s->H, s->n_seq), threads, smem, st>>>(
         s->n_seq, s->rows, s->H, s->p, s->n, s->G, (const T *)x, dt, A, (const T *)B, (const T *)C, D, start, state, (T *)y, final_state, ctx->status_dev);
