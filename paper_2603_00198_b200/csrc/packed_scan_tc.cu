@@ -12,8 +12,10 @@
 //               chunk after next is loaded there.
 //   not finite  W is zero above the diagonal, and zero times infinity or NaN is NaN: an x that is not finite would reach the up to 127 tokens
 //               before it.  The warps that form Xs look for one; a CTA that found one runs its sequence anew token by token (scan_rows).
-// Warp roles: 0-3, 14, 15 W; 4-7 state (lane 0 of 4: TMA producer); 8-11 Xs, Xs' and epilogue; 12 decay vectors; 13 MMA issuer; iteration c
-// issues CB_c, Y_intra_{c-1}, Y_inter_c, dS_c, dS'_c.
+// Warp roles: 0-3, 14, 15 W; 4-7 Xs, Xs' and the state; 8-11 epilogue; 12 decay vectors and TMA producer; 13 MMA issuer; iteration c
+// issues CB_c, Y_intra_{c-1}, Y_inter_c, then dS_c and dS'_c in halves of 64 tokens, as soon as these are there.  The chain from chunk to chunk is
+// dS -> state (and its copy) -> Xs -> dS; the state warps, who wait for dS anyhow, form Xs, so that no other role's work lies on it (formed by
+// the epilogue's warps, in front of each epilogue, it took 4400 clocks a chunk).
 // All mbarrier waits are bounded; a give-up records STR_ERR_TIMEOUT and tears the CTA down.
 #include "dispatch.cuh"
 #include "packed.cuh"
@@ -34,8 +36,8 @@ constexpr int OFF_BARS = OFF_DEC + DEC_DEPTH * DEC_FLOATS * 4;
 // decay vectors of one chunk (floats): log2-domain cumulative decay l_j, log2(dt_j) - l_j, column / state / row factors
 constexpr int D_LS = 0, D_NLC = 128, D_COLF = 256, D_XW = 384, D_ROWF = 512, D_EROW = 640, D_BLK = 768, D_EEND = 784;
 enum {
-    B_XF = 0, B_BCF = 3, B_DECF = 5, B_DECE = 9, B_CBF = 13, B_WF = 15, B_XSF = 17, B_DSF, B_DSE,
-    B_SF, B_YF, B_YE, B_XLF, B_COUNT
+    B_XF = 0, B_BCF = 3, B_DECF = 5, B_DECE = 9, B_CBF = 13, B_WF = 15, B_XSF = 17, B_DSF = 19, B_DSE = 21,
+    B_SF, B_YF, B_YE, B_COUNT
 };
 constexpr size_t SMEM_BYTES = (size_t)OFF_BARS + B_COUNT * 8 + 32;
 constexpr int NUM_WARPS = 16, NUM_THREADS = NUM_WARPS * 32;
@@ -44,31 +46,49 @@ constexpr int DEC_READERS = W_WARPS + 4 + 4;              // warps that read a c
 constexpr uint32_t TM_CB = 0, TM_YO = 256, TM_YI = 384, TM_DS = 448;
 constexpr float LOG2E = 1.4426950408889634f;
 
+// Sixteen fp32 values of a row as bf16: one 32-byte store where the row has room and its address allows it.
+__device__ __forceinline__ void store16(__nv_bfloat16 *to, const uint32_t *v, int room, bool wide) {
+    uint32_t w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = tc::pack_bf16x2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
+    if (wide && room >= 16) {
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                     : "memory");
+    } else {
+        if (room >= 8) *(uint4 *)to = make_uint4(w[0], w[1], w[2], w[3]);
+        if (room >= 16) *(uint4 *)(to + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+    }
+}
 __device__ __forceinline__ void warp_arrive(uint64_t *bar, int lane) {
     __syncwarp();
     if (lane == 0) tc::mbar_arrive(bar);
 }
 
-// The state warps and the epilogue warps have left their loops.
-__device__ __forceinline__ void both_done() { asm volatile("barrier.sync 1, 256;" ::: "memory"); }
+// The state warps among themselves.
+__device__ __forceinline__ void state_warps_sync() { asm volatile("barrier.sync 1, 128;" ::: "memory"); }
 
 // Descriptor arithmetic: the 14-bit start-address field holds (shared address >> 4); every operand of
 // this kernel lies below 256 KB, so adding a byte offset >> 4 to the descriptor never carries out of it.
 __device__ __forceinline__ uint64_t desc_add(uint64_t d, uint32_t bytes) { return d + (uint64_t)(bytes >> 4); }
-// Xs and Xs' of one chunk (same swizzled layout as the X tile), 128 threads, eight 16-byte units each, in registers: hi = bf16(w x), lo = bf16(w x - hi).
-// Rows from `valid` on are another sequence's: zeroed, in the X tile too.  Returns NaN when some x is not finite, else zero.
-__device__ __forceinline__ float split_x(uint8_t *x_tile, const float *dec_xw, int tid_g, int valid, uint4 (&hi)[8], uint4 (&lo)[8]) {
-    uint4 *src = (uint4 *)x_tile;
+// Half (64 tokens) of Xs and Xs' of one chunk (same swizzled layout as the X tile), 128 threads, four 16-byte units each: hi = bf16(w x),
+// lo = bf16(w x - hi).  Rows from `valid` on are another sequence's: zeroed, in the X tile too.  Returns NaN when some x is not finite, else zero.
+__device__ __forceinline__ float split_x(uint8_t *x_tile, uint8_t *hi_tile, uint8_t *lo_tile, const float *dec_xw, int tid_g, int half, int valid) {
     const __nv_bfloat162 zero = __float2bfloat162_rn(0.f);
     __nv_bfloat162 odd = zero;
+    uint4 v[4];
+    float sc[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int u = tid_g + 128 * i;
-        const float sc = dec_xw[u >> 3];
-        const float2 sc2 = make_float2(sc, sc);
-        uint4 v = src[u];
-        if ((u >> 3) >= valid) src[u] = v = make_uint4(0u, 0u, 0u, 0u);
-        const uint32_t in[4] = {v.x, v.y, v.z, v.w};
+    for (int i = 0; i < 4; ++i) {
+        const int u = tid_g + 128 * (4 * half + i);
+        v[i] = ((const uint4 *)x_tile)[u];
+        sc[i] = dec_xw[u >> 3];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int u = tid_g + 128 * (4 * half + i);
+        if ((u >> 3) >= valid) ((uint4 *)x_tile)[u] = v[i] = make_uint4(0u, 0u, 0u, 0u);
+        const float2 sc2 = make_float2(sc[i], sc[i]);
+        const uint32_t in[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
         uint32_t h[4], l[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -78,8 +98,8 @@ __device__ __forceinline__ float split_x(uint8_t *x_tile, const float *dec_xw, i
             const float2 r = __fadd2_rn(p, make_float2(-__uint_as_float(h[j] << 16), -__uint_as_float(h[j] & 0xFFFF0000u)));
             l[j] = tc::pack_bf16x2(r.x, r.y);
         }
-        hi[i] = make_uint4(h[0], h[1], h[2], h[3]);
-        lo[i] = make_uint4(l[0], l[1], l[2], l[3]);
+        ((uint4 *)hi_tile)[u] = make_uint4(h[0], h[1], h[2], h[3]);
+        ((uint4 *)lo_tile)[u] = make_uint4(l[0], l[1], l[2], l[3]);
     }
     return __low2float(odd) + __high2float(odd);
 }
@@ -199,8 +219,8 @@ scan_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_c
             tc::mbar_init(bars + B_CBF + i, 1); tc::mbar_init(bars + B_WF + i, W_WARPS);
         }
         for (int i = 0; i < DEC_DEPTH; ++i) { tc::mbar_init(bars + B_DECF + i, 1); tc::mbar_init(bars + B_DECE + i, DEC_READERS); }
-        tc::mbar_init(bars + B_XSF, 4); tc::mbar_init(bars + B_DSF, 1); tc::mbar_init(bars + B_DSE, 4);
-        tc::mbar_init(bars + B_SF, 4); tc::mbar_init(bars + B_YF, 1); tc::mbar_init(bars + B_YE, 4); tc::mbar_init(bars + B_XLF, 4);
+        tc::mbar_init(bars + B_XSF, 4); tc::mbar_init(bars + B_XSF + 1, 4); tc::mbar_init(bars + B_DSF, 1); tc::mbar_init(bars + B_DSF + 1, 1); tc::mbar_init(bars + B_DSE, 4);
+        tc::mbar_init(bars + B_SF, 4); tc::mbar_init(bars + B_YF, 1); tc::mbar_init(bars + B_YE, 4);
         abort_flag[0] = 0; abort_flag[1] = 0; found[0] = 0;
         tc::fence_mbar_init();
         tc::prefetch_tmap(&tmap_x); tc::prefetch_tmap(&tmap_b); tc::prefetch_tmap(&tmap_c);
@@ -216,6 +236,28 @@ scan_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_c
         const float Ah2 = A[h] * LOG2E;
         const float *dtb = dt + (size_t)row0 * H + h;
         bool ok = true;
+        // Lane 0 is the TMA producer too.  The operands of chunk c go into the slots of chunk c-2 (B, C: ring of 2) and chunk c-3 (X: ring of 3)
+        // once dS_{c-2} is seen complete: the tensor pipe runs in order, so CB_{c-2}, Y_inter_{c-2}, Y_intra_{c-3} and both products with the
+        // pieces of chunk c-2, one of which lay in that X slot, are complete too.  No slot-release barriers are needed.  (Two barriers for dS in turn: the next arrival on the one
+        // waited for is that of chunk c itself, so it cannot be passed over.)
+        int n_loaded = 0;
+        auto load_chunk = [&](int c) {
+            const int t0 = row0 + c * Q, s = c & 1, sx = c % X_SLOTS;
+            uint64_t *fb = bars + B_BCF + s;
+            tc::mbar_arrive_expect_tx(fb, 4 * TILE_16K);
+            tc::tma_load_3d(smem + OFF_B + (s * 2) * TILE_16K, &tmap_b, fb, 0, g, t0);
+            tc::tma_load_3d(smem + OFF_B + (s * 2 + 1) * TILE_16K, &tmap_b, fb, 64, g, t0);
+            tc::tma_load_3d(smem + OFF_C + (s * 2) * TILE_16K, &tmap_c, fb, 0, g, t0);
+            tc::tma_load_3d(smem + OFF_C + (s * 2 + 1) * TILE_16K, &tmap_c, fb, 64, g, t0);
+            tc::mbar_arrive_expect_tx(bars + B_XF + sx, TILE_16K);
+            tc::tma_load_3d(smem + OFF_X + sx * TILE_16K, &tmap_x, bars + B_XF + sx, 0, h, t0);
+            ++n_loaded;
+        };
+        if (lane == 0) {
+            load_chunk(0);
+            if (nchunks > 1) load_chunk(1);
+        }
+        __syncwarp();
         float dv[4], dn[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) dn[i] = (4 * lane + i < Tlen) ? __ldg(dtb + (size_t)(4 * lane + i) * H) : 0.f;
@@ -278,8 +320,20 @@ scan_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_c
             if (lane < 16) dec[D_BLK + lane] = ((lane & 3) < (lane >> 2)) ? tc::ex2(bs - be) : 0.f;
             if (lane == 0) dec[D_EEND] = tc::ex2(l_end);
             warp_arrive(bars + B_DECF + d, lane);
+            if (c >= 2) {
+                if (!tc::mbar_wait(bars + B_DSF + (c & 1), ((c - 2) >> 1) & 1, abort_flag)) { ok = false; break; }
+                if (lane == 0) load_chunk(c);
+                __syncwarp();
+            }
         }
-        if (!ok && lane == 0) atomicCAS(status, 0, STR_ERR_TIMEOUT);
+        if (!ok && lane == 0) {
+            atomicCAS(status, 0, STR_ERR_TIMEOUT);
+            for (int back = 1; back <= 2 && back <= n_loaded; ++back) {       // let copies already issued land before the CTA goes away
+                const int j = n_loaded - back;
+                tc::mbar_wait(bars + B_BCF + (j & 1), (j >> 1) & 1, abort_flag + 1);
+                tc::mbar_wait(bars + B_XF + j % X_SLOTS, (j / X_SLOTS) & 1, abort_flag + 1);
+            }
+        }
     } else if (warp == 13) {
         // ------------------------------------------------------------------ MMA issuer
         // One elected thread runs the whole loop (the region is entered once, so the compiler knows it to be
@@ -328,18 +382,20 @@ scan_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_c
                         // Y_inter_c = C S_{c-1}^T
                         tc::mma8_ss<tc::StepKMajor2x64, tc::StepMNMajor>(tmem + TM_YO + (uint32_t)s * 64, dk_c, dm_sb, id_kn, false);
                     }
+                    // dS_c^T = B^T Xs + B^T Xs', half of the tokens after the other
+                    const uint64_t dm_b = desc_add(dm_b0, (uint32_t)s * 2 * TILE_16K);
+                    const uint64_t dm_lo = desc_add(dm_x0, (uint32_t)((c + X_SLOTS - 1) % X_SLOTS) * TILE_16K);
                     ok = tc::mbar_wait(bars + B_XSF, c & 1, abort_flag) && (c == 0 || tc::mbar_wait(bars + B_DSE, (c - 1) & 1, abort_flag));
                     if (!ok) break;
                     tc::tc_fence_after();
-                    // dS_c^T = B^T Xs
-                    tc::mma8_ss<tc::StepMNMajor, tc::StepMNMajor>(tmem + TM_DS, desc_add(dm_b0, (uint32_t)s * 2 * TILE_16K), dm_xs, id_nn, false);
-                    ok = tc::mbar_wait(bars + B_XLF, c & 1, abort_flag);
+                    tc::mma4_ss<tc::StepMNMajor, tc::StepMNMajor>(tmem + TM_DS, dm_b, dm_xs, id_nn, false);
+                    tc::mma4_ss<tc::StepMNMajor, tc::StepMNMajor>(tmem + TM_DS, dm_b, dm_lo, id_nn, true);
+                    ok = tc::mbar_wait(bars + B_XSF + 1, c & 1, abort_flag);
                     if (!ok) break;
                     tc::tc_fence_after();
-                    // dS_c^T += B^T Xs'
-                    tc::mma8_ss<tc::StepMNMajor, tc::StepMNMajor>(tmem + TM_DS, desc_add(dm_b0, (uint32_t)s * 2 * TILE_16K),
-                                                                  desc_add(dm_x0, (uint32_t)((c + X_SLOTS - 1) % X_SLOTS) * TILE_16K), id_nn, true);
-                    tc::mma_commit(bars + B_DSF);
+                    tc::mma4_ss<tc::StepMNMajor, tc::StepMNMajor>(tmem + TM_DS, desc_add(dm_b, 8192), desc_add(dm_xs, 8192), id_nn, true);
+                    tc::mma4_ss<tc::StepMNMajor, tc::StepMNMajor>(tmem + TM_DS, desc_add(dm_b, 8192), desc_add(dm_lo, 8192), id_nn, true);
+                    tc::mma_commit(bars + B_DSF + s);
                 }
             }
             if (!ok) atomicCAS(status, 0, STR_ERR_TIMEOUT);
@@ -418,42 +474,39 @@ scan_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_c
                                tc::pack_bf16x2(S[8 * q4 + 4], S[8 * q4 + 5]), tc::pack_bf16x2(S[8 * q4 + 6], S[8 * q4 + 7]));
             }
         };
-        // Lane 0 of the first state warp is the TMA producer.  The operands of chunk c+2 go into the slots of chunk
-        // c (B, C: ring of 2) and chunk c-1 (X: ring of 3) once dS_c is seen complete: the tensor pipe runs in
-        // order, so CB_c, Y_inter_c, Y_intra_{c-1} and dS_{c-1} (issued after all of Xs_{c-1} was written, i.e.
-        // after every read of X_{c-1}) are complete too.  No slot-release barriers are needed.
-        const bool loader = warp == 4 && lane == 0;
-        int n_loaded = 0;
-        auto load_chunk = [&](int c) {
-            const int t0 = row0 + c * Q, s = c & 1, sx = c % X_SLOTS;
-            uint64_t *fb = bars + B_BCF + s;
-            tc::mbar_arrive_expect_tx(fb, 4 * TILE_16K);
-            tc::tma_load_3d(smem + OFF_B + (s * 2) * TILE_16K, &tmap_b, fb, 0, g, t0);
-            tc::tma_load_3d(smem + OFF_B + (s * 2 + 1) * TILE_16K, &tmap_b, fb, 64, g, t0);
-            tc::tma_load_3d(smem + OFF_C + (s * 2) * TILE_16K, &tmap_c, fb, 0, g, t0);
-            tc::tma_load_3d(smem + OFF_C + (s * 2 + 1) * TILE_16K, &tmap_c, fb, 64, g, t0);
-            tc::mbar_arrive_expect_tx(bars + B_XF + sx, TILE_16K);
-            tc::tma_load_3d(smem + OFF_X + sx * TILE_16K, &tmap_x, bars + B_XF + sx, 0, h, t0);
-            ++n_loaded;
-        };
-        if (loader) {
-            load_chunk(0);
-            if (nchunks > 1) load_chunk(1);
-        }
         if (init) {
             copy_state(0);
             copy_state(1);
             tc::fence_proxy_async();
         }
         warp_arrive(bars + B_SF, lane);
+        const int tid_g = quad * 32 + lane;
+        bool odd = false;
 #pragma unroll 1
         for (int c = 0; c < nchunks && ok; ++c) {
-            const int d = c & (DEC_DEPTH - 1);
+            const int d = c & (DEC_DEPTH - 1), sx = c % X_SLOTS;
+            const float *dec = decs + d * DEC_FLOATS;
             if (!tc::mbar_wait(bars + B_DECF + d, (c >> 2) & 1, abort_flag)) { ok = false; break; }
-            const float eend = decs[d * DEC_FLOATS + D_EEND];
+            if (!tc::mbar_wait(bars + B_XF + sx, (c / X_SLOTS) & 1, abort_flag)) { ok = false; break; }
+            const int valid = min(Tlen - c * Q, Q);
+            if (valid < Q) {                          // B's rows behind the sequence (CB may be reading them: those columns are masked)
+                if (!tc::mbar_wait(bars + B_BCF + (c & 1), (c >> 1) & 1, abort_flag)) { ok = false; break; }
+                uint4 *bt = (uint4 *)(smem + OFF_B + (c & 1) * 2 * TILE_16K);
+                for (int u = valid * 8 + tid_g; u < Q * 8; u += 128) bt[u] = bt[u + TILE_16K / 16] = make_uint4(0u, 0u, 0u, 0u);
+            }
+            // Xs: dS_{c-1}, its last reader, is complete (seen below, one chunk ago).  Xs': so has to be Y_intra of the chunk whose X it replaces.
+            if (c > 0 && !tc::mbar_wait(bars + B_YF, (c - 1) & 1, abort_flag)) { ok = false; break; }
+#pragma unroll 1
+            for (int half = 0; half < 2; ++half) {
+                odd |= split_x(smem + OFF_X + sx * TILE_16K, smem + OFF_XS, smem + OFF_X + ((c + X_SLOTS - 1) % X_SLOTS) * TILE_16K, dec + D_XW, tid_g, half,
+                               valid) != 0.f;
+                tc::fence_proxy_async();
+                warp_arrive(bars + B_XSF + half, lane);
+            }
+            const float eend = dec[D_EEND];
             __syncwarp();
             if (lane == 0) tc::mbar_arrive(bars + B_DECE + d);
-            if (!tc::mbar_wait(bars + B_DSF, c & 1, abort_flag)) { ok = false; break; }
+            if (!tc::mbar_wait(bars + B_DSF + (c & 1), (c >> 1) & 1, abort_flag)) { ok = false; break; }
             tc::tc_fence_after();
 #pragma unroll
             for (int hf = 0; hf < 2; ++hf) {
@@ -476,65 +529,33 @@ scan_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_c
             }
             tc::fence_proxy_async();
             warp_arrive(bars + B_SF, lane);
-            if (loader && c + 2 < nchunks) load_chunk(c + 2);
         }
         if (!ok && lane == 0) atomicCAS(status, 0, STR_ERR_TIMEOUT);
-        if (!ok && loader) {                          // let copies already issued land before the CTA goes away
-            for (int back = 1; back <= 2 && back <= n_loaded; ++back) {
-                const int j = n_loaded - back;
-                tc::mbar_wait(bars + B_BCF + (j & 1), (j >> 1) & 1, abort_flag + 1);
-                tc::mbar_wait(bars + B_XF + j % X_SLOTS, (j / X_SLOTS) & 1, abort_flag + 1);
-            }
-        }
-        both_done();                                  // every x of the sequence has been looked at
+        if (odd) found[0] = 1;
+        state_warps_sync();                           // every x of the sequence has been looked at
         if (ok && fin && found[0] == 0 && row < n) {
 #pragma unroll
             for (int i = 0; i < 64; ++i)
                 if (i < p) fin[(size_t)i * n + row] = S[i];
         }
     } else if (warp < 12) {
-        // ------------------------------------------------------------------ Xs_{c+1}, then y of chunk c
+        // ------------------------------------------------------------------ y of chunk c
         const int quad = warp & 3, row = quad * 32 + lane;
-        const int tid_g = threadIdx.x - 256;
         const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
         __nv_bfloat16 *yb = y + ((size_t)row0 * H + h) * p;
+        const bool wide = p % 16 == 0 && ((uintptr_t)y & 31) == 0;
         bool ok = true;
 #pragma unroll 1
-        for (int c = 0; c <= nchunks; ++c) {
-            if (c < nchunks) {
-                const int d = c & (DEC_DEPTH - 1), sx = c % X_SLOTS;
-                const float *dec = decs + d * DEC_FLOATS;
-                if (!tc::mbar_wait(bars + B_DECF + d, (c >> 2) & 1, abort_flag)) { ok = false; break; }
-                if (!tc::mbar_wait(bars + B_XF + sx, (c / X_SLOTS) & 1, abort_flag)) { ok = false; break; }
-                uint4 hi[8], lo[8];
-                const int valid = min(Tlen - c * Q, Q);
-                if (split_x(smem + OFF_X + sx * TILE_16K, dec + D_XW, tid_g, valid, hi, lo) != 0.f) found[0] = 1;
-                if (valid < Q) {                      // B's rows behind the sequence (CB may be reading them: those columns are masked)
-                    if (!tc::mbar_wait(bars + B_BCF + (c & 1), (c >> 1) & 1, abort_flag)) { ok = false; break; }
-                    uint4 *bt = (uint4 *)(smem + OFF_B + (c & 1) * 2 * TILE_16K);
-                    for (int u = valid * 8 + tid_g; u < Q * 8; u += 128) bt[u] = bt[u + TILE_16K / 16] = make_uint4(0u, 0u, 0u, 0u);
-                }
-                if (c > 0 && !tc::mbar_wait(bars + B_DSF, (c - 1) & 1, abort_flag)) { ok = false; break; }   // Xs buffer free
-                uint4 *xs = (uint4 *)(smem + OFF_XS) + tid_g;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) xs[128 * i] = hi[i];
-                tc::fence_proxy_async();
-                warp_arrive(bars + B_XSF, lane);
-                if (c > 0 && !tc::mbar_wait(bars + B_YF, (c - 1) & 1, abort_flag)) { ok = false; break; }    // X of the chunk before: read
-                uint4 *xl = (uint4 *)(smem + OFF_X + ((c + X_SLOTS - 1) % X_SLOTS) * TILE_16K) + tid_g;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) xl[128 * i] = lo[i];
-                tc::fence_proxy_async();
-                warp_arrive(bars + B_XLF, lane);
-            }
-            if (c >= 1) {
-                const int cp = c - 1, d = cp & (DEC_DEPTH - 1), t0 = cp * Q;
-                const float er = decs[d * DEC_FLOATS + D_EROW + row];      // DECF of chunk cp was seen one iteration ago
+        for (int cp = 0; cp < nchunks; ++cp) {
+            {
+                const int d = cp & (DEC_DEPTH - 1), t0 = cp * Q;
+                if (!tc::mbar_wait(bars + B_DECF + d, (cp >> 2) & 1, abort_flag)) { ok = false; break; }
+                const float er = decs[d * DEC_FLOATS + D_EROW + row];
                 __syncwarp();
                 if (lane == 0) tc::mbar_arrive(bars + B_DECE + d);
                 if (!tc::mbar_wait(bars + B_YF, cp & 1, abort_flag)) { ok = false; break; }
                 tc::tc_fence_after();
-                uint4 *dst = (uint4 *)(yb + (size_t)(t0 + row) * H * p);
+                __nv_bfloat16 *dst = yb + (size_t)(t0 + row) * H * p;
                 const bool valid = t0 + row < Tlen;
                 uint32_t ya[32], yb2[32], yo[32];
                 tc::tmem_ld32(tmem + lane_base + TM_YI, ya);
@@ -553,12 +574,8 @@ scan_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_c
                 tc::tmem_ld32(tmem + lane_base + TM_YI + 32, yb2);
                 if (cp > 0 || init) tc::tmem_ld32(tmem + lane_base + TM_YO + (uint32_t)((cp & 1) * 64 + 32), yo);
                 if (valid) {
-#pragma unroll
-                    for (int ci = 0; ci < 4; ++ci)
-                        if (8 * ci < p) dst[ci] = make_uint4(tc::pack_bf16x2(__uint_as_float(ya[8 * ci]), __uint_as_float(ya[8 * ci + 1])),
-                                             tc::pack_bf16x2(__uint_as_float(ya[8 * ci + 2]), __uint_as_float(ya[8 * ci + 3])),
-                                             tc::pack_bf16x2(__uint_as_float(ya[8 * ci + 4]), __uint_as_float(ya[8 * ci + 5])),
-                                             tc::pack_bf16x2(__uint_as_float(ya[8 * ci + 6]), __uint_as_float(ya[8 * ci + 7])));
+                    store16(dst, ya, p, wide);
+                    store16(dst + 16, ya + 16, p - 16, wide);
                 }
                 tc::tmem_ld_wait();
                 tc::tc_fence_before();               // both accumulators are in registers
@@ -573,16 +590,11 @@ scan_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_c
                     }
                 }
                 if (valid) {
-#pragma unroll
-                    for (int ci = 0; ci < 4; ++ci)
-                        if (32 + 8 * ci < p) dst[4 + ci] = make_uint4(tc::pack_bf16x2(__uint_as_float(yb2[8 * ci]), __uint_as_float(yb2[8 * ci + 1])),
-                                                 tc::pack_bf16x2(__uint_as_float(yb2[8 * ci + 2]), __uint_as_float(yb2[8 * ci + 3])),
-                                                 tc::pack_bf16x2(__uint_as_float(yb2[8 * ci + 4]), __uint_as_float(yb2[8 * ci + 5])),
-                                                 tc::pack_bf16x2(__uint_as_float(yb2[8 * ci + 6]), __uint_as_float(yb2[8 * ci + 7])));
+                    store16(dst + 32, yb2, p - 32, wide);
+                    store16(dst + 48, yb2 + 16, p - 48, wide);
                 }
             }
         }
-        both_done();
         if (!ok && lane == 0) atomicCAS(status, 0, STR_ERR_TIMEOUT);
     }
     tc::tc_fence_before();
