@@ -5,15 +5,16 @@
 //               others: their dt counts as zero and their rows of X and B are zeroed in shared memory, as zero times what stands there need not be zero.
 //   states      The state starts from init_state; its bf16 copy is written before the first chunk, so Y_inter exists for every chunk.
 //   D skip      D_h is added to the diagonal of W: Y_intra = (W + D_h I) X.
-//   accuracy    The final state is an fp32 result.  Xs_j = exp(l_end - l_j) dt_j x_j is formed in fp32 and enters the tensor pipe as two bf16
+//   accuracy    The final state is an fp32 result.  Xs_j = exp(l_end - l_j) dt_j x_j is formed to 16 bits and enters the tensor pipe as two bf16
 //               pieces, Xs + Xs', relative error 2^-17 instead of 2^-8, and l_end - l_j as a sum from the end of the chunk, not as a difference.
 //               y is bf16 itself: W and the state's copy are narrowed once, relative error 2^-8 of each term at most, random in sign.
 //               Xs' has no buffer of its own: it takes the X slot of the chunk before, once that chunk's Y_intra is complete and until the
 //               chunk after next is loaded there.
 //   not finite  W is zero above the diagonal, and zero times infinity or NaN is NaN: an x that is not finite would reach the up to 127 tokens
-//               before it.  The warps that form Xs look for one; a CTA that found one runs its sequence anew token by token (scan_rows).
+//               before it.  It also makes the state infinite or NaN, to the end: a CTA whose state ends so runs its sequence anew token by token
+//               (scan_rows).
 // Warp roles: 0-3, 14, 15 W; 4-7 Xs, Xs' and the state; 8-11 epilogue; 12 decay vectors and TMA producer; 13 MMA issuer; iteration c
-// issues CB_c, Y_intra_{c-1}, Y_inter_c, then dS_c and dS'_c in halves of 64 tokens, as soon as these are there.  The chain from chunk to chunk is
+// issues CB_c, Y_intra_{c-1}, Y_inter_c, dS_c in halves of 64 tokens, as soon as these are there, and dS'_c.  The chain from chunk to chunk is
 // dS -> state (and its copy) -> Xs -> dS; the state warps, who wait for dS anyhow, form Xs, so that no other role's work lies on it (formed by
 // the epilogue's warps, in front of each epilogue, it took 4400 clocks a chunk).
 // All mbarrier waits are bounded; a give-up records STR_ERR_TIMEOUT and tears the CTA down.
@@ -25,19 +26,20 @@ namespace {
 
 constexpr int Q = 128, P = 64, NS = 128;
 constexpr int TILE_16K = 16384;
-constexpr int X_SLOTS = 3, DEC_DEPTH = 4, DEC_FLOATS = 800;
+constexpr int X_SLOTS = 3, DEC_DEPTH = 4, DEC_FLOATS = 928;
 constexpr int OFF_X = 0;                                  // 3 x 16 KB
 constexpr int OFF_B = OFF_X + X_SLOTS * TILE_16K;         // 2 x 32 KB
 constexpr int OFF_C = OFF_B + 4 * TILE_16K;               // 2 x 32 KB
 constexpr int OFF_XS = OFF_C + 4 * TILE_16K;              // 16 KB
 constexpr int OFF_SB = OFF_XS + TILE_16K;                 // 16 KB
-constexpr int OFF_DEC = OFF_SB + TILE_16K;                // 4 x 3200 B
-constexpr int OFF_BARS = OFF_DEC + DEC_DEPTH * DEC_FLOATS * 4;
+constexpr int OFF_DEC = OFF_SB + TILE_16K;                // 4 x 3712 B
+constexpr int OFF_MASK = OFF_DEC + DEC_DEPTH * DEC_FLOATS * 4;   // 2 KB: which pairs of columns of a 32 x 32 block lie on or below its diagonal
+constexpr int OFF_BARS = OFF_MASK + 2048;
 // decay vectors of one chunk (floats): log2-domain cumulative decay l_j, log2(dt_j) - l_j, column / state / row factors
-constexpr int D_LS = 0, D_NLC = 128, D_COLF = 256, D_XW = 384, D_ROWF = 512, D_EROW = 640, D_BLK = 768, D_EEND = 784;
+constexpr int D_LS = 0, D_NLC = 128, D_COLF = 256, D_XW = 384, D_ROWF = 640, D_EROW = 768, D_BLK = 896, D_EEND = 912;
 enum {
     B_XF = 0, B_BCF = 3, B_DECF = 5, B_DECE = 9, B_CBF = 13, B_WF = 15, B_XSF = 17, B_DSF = 19, B_DSE = 21,
-    B_SF, B_YF, B_YE, B_COUNT
+    B_SF, B_YF, B_YE, B_XLF, B_COUNT
 };
 constexpr size_t SMEM_BYTES = (size_t)OFF_BARS + B_COUNT * 8 + 32;
 constexpr int NUM_WARPS = 16, NUM_THREADS = NUM_WARPS * 32;
@@ -70,51 +72,58 @@ __device__ __forceinline__ void state_warps_sync() { asm volatile("barrier.sync 
 // Descriptor arithmetic: the 14-bit start-address field holds (shared address >> 4); every operand of
 // this kernel lies below 256 KB, so adding a byte offset >> 4 to the descriptor never carries out of it.
 __device__ __forceinline__ uint64_t desc_add(uint64_t d, uint32_t bytes) { return d + (uint64_t)(bytes >> 4); }
-// Half (64 tokens) of Xs and Xs' of one chunk (same swizzled layout as the X tile), 128 threads, four 16-byte units each: hi = bf16(w x),
-// lo = bf16(w x - hi).  Rows from `valid` on are another sequence's: zeroed, in the X tile too.  Returns NaN when some x is not finite, else zero.
-__device__ __forceinline__ float split_x(uint8_t *x_tile, uint8_t *hi_tile, uint8_t *lo_tile, const float *dec_xw, int tid_g, int half, int valid) {
-    const __nv_bfloat162 zero = __float2bfloat162_rn(0.f);
-    __nv_bfloat162 odd = zero;
+// Half (64 tokens) of Xs and Xs' of one chunk (same swizzled layout as the X tile), 128 threads, four 16-byte units each.  The factor comes as two
+// bf16 pieces, w = w1 + w2 to 2^-17; hi = bf16(w1 x), whose rounding error w1 x - hi is itself a bf16 number, and lo = bf16(w2 x + that error): hi + lo is
+// w x to 2^-16, in three packed instructions a pair.  lo stays in registers until its place is free.  Rows from `valid` on are another sequence's: zeroed, in the X tile too.
+__device__ __forceinline__ void split_x(uint8_t *x_tile, uint8_t *hi_tile, uint4 (&lo)[4], const float *dec_xw, int tid_g, int half, int valid) {
     uint4 v[4];
-    float sc[4];
+    uint2 w[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int u = tid_g + 128 * (4 * half + i);
         v[i] = ((const uint4 *)x_tile)[u];
-        sc[i] = dec_xw[u >> 3];
+        w[i] = ((const uint2 *)dec_xw)[u >> 3];
     }
+    if (valid < Q)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int u = tid_g + 128 * (4 * half + i);
+            if ((u >> 3) >= valid) ((uint4 *)x_tile)[u] = v[i] = make_uint4(0u, 0u, 0u, 0u);
+        }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int u = tid_g + 128 * (4 * half + i);
-        if ((u >> 3) >= valid) ((uint4 *)x_tile)[u] = v[i] = make_uint4(0u, 0u, 0u, 0u);
-        const float2 sc2 = make_float2(sc[i], sc[i]);
-        const uint32_t in[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
-        uint32_t h[4], l[4];
+        const __nv_bfloat162 w1 = *reinterpret_cast<const __nv_bfloat162 *>(&w[i].x), w2 = *reinterpret_cast<const __nv_bfloat162 *>(&w[i].y);
+        __nv_bfloat162 *x = reinterpret_cast<__nv_bfloat162 *>(&v[i]);
+        __nv_bfloat162 *l = reinterpret_cast<__nv_bfloat162 *>(&lo[i]);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            odd = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&in[j]), zero, odd);
-            const float2 p = __fmul2_rn(make_float2(__uint_as_float(in[j] << 16), __uint_as_float(in[j] & 0xFFFF0000u)), sc2);
-            h[j] = tc::pack_bf16x2(p.x, p.y);
-            const float2 r = __fadd2_rn(p, make_float2(-__uint_as_float(h[j] << 16), -__uint_as_float(h[j] & 0xFFFF0000u)));
-            l[j] = tc::pack_bf16x2(r.x, r.y);
+            const __nv_bfloat162 h = __hmul2(x[j], w1);
+            l[j] = __hfma2(x[j], w2, __hfma2(x[j], w1, __hneg2(h)));
+            x[j] = h;
         }
-        ((uint4 *)hi_tile)[u] = make_uint4(h[0], h[1], h[2], h[3]);
-        ((uint4 *)lo_tile)[u] = make_uint4(l[0], l[1], l[2], l[3]);
+        ((uint4 *)hi_tile)[u] = v[i];
     }
-    return __low2float(odd) + __high2float(odd);
 }
 
 // One 16-column piece of W = CB o decay for this thread's token row: fp32 CB values in, eight packed bf16 pairs out.
-// Diagonal 32x32 block: one exponential per element, exp2(l_t + (log2 dt_j - l_j)), masked above the diagonal.
-__device__ __forceinline__ void w_piece_diag(const uint32_t (&v)[16], uint32_t (&packed)[8], const float *dec, int col0, int row, float l_t, float skip) {
+// Diagonal 32x32 block: one exponential per element, exp2(l_t + (log2 dt_j - l_j)).  Above the diagonal anything may come of it (infinities, and NaN where B
+// is not finite): those elements are cleared as bits.  D is added to the pair that holds this row's diagonal element.
+__device__ __forceinline__ void w_piece_diag(const uint32_t (&v)[16], uint32_t (&packed)[8], const float *dec, const uint4 *mask, int col0, int lane, float l_t, float2 skip) {
     const float2 lt2 = make_float2(l_t, l_t);
+    const int pair0 = (col0 & 31) >> 1;
 #pragma unroll
-    for (int i2 = 0; i2 < 8; ++i2) {
-        const float2 nl = *(const float2 *)(dec + D_NLC + col0 + 2 * i2);
-        const int j0 = col0 + 2 * i2;
-        const float2 a = __fadd2_rn(lt2, nl);
-        const float w0 = __uint_as_float(v[2 * i2]) * tc::ex2(a.x), w1 = __uint_as_float(v[2 * i2 + 1]) * tc::ex2(a.y);
-        packed[i2] = tc::pack_bf16x2(j0 < row ? w0 : j0 == row ? w0 + skip : 0.f, j0 + 1 < row ? w1 : j0 + 1 == row ? w1 + skip : 0.f);
+    for (int i4 = 0; i4 < 2; ++i4) {
+        const uint4 m4 = mask[(pair0 / 4 + i4) * 32 + lane];
+        const uint32_t m[4] = {m4.x, m4.y, m4.z, m4.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int i2 = 4 * i4 + k;
+            const float2 a = __fadd2_rn(lt2, *(const float2 *)(dec + D_NLC + col0 + 2 * i2));
+            float2 w = __fmul2_rn(make_float2(__uint_as_float(v[2 * i2]), __uint_as_float(v[2 * i2 + 1])), make_float2(tc::ex2(a.x), tc::ex2(a.y)));
+            if ((lane >> 1) == pair0 + i2) w = __fadd2_rn(w, skip);
+            packed[i2] = tc::pack_bf16x2(w.x, w.y) & m[k];
+        }
     }
 }
 // Block below the diagonal: exp(l_t - l_j) dt_j = f (row part times block-pair scalar) * column part, each <= 1.
@@ -185,7 +194,7 @@ scan_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_c
     uint64_t *bars = (uint64_t *)(smem + OFF_BARS);
     uint32_t *tmem_slot = (uint32_t *)(bars + B_COUNT);
     volatile int *abort_flag = (volatile int *)(tmem_slot + 1);       // [2]
-    volatile int *found = abort_flag + 2;                             // an x that is not finite
+    volatile int *found = abort_flag + 2;                             // the state is not finite
 
     // Role numbers (the `warp` used below) are decoupled from hardware warp numbers: when several warps of a
     // scheduler are ready it favours the lower-numbered one, so the MMA issuer and the decay warp, which need
@@ -220,10 +229,14 @@ scan_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_c
         }
         for (int i = 0; i < DEC_DEPTH; ++i) { tc::mbar_init(bars + B_DECF + i, 1); tc::mbar_init(bars + B_DECE + i, DEC_READERS); }
         tc::mbar_init(bars + B_XSF, 4); tc::mbar_init(bars + B_XSF + 1, 4); tc::mbar_init(bars + B_DSF, 1); tc::mbar_init(bars + B_DSF + 1, 1); tc::mbar_init(bars + B_DSE, 4);
-        tc::mbar_init(bars + B_SF, 4); tc::mbar_init(bars + B_YF, 1); tc::mbar_init(bars + B_YE, 4);
+        tc::mbar_init(bars + B_SF, 4); tc::mbar_init(bars + B_YF, 1); tc::mbar_init(bars + B_YE, 4); tc::mbar_init(bars + B_XLF, 4);
         abort_flag[0] = 0; abort_flag[1] = 0; found[0] = 0;
         tc::fence_mbar_init();
         tc::prefetch_tmap(&tmap_x); tc::prefetch_tmap(&tmap_b); tc::prefetch_tmap(&tmap_c);
+    }
+    {
+        const int k = threadIdx.x >> 5;               // pair of columns 2k, 2k + 1 of a block, against row `lane`
+        ((uint32_t *)(smem + OFF_MASK))[((k >> 2) * 32 + lane) * 4 + (k & 3)] = (2 * k <= lane ? 0xFFFFu : 0u) | (2 * k + 1 <= lane ? 0xFFFF0000u : 0u);
     }
     if (warp == 13) { tc::tmem_alloc(tmem_slot, 512); tc::tmem_relinquish(); }
     tc::tc_fence_before();
@@ -300,21 +313,26 @@ scan_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_c
             const float bs = __shfl_sync(0xffffffffu, excl, ((lane >> 2) & 3) * 8);
             const float be = __shfl_sync(0xffffffffu, incl, (lane & 3) * 8 + 7);
             float *dec = decs + d * DEC_FLOATS;
-            float o_ls[4], o_nlc[4], o_colf[4], o_xw[4], o_rowf[4], o_erow[4];
+            float o_ls[4], o_nlc[4], o_colf[4], o_rowf[4], o_erow[4];
+            uint32_t o_xw[8];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float li = excl + l[i];
                 o_ls[i] = li;
                 o_nlc[i] = tc::lg2(dv[i]) - li;          // exp2(l_t + nlc_j) = exp(l_t - l_j) dt_j; a padded token (dt = 0) gives -inf
                 o_colf[i] = tc::ex2(l_endb - li) * dv[i];
-                o_xw[i] = tc::ex2(behind + tail[i]) * dv[i];
+                const float xw = tc::ex2(behind + tail[i]) * dv[i];
+                o_xw[2 * i] = tc::pack_bf16x2(xw, xw);
+                const float rest = xw - __uint_as_float(o_xw[2 * i] & 0xFFFF0000u);
+                o_xw[2 * i + 1] = tc::pack_bf16x2(rest, rest);
                 o_rowf[i] = tc::ex2(li - l_start);
                 o_erow[i] = tc::ex2(li);
             }
             *(float4 *)(dec + D_LS + 4 * lane) = make_float4(o_ls[0], o_ls[1], o_ls[2], o_ls[3]);
             *(float4 *)(dec + D_NLC + 4 * lane) = make_float4(o_nlc[0], o_nlc[1], o_nlc[2], o_nlc[3]);
             *(float4 *)(dec + D_COLF + 4 * lane) = make_float4(o_colf[0], o_colf[1], o_colf[2], o_colf[3]);
-            *(float4 *)(dec + D_XW + 4 * lane) = make_float4(o_xw[0], o_xw[1], o_xw[2], o_xw[3]);
+            *(uint4 *)(dec + D_XW + 8 * lane) = make_uint4(o_xw[0], o_xw[1], o_xw[2], o_xw[3]);
+            *(uint4 *)(dec + D_XW + 8 * lane + 4) = make_uint4(o_xw[4], o_xw[5], o_xw[6], o_xw[7]);
             *(float4 *)(dec + D_ROWF + 4 * lane) = make_float4(o_rowf[0], o_rowf[1], o_rowf[2], o_rowf[3]);
             *(float4 *)(dec + D_EROW + 4 * lane) = make_float4(o_erow[0], o_erow[1], o_erow[2], o_erow[3]);
             if (lane < 16) dec[D_BLK + lane] = ((lane & 3) < (lane >> 2)) ? tc::ex2(bs - be) : 0.f;
@@ -382,19 +400,21 @@ scan_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_c
                         // Y_inter_c = C S_{c-1}^T
                         tc::mma8_ss<tc::StepKMajor2x64, tc::StepMNMajor>(tmem + TM_YO + (uint32_t)s * 64, dk_c, dm_sb, id_kn, false);
                     }
-                    // dS_c^T = B^T Xs + B^T Xs', half of the tokens after the other
+                    // dS_c^T = B^T Xs, half of the tokens after the other, + B^T Xs'
                     const uint64_t dm_b = desc_add(dm_b0, (uint32_t)s * 2 * TILE_16K);
                     const uint64_t dm_lo = desc_add(dm_x0, (uint32_t)((c + X_SLOTS - 1) % X_SLOTS) * TILE_16K);
                     ok = tc::mbar_wait(bars + B_XSF, c & 1, abort_flag) && (c == 0 || tc::mbar_wait(bars + B_DSE, (c - 1) & 1, abort_flag));
                     if (!ok) break;
                     tc::tc_fence_after();
                     tc::mma4_ss<tc::StepMNMajor, tc::StepMNMajor>(tmem + TM_DS, dm_b, dm_xs, id_nn, false);
-                    tc::mma4_ss<tc::StepMNMajor, tc::StepMNMajor>(tmem + TM_DS, dm_b, dm_lo, id_nn, true);
                     ok = tc::mbar_wait(bars + B_XSF + 1, c & 1, abort_flag);
                     if (!ok) break;
                     tc::tc_fence_after();
                     tc::mma4_ss<tc::StepMNMajor, tc::StepMNMajor>(tmem + TM_DS, desc_add(dm_b, 8192), desc_add(dm_xs, 8192), id_nn, true);
-                    tc::mma4_ss<tc::StepMNMajor, tc::StepMNMajor>(tmem + TM_DS, desc_add(dm_b, 8192), desc_add(dm_lo, 8192), id_nn, true);
+                    ok = tc::mbar_wait(bars + B_XLF, c & 1, abort_flag);
+                    if (!ok) break;
+                    tc::tc_fence_after();
+                    tc::mma8_ss<tc::StepMNMajor, tc::StepMNMajor>(tmem + TM_DS, dm_b, dm_lo, id_nn, true);
                     tc::mma_commit(bars + B_DSF + s);
                 }
             }
@@ -415,6 +435,7 @@ scan_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_c
         const int first = half ? (quad == 2 ? 64 : 80) : 0;
         const int n_real = half ? (quad == 2 ? 2 : 3) : (quad == 0 ? 2 : quad == 1 ? 4 : quad + 2);
         const int zero_first = half ? 96 : (quad == 0 ? 32 : 64);
+        const float2 skip2 = lane & 1 ? make_float2(0.f, skip) : make_float2(skip, 0.f);
         const int n_zero = half ? (quad == 2 ? 2 : 0) : (quad == 0 ? 6 : quad == 1 ? 4 : 0);
         bool ok = true;
 #pragma unroll 1
@@ -438,7 +459,7 @@ scan_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_c
                 if (k < n_real) {
                     const int col0 = first + 16 * k, bj = col0 >> 5;
                     uint32_t packed[8];
-                    if (bj == quad) w_piece_diag(v[k], packed, dec, col0, row, l_t, skip);
+                    if (bj == quad) w_piece_diag(v[k], packed, dec, (const uint4 *)(smem + OFF_MASK), col0, lane, l_t, skip2);
                     else w_piece_below(v[k], packed, dec, col0, rf * dec[D_BLK + quad * 4 + bj]);
                     tc::tmem_st8(tW + (uint32_t)col0, packed);
                 }
@@ -481,31 +502,41 @@ scan_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_c
         }
         warp_arrive(bars + B_SF, lane);
         const int tid_g = quad * 32 + lane;
-        bool odd = false;
+        auto inputs_there = [&](int c) {              // decay vectors and X of chunk c
+            return tc::mbar_wait(bars + B_DECF + (c & (DEC_DEPTH - 1)), (c >> 2) & 1, abort_flag) &&
+                   tc::mbar_wait(bars + B_XF + c % X_SLOTS, (c / X_SLOTS) & 1, abort_flag);
+        };
+        ok = inputs_there(0);
 #pragma unroll 1
         for (int c = 0; c < nchunks && ok; ++c) {
             const int d = c & (DEC_DEPTH - 1), sx = c % X_SLOTS;
             const float *dec = decs + d * DEC_FLOATS;
-            if (!tc::mbar_wait(bars + B_DECF + d, (c >> 2) & 1, abort_flag)) { ok = false; break; }
-            if (!tc::mbar_wait(bars + B_XF + sx, (c / X_SLOTS) & 1, abort_flag)) { ok = false; break; }
             const int valid = min(Tlen - c * Q, Q);
             if (valid < Q) {                          // B's rows behind the sequence (CB may be reading them: those columns are masked)
                 if (!tc::mbar_wait(bars + B_BCF + (c & 1), (c >> 1) & 1, abort_flag)) { ok = false; break; }
                 uint4 *bt = (uint4 *)(smem + OFF_B + (c & 1) * 2 * TILE_16K);
                 for (int u = valid * 8 + tid_g; u < Q * 8; u += 128) bt[u] = bt[u + TILE_16K / 16] = make_uint4(0u, 0u, 0u, 0u);
             }
-            // Xs: dS_{c-1}, its last reader, is complete (seen below, one chunk ago).  Xs': so has to be Y_intra of the chunk whose X it replaces.
+            // Xs: its last reader, dS_{c-1}, is complete (seen below, one chunk ago).  Xs': so has to be Y_intra of the chunk whose X it replaces.
+            uint4 lo[2][4];
+            split_x(smem + OFF_X + sx * TILE_16K, smem + OFF_XS, lo[0], dec + D_XW, tid_g, 0, valid);
+            tc::fence_proxy_async();
+            warp_arrive(bars + B_XSF, lane);
+            split_x(smem + OFF_X + sx * TILE_16K, smem + OFF_XS, lo[1], dec + D_XW, tid_g, 1, valid);
+            tc::fence_proxy_async();
+            warp_arrive(bars + B_XSF + 1, lane);
             if (c > 0 && !tc::mbar_wait(bars + B_YF, (c - 1) & 1, abort_flag)) { ok = false; break; }
-#pragma unroll 1
-            for (int half = 0; half < 2; ++half) {
-                odd |= split_x(smem + OFF_X + sx * TILE_16K, smem + OFF_XS, smem + OFF_X + ((c + X_SLOTS - 1) % X_SLOTS) * TILE_16K, dec + D_XW, tid_g, half,
-                               valid) != 0.f;
+            {
+                uint4 *lo_tile = (uint4 *)(smem + OFF_X + ((c + X_SLOTS - 1) % X_SLOTS) * TILE_16K) + tid_g;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) lo_tile[128 * i] = lo[i >> 2][i & 3];
                 tc::fence_proxy_async();
-                warp_arrive(bars + B_XSF + half, lane);
+                warp_arrive(bars + B_XLF, lane);
             }
             const float eend = dec[D_EEND];
             __syncwarp();
             if (lane == 0) tc::mbar_arrive(bars + B_DECE + d);
+            if (c + 1 < nchunks && !inputs_there(c + 1)) { ok = false; break; }       // waited for before dS, not behind it
             if (!tc::mbar_wait(bars + B_DSF + (c & 1), (c >> 1) & 1, abort_flag)) { ok = false; break; }
             tc::tc_fence_after();
 #pragma unroll
@@ -531,8 +562,12 @@ scan_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_c
             warp_arrive(bars + B_SF, lane);
         }
         if (!ok && lane == 0) atomicCAS(status, 0, STR_ERR_TIMEOUT);
+        // An x that is not finite has made its column of dS, and with it of the state, NaN or infinite to the end.
+        bool odd = false;
+#pragma unroll
+        for (int i = 0; i < 64; ++i) odd |= !isfinite(S[i]);
         if (odd) found[0] = 1;
-        state_warps_sync();                           // every x of the sequence has been looked at
+        state_warps_sync();
         if (ok && fin && found[0] == 0 && row < n) {
 #pragma unroll
             for (int i = 0; i < 64; ++i)
