@@ -170,7 +170,9 @@ extern "C" int str_mamba2_prefill_packed(str_ctx *ctx, const str_ssd_packed_shap
     if (!dev.ok) return STR_ERR_CUDA;
     StrProfScope prof_scope(ctx, STR_CAT_SSD, stream);
     cudaStream_t st = (cudaStream_t)stream;
-    if (!str_force_simt() && str_scan_packed_tc_supported(s, x, B, C, y))
+    // The chunked kernel's CTAs cost what a chunk of 128 rows costs however few there are.  Sequences of 16 rows on average are where the two meet (one
+    // sequence, 128 heads of 64 x 128: 8 rows 6.6 us token by token against 9.0, 16 rows 9.5 against 9.0; 33 sequences, 24 heads: 16 rows 15 against 49).
+    if (!str_force_simt() && s->rows > 16LL * s->n_seq && str_scan_packed_tc_supported(s, x, B, C, y))
         return ++ctx->tc_calls, str_scan_packed_tc(ctx, s, x, dt, A, B, C, D, seq_start, init_state, y, final_state, st);
     ++ctx->fallback_calls;
     if (s->dtype == STR_BF16) return dispatch<__nv_bfloat16>(ctx, s, x, dt, A, B, C, D, seq_start, init_state, y, final_state, st);
