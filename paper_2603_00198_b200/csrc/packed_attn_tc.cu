@@ -30,6 +30,7 @@ constexpr int BQ = 128, BKV = 128, TILE_16K = 16384;      // rows x 64 bf16
 enum { B_Q = 0, B_KF, B_KE = B_KF + 2, B_VF = B_KE + 2, B_VR = B_VF + 2, B_VE = B_VR + 2, B_SF = B_VE + 2, B_PA = B_SF + 2, B_PB = B_PA + 2, B_OF = B_PB + 2,
        B_COUNT = B_OF + 2 };
 constexpr int NUM_WARPS = 11, NUM_THREADS = NUM_WARPS * 32;
+constexpr int POLY_EVERY = 6;                             // every so many pairs of exponentials run on the FMA pipe (0: none)
 constexpr uint32_t TM_S = 0, TM_O = 256;
 constexpr float RESCALE_THRESHOLD = 8.0f;                 // in log2 units
 
@@ -38,6 +39,37 @@ template <int HD> struct Smem {
     static constexpr int Q = 0, K = 2 * TILE, V = 4 * TILE, MISC = 6 * TILE;
     static constexpr size_t BYTES = (size_t)MISC + B_COUNT * 8 + 32 + sizeof(PackedBlock);
 };
+
+// 2^x of two numbers on the FMA pipe: x = n + f with n the nearest whole number, a cubic in f on [-1/2, 1/2] (minimax, relative error 7.5e-5: a
+// fiftieth of the rounding to bf16 that follows), and n added to the exponent.  x <= 2^7; below -126 it stays at 2^-126.
+__device__ __forceinline__ float2 ex2_poly(float2 x) {
+    const float2 magic = make_float2(12582912.f, 12582912.f);         // 1.5 * 2^23: the sum's last bits are the whole number
+    x = make_float2(fmaxf(x.x, -126.f), fmaxf(x.y, -126.f));
+    const float2 t = __fadd2_rn(x, magic);
+    const float2 n = __fadd2_rn(t, make_float2(-12582912.f, -12582912.f));
+    const float2 f = __ffma2_rn(n, make_float2(-1.f, -1.f), x);
+    float2 p = __ffma2_rn(make_float2(0.05517166853f, 0.05517166853f), f, make_float2(0.24261112511f, 0.24261112511f));
+    p = __ffma2_rn(p, f, make_float2(0.69326096773f, 0.69326096773f));
+    p = __ffma2_rn(p, f, make_float2(0.99992805719f, 0.99992805719f));
+    return make_float2(__uint_as_float(__float_as_uint(p.x) + (__float_as_uint(t.x) << 23)), __uint_as_float(__float_as_uint(p.y) + (__float_as_uint(t.y) << 23)));
+}
+
+// Weights of 64 keys, exp2(scale (s - m)), narrowed and in pairs; their sum is added up as it was before.
+__device__ __forceinline__ void weights(const uint32_t (&s0)[32], const uint32_t (&s1)[32], float2 scale2, float m, uint32_t (&pk)[32], float2 &sum) {
+    const float mc = m == -INFINITY ? 0.f : m * scale2.x;
+    const float2 nmc2 = make_float2(-mc, -mc);
+#pragma unroll
+    for (int e = 0; e < 32; ++e) {
+        const uint32_t *s = e < 16 ? s0 : s1;
+        const int k = (2 * e) & 31;
+        const float2 a = __ffma2_rn(make_float2(__uint_as_float(s[k]), __uint_as_float(s[k + 1])), scale2, nmc2);
+        float2 p;
+        if (POLY_EVERY > 0 && e % (POLY_EVERY > 0 ? POLY_EVERY : 1) == POLY_EVERY - 1) p = ex2_poly(a);
+        else p = make_float2(tc::ex2(a.x), tc::ex2(a.y));
+        sum = __fadd2_rn(sum, p);
+        pk[e] = tc::pack_bf16x2(p.x, p.y);
+    }
+}
 
 // One row's output in fp32 arithmetic, by one warp: a lane takes a key for the scores and every 32nd column for the values.
 __device__ __noinline__ void attn_row(const __nv_bfloat16 *q, const __nv_bfloat16 *k, const __nv_bfloat16 *v, __nv_bfloat16 *o, size_t ld, int keys, int d,
@@ -288,11 +320,12 @@ attn_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_c
 #pragma unroll
             for (int e = 0; e < 32; e += 2)
 #pragma unroll
-                for (int c = 0; c < 4; ++c) top[c] = tc::max3(top[c], __uint_as_float(w[c][e]), __uint_as_float(w[c][e + 1]));
-            const float m_new = fmaxf(tc::max3(top[0], top[1], top[2]), top[3]);
+                for (int c = 0; c < 4; ++c) top[c] = tc::max3_nan(top[c], __uint_as_float(w[c][e]), __uint_as_float(w[c][e + 1]));
+            float m_new = tc::max3_nan(tc::max3_nan(top[0], top[1], top[2]), top[3], top[3]);
+            if (m_new == INFINITY) m_new = __int_as_float(0x7FFFFFFF);    // infinity minus infinity: the row is NaN, as with a NaN score
             // A row raises its maximum only when it has grown by more than the threshold: a decision of the row alone.  From minus infinity
             // (nothing seen yet) any score is growth.
-            const bool grow = (m_new - m) * scale_log2 > RESCALE_THRESHOLD;
+            const bool grow = (m_new - m) * scale_log2 > RESCALE_THRESHOLD || m_new != m_new;
             if (j == 0) {
                 m = m_new;
             } else if (__any_sync(0xffffffffu, grow)) {
@@ -311,20 +344,11 @@ attn_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_c
                 }
                 tc::tmem_st_wait();
             }
-            const float mc = m == -INFINITY ? 0.f : m * scale_log2;
-            const float2 nmc2 = make_float2(-mc, -mc);
             float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
             for (int hf = 0; hf < 2; ++hf) {
                 uint32_t pk[32];
-#pragma unroll
-                for (int e = 0; e < 32; ++e) {
-                    const int cc = 2 * hf + (e >> 4), ee = (2 * e) & 31;
-                    const float2 a = __ffma2_rn(make_float2(__uint_as_float(w[cc][ee]), __uint_as_float(w[cc][ee + 1])), scale2, nmc2);
-                    const float2 p = make_float2(tc::ex2(a.x), tc::ex2(a.y));
-                    sum = __fadd2_rn(sum, p);
-                    pk[e] = tc::pack_bf16x2(p.x, p.y);
-                }
+                weights(w[2 * hf], w[2 * hf + 1], scale2, m, pk, sum);
                 tc::tmem_st32(tS + hf * 32, pk);
                 tc::tmem_st_wait();
                 tc::tc_fence_before();
