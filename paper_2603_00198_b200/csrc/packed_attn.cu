@@ -209,11 +209,13 @@ int dispatch(str_ctx *ctx, const str_attn_packed_shape *s, const void *q, const 
 
 }  // namespace
 
-extern "C" size_t str_attn_prefill_packed_workspace_size(const str_attn_packed_shape *) { return 0; }
+extern "C" size_t str_attn_prefill_packed_workspace_size(const str_attn_packed_shape *s) {
+    if (!s || s->n_seq <= 0 || s->rows_q <= 0 || s->rows_k <= 0 || s->Hq <= 0 || s->Hkv <= 0 || s->Hq % s->Hkv != 0 || s->d <= 0) return 0;
+    return str_attn_packed_tc_workspace(s);
+}
 
 extern "C" int str_attn_prefill_packed(str_ctx *ctx, const str_attn_packed_shape *s, const void *q, const void *k, const void *v, const int32_t *q_start,
                                        const int32_t *k_start, float softmax_scale, void *o, void *workspace, size_t workspace_bytes, void *stream) {
-    (void)workspace;
     if (!ctx || !s || !q_start) return STR_ERR_INVALID_ARG;
     if (s->n_seq <= 0 || s->rows_q < 0 || s->rows_k < 0 || s->Hq <= 0 || s->Hkv <= 0 || s->Hq % s->Hkv != 0 || s->d <= 0 ||
         (s->dtype != STR_F32 && s->dtype != STR_BF16) || !(softmax_scale > 0.f) || !isfinite(softmax_scale * 1.4426950408889634f))
@@ -230,13 +232,15 @@ extern "C" int str_attn_prefill_packed(str_ctx *ctx, const str_attn_packed_shape
         return STR_ERR_UNSUPPORTED_SHAPE;
     const size_t es = dtype_size(s->dtype), qb = es * s->rows_q * s->Hq * s->d, kb = es * s->rows_k * s->Hkv * s->d;
     if (kv4_overlap(q, qb, o, qb) || kv4_overlap(k, kb, o, qb) || kv4_overlap(v, kb, o, qb)) return STR_ERR_INVALID_ARG;
-    if (workspace_bytes < str_attn_prefill_packed_workspace_size(s)) return STR_ERR_WORKSPACE_TOO_SMALL;
+    const size_t need = str_attn_prefill_packed_workspace_size(s);
+    if (workspace_bytes < need) return STR_ERR_WORKSPACE_TOO_SMALL;
+    if (need && (!workspace || ((uintptr_t)workspace & 255) != 0 || kv4_overlap(workspace, need, o, qb))) return STR_ERR_INVALID_ARG;
     StrDeviceScope dev(ctx);
     if (!dev.ok) return STR_ERR_CUDA;
     StrProfScope prof_scope(ctx, STR_CAT_ATTN_FWD, stream);
     cudaStream_t st = (cudaStream_t)stream;
     if (!str_force_simt() && str_attn_packed_tc_supported(s, q, k, v, o))
-        return ++ctx->tc_calls, str_attn_packed_tc(ctx, s, q, k, v, q_start, k_start, softmax_scale, o, st);
+        return ++ctx->tc_calls, str_attn_packed_tc(ctx, s, q, k, v, q_start, k_start, softmax_scale, o, workspace, st);
     ++ctx->fallback_calls;
     return s->dtype == STR_BF16 ? dispatch<__nv_bfloat16>(ctx, s, q, k, v, q_start, k_start, softmax_scale, o, st)
                                 : dispatch<float>(ctx, s, q, k, v, q_start, k_start, softmax_scale, o, st);

@@ -101,12 +101,22 @@ __device__ __noinline__ void attn_row(const __nv_bfloat16 *q, const __nv_bfloat1
         if (lane + 32 * i < d) stf(o + lane + 32 * i, keys > 0 ? acc[i] / l : 0.f);
 }
 
+// What CTAs that share a block's key tiles leave for the joining kernel (number n of them: unscaled outputs, maxima and sums of 256 rows, and whether a
+// hidden value was not finite).
+struct Parts {
+    int splits;                  // 1: there are none
+    float *o;                    // [n][256][HD]
+    float2 *stat;                // [n][256]: maximum (of unscaled scores), sum
+    int *found;                  // [n]
+    PackedBlock *block;          // [n / splits]: the block itself, so that the joining kernel need not look for it
+};
+
 template <int HD>
 __global__ void __launch_bounds__(NUM_THREADS, 1)
 attn_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
                       int n_seq, int rows_q, int rows_k, int Hq, int Hkv, int d, float scale_log2, const int32_t *__restrict__ q_start,
                       const int32_t *__restrict__ k_start, const __nv_bfloat16 *__restrict__ q, const __nv_bfloat16 *__restrict__ k,
-                      const __nv_bfloat16 *__restrict__ v, __nv_bfloat16 *__restrict__ out, int *status) {
+                      const __nv_bfloat16 *__restrict__ v, __nv_bfloat16 *__restrict__ out, const Parts parts, int *status) {
     typedef Smem<HD> SM;
     constexpr int HALVES = HD / 64;
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -118,7 +128,8 @@ attn_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_c
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int group = Hq / Hkv, TQ = BQ / group;                      // queries per tile
-    const int kv = blockIdx.x % Hkv;
+    const int kv = blockIdx.x % Hkv, split = blockIdx.x / Hkv % parts.splits, rank = blockIdx.x / Hkv / parts.splits;
+    const size_t part = ((size_t)rank * Hkv + kv) * parts.splits + split;
 
     if ((tc::smem_u32(smem) & 1023u) != 0) {
         if (threadIdx.x == 0) atomicCAS(status, 0, STR_ERR_CUDA);
@@ -130,7 +141,7 @@ attn_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_c
         packed_check(k_start, n_seq, rows_k, status);
     }
     if (warp == 0) {
-        const PackedBlock b = packed_block(q_start, k_start, n_seq, rows_q, rows_k, 2 * TQ, BKV, blockIdx.x / Hkv);
+        const PackedBlock b = packed_block(q_start, k_start, n_seq, rows_q, rows_k, 2 * TQ, BKV, rank);
         if (lane == 0) *blk = b;
     }
     if (threadIdx.x == 32) {
@@ -147,6 +158,7 @@ attn_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_c
     }
     __syncthreads();
     const PackedBlock b = *blk;
+    if (parts.splits > 1 && split == 0 && threadIdx.x == 0) parts.block[(size_t)rank * Hkv + kv] = b;
     if (b.n <= 0) return;                                             // more CTAs than blocks of queries
     if (warp == 9) { tc::tmem_alloc(tmem_slot, 512); tc::tmem_relinquish(); }
     tc::tc_fence_before();
@@ -156,9 +168,11 @@ attn_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_c
 
     // Query number t of the block sees the keys 0 .. first_limit + t.
     const int first_limit = b.lk - b.lq + b.first;
-    const int n0 = (max(first_limit + min(b.n, TQ), 0) + BKV - 1) / BKV;              // key tiles of row tile 0
-    const int n1 = b.n > TQ ? (max(first_limit + b.n, 0) + BKV - 1) / BKV : 0;        // of row tile 1; not fewer unless it is empty
-    const int nt = max(n0, n1);
+    const int all0 = (max(first_limit + min(b.n, TQ), 0) + BKV - 1) / BKV;            // key tiles of row tile 0
+    const int all1 = b.n > TQ ? (max(first_limit + b.n, 0) + BKV - 1) / BKV : 0;      // of row tile 1; not fewer unless it is empty
+    // This CTA's share of them: tiles j0 + j, j < n0 or n1.
+    const int share = (max(all0, all1) + parts.splits - 1) / parts.splits, j0 = split * share;
+    const int n0 = max(min(all0, j0 + share) - j0, 0), n1 = max(min(all1, j0 + share) - j0, 0), nt = max(n0, n1);
 
     if (warp == 8) {
         // ------------------------------------------------------------------ TMA producer
@@ -175,12 +189,12 @@ attn_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_c
                 if (!tc::mbar_wait(bars + B_KE + s, ph, abort_flag)) { ok = false; break; }
                 tc::mbar_arrive_expect_tx(bars + B_KF + s, SM::TILE);
                 for (int hf = 0; hf < HALVES; ++hf)
-                    tc::tma_load_3d(smem + SM::K + s * SM::TILE + hf * TILE_16K, &tmap_k, bars + B_KF + s, hf * 64, kv, b.k0 + j * BKV);
+                    tc::tma_load_3d(smem + SM::K + s * SM::TILE + hf * TILE_16K, &tmap_k, bars + B_KF + s, hf * 64, kv, b.k0 + (j0 + j) * BKV);
                 ++issued_k;
                 if (!tc::mbar_wait(bars + B_VE + s, ph, abort_flag)) { ok = false; break; }
                 tc::mbar_arrive_expect_tx(bars + B_VF + s, SM::TILE);
                 for (int hf = 0; hf < HALVES; ++hf)
-                    tc::tma_load_3d(smem + SM::V + s * SM::TILE + hf * TILE_16K, &tmap_v, bars + B_VF + s, hf * 64, kv, b.k0 + j * BKV);
+                    tc::tma_load_3d(smem + SM::V + s * SM::TILE + hf * TILE_16K, &tmap_v, bars + B_VF + s, hf * 64, kv, b.k0 + (j0 + j) * BKV);
                 ++issued_v;
             }
             if (!ok) {
@@ -263,7 +277,7 @@ attn_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_c
             const int s = j & 1;
             if (!tc::mbar_wait(bars + B_VF + s, (j >> 1) & 1, abort_flag)) { ok = false; break; }
             uint8_t *tile = smem + SM::V + s * SM::TILE;
-            const int valid = min(b.lk - j * BKV, BKV);               // rows of the tile that are the sequence's
+            const int valid = min(b.lk - (j0 + j) * BKV, BKV);               // rows of the tile that are the sequence's
             if (valid < BKV) {
                 for (int e = valid * 8 + lane; e < BKV * 8; e += 32)
 #pragma unroll
@@ -272,7 +286,7 @@ attn_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_c
                 __syncwarp();
             }
             if (lane == 0) tc::mbar_arrive(bars + B_VR + s);
-            if (j * BKV + BKV - 1 > first_limit) {                    // hidden in part: zero times what is finite stays zero
+            if ((j0 + j) * BKV + BKV - 1 > first_limit) {                    // hidden in part: zero times what is finite stays zero
                 const __nv_bfloat162 zero = __float2bfloat162_rn(0.f);
                 __nv_bfloat162 sum = zero;
 #pragma unroll 4
@@ -308,8 +322,8 @@ attn_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_c
 #pragma unroll
             for (int c = 0; c < 4; ++c) tc::tmem_ld32(tS + c * 32, w[c]);
             tc::tmem_ld_wait();
-            if (__any_sync(0xffffffffu, j * BKV + BKV - 1 > limit)) { // some row of this warp ends inside (or before) this tile
-                const int lim = limit - j * BKV;
+            if (__any_sync(0xffffffffu, (j0 + j) * BKV + BKV - 1 > limit)) { // some row of this warp ends inside (or before) this tile
+                const int lim = limit - (j0 + j) * BKV;
 #pragma unroll
                 for (int c = 0; c < 4; ++c)
 #pragma unroll
@@ -360,25 +374,40 @@ attn_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_c
         if (ok && ni > 0) ok = tc::mbar_wait(bars + B_OF + i, 0, abort_flag);
         if (ok) {
             tc::tc_fence_after();
-            const bool sees = limit >= 0;
-            const float inv = sees ? 1.0f / l : 0.f;
-            __nv_bfloat16 *dst = out + ((size_t)(b.q0 + b.first + t) * Hq + kv * group + row % group) * d;
-#pragma unroll 1
-            for (int c = 0; c < HD / 32; ++c) {
-                uint32_t o[32];
+            if (parts.splits > 1) {
+                const size_t at = part * 2 * BQ + i * BQ + row;
+                parts.stat[at] = make_float2(ni > 0 ? m : -INFINITY, l);
                 if (ni > 0) {
-                    tc::tmem_ld32(tO + c * 32, o);
-                    tc::tmem_ld_wait();
+#pragma unroll 1
+                    for (int c = 0; c < HD / 32; ++c) {
+                        uint32_t o[32];
+                        tc::tmem_ld32(tO + c * 32, o);
+                        tc::tmem_ld_wait();
+#pragma unroll
+                        for (int g = 0; g < 8; ++g) *(uint4 *)(parts.o + at * HD + c * 32 + 4 * g) = make_uint4(o[4 * g], o[4 * g + 1], o[4 * g + 2], o[4 * g + 3]);
+                    }
                 }
-                if (live) {
+            } else {
+                const bool sees = limit >= 0;
+                const float inv = sees ? 1.0f / l : 0.f;
+                __nv_bfloat16 *dst = out + ((size_t)(b.q0 + b.first + t) * Hq + kv * group + row % group) * d;
+#pragma unroll 1
+                for (int c = 0; c < HD / 32; ++c) {
+                    uint32_t o[32];
+                    if (ni > 0) {
+                        tc::tmem_ld32(tO + c * 32, o);
+                        tc::tmem_ld_wait();
+                    }
+                    if (live) {
 #pragma unroll
-                    for (int g = 0; g < 4; ++g) {
-                        if (c * 32 + g * 8 >= d) break;
-                        uint32_t r[4];
+                        for (int g = 0; g < 4; ++g) {
+                            if (c * 32 + g * 8 >= d) break;
+                            uint32_t r[4];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            r[e] = sees ? tc::pack_bf16x2(__uint_as_float(o[8 * g + 2 * e]) * inv, __uint_as_float(o[8 * g + 2 * e + 1]) * inv) : 0u;
-                        *reinterpret_cast<uint4 *>(dst + c * 32 + g * 8) = make_uint4(r[0], r[1], r[2], r[3]);
+                            for (int e = 0; e < 4; ++e)
+                                r[e] = sees ? tc::pack_bf16x2(__uint_as_float(o[8 * g + 2 * e]) * inv, __uint_as_float(o[8 * g + 2 * e + 1]) * inv) : 0u;
+                            *reinterpret_cast<uint4 *>(dst + c * 32 + g * 8) = make_uint4(r[0], r[1], r[2], r[3]);
+                        }
                     }
                 }
             }
@@ -389,7 +418,8 @@ attn_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_c
     tc::tc_fence_before();
     __syncthreads();
     if (warp == 9) { tc::tc_fence_after(); tc::tmem_dealloc(tmem, 512); }
-    if (found[0] == 0) return;
+    if (parts.splits > 1 && threadIdx.x == 0) parts.found[part] = found[0];
+    if (found[0] == 0 || parts.splits > 1) return;
     for (int r = warp; r < b.n * group; r += NUM_WARPS) {
         const int t = r / group;
         const size_t at = ((size_t)(b.q0 + b.first + t) * Hq + kv * group + r % group) * d, keys = ((size_t)b.k0 * Hkv + kv) * d;
@@ -397,9 +427,78 @@ attn_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_c
     }
 }
 
+// Joins the shares of each block: o = sum_s exp2(scale (m_s - m)) o_s / sum_s exp2(scale (m_s - m)) l_s, a warp a row.
+constexpr int JOIN_WARPS = 8, MAX_SPLITS = 16;
+template <int HD>
+__global__ void __launch_bounds__(JOIN_WARPS * 32)
+attn_packed_join_kernel(int Hq, int Hkv, int d, float scale_log2, const __nv_bfloat16 *__restrict__ q, const __nv_bfloat16 *__restrict__ k,
+                        const __nv_bfloat16 *__restrict__ v, __nv_bfloat16 *__restrict__ out, const Parts parts, const int *status) {
+    if (*(volatile const int *)status != 0) return;   // a share may be missing
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int group = Hq / Hkv, TQ = BQ / group, kv = blockIdx.x % Hkv;
+    const size_t part = (size_t)blockIdx.x * parts.splits;
+    const PackedBlock b = parts.block[blockIdx.x];
+    const bool any = b.n > 0 && __any_sync(0xffffffffu, lane < parts.splits && parts.found[part + lane] != 0);
+    const int first_limit = b.lk - b.lq + b.first;
+    for (int r = blockIdx.y * JOIN_WARPS + warp; r < b.n * group; r += gridDim.y * JOIN_WARPS) {
+        const int t = r / group;
+        const size_t at = ((size_t)(b.q0 + b.first + t) * Hq + kv * group + r % group) * d;
+        const int keys = max(first_limit + t + 1, 0);
+        if (any) {
+            const size_t k0 = ((size_t)b.k0 * Hkv + kv) * d;
+            attn_row(q + at, k + k0, v + k0, out + at, (size_t)Hkv * d, keys, d, scale_log2);
+            continue;
+        }
+        const int row = t < TQ ? r : BQ + (t - TQ) * group + r % group;
+        // lane s looks at share s; shares that saw nothing weigh nothing, and their outputs, which were never written, are not read
+        const float2 st = lane < parts.splits ? parts.stat[(part + lane) * 2 * BQ + row] : make_float2(-INFINITY, 0.f);
+        const float m = warp_max(st.x);
+        const float w = st.x == -INFINITY ? 0.f : exp2f((st.x - m) * scale_log2);
+        const float l = warp_sum(w * st.y);
+        const unsigned saw = __ballot_sync(0xffffffffu, st.x != -INFINITY);
+        float acc[HD / 32] = {};
+#pragma unroll 4
+        for (int s = 0; s < parts.splits; ++s) {
+            const float ws = __shfl_sync(0xffffffffu, w, s);
+            const float *o = parts.o + ((part + s) * 2 * BQ + row) * HD + lane * (HD / 32);
+            alignas(16) float x[HD / 32] = {};
+            if (saw >> s & 1) {
+                if constexpr (HD == 128) *(float4 *)x = *(const float4 *)o;
+                else *(float2 *)x = *(const float2 *)o;
+            }
+#pragma unroll
+            for (int i = 0; i < HD / 32; ++i) acc[i] = fmaf(ws, x[i], acc[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < HD / 32; ++i)
+            if (lane * (HD / 32) + i < d) stf(out + at + lane * (HD / 32) + i, keys > 0 ? acc[i] / l : 0.f);
+    }
+}
+
+// CTAs a block's key tiles are shared out to.  A turn of a few queries over many earlier keys makes few blocks, each a long walk: where they leave half of
+// the SMs without work, the walk is shared by as many CTAs as there is room for, four tiles each at least.  From the shape alone (the lengths are
+// on the device), so that the workspace is known beforehand.
+constexpr int SMS = 148;
+int splits_of(const str_attn_packed_shape *s) {
+    if (s->dtype != STR_BF16 || s->rows_q <= 0 || s->rows_k <= 0 || s->d > 128 || s->d % 8 != 0 || s->Hq / s->Hkv > BQ) return 1;
+    const long long ctas = ((long long)s->rows_q / (2 * (BQ / (s->Hq / s->Hkv))) + s->n_seq) * s->Hkv, tiles = s->rows_k / s->n_seq / BKV;
+    if (2 * ctas > SMS || tiles < 8) return 1;
+    const long long n = SMS / ctas < tiles / 4 ? SMS / ctas : tiles / 4;
+    return (int)(n < MAX_SPLITS ? n : MAX_SPLITS);
+}
+int blocks_of(const str_attn_packed_shape *s) { return s->rows_q / (2 * (BQ / (s->Hq / s->Hkv))) + s->n_seq; }   // at least as many as there are
+int padded(int d) { return d <= 64 ? 64 : 128; }
+Parts parts_in(const str_attn_packed_shape *s, void *workspace) {
+    const int splits = splits_of(s);
+    const size_t n = (size_t)blocks_of(s) * s->Hkv * splits;
+    uint8_t *o = (uint8_t *)workspace, *stat = o + n * 2 * BQ * padded(s->d) * sizeof(float);
+    int *found = (int *)(stat + n * 2 * BQ * sizeof(float2));
+    return {splits, (float *)o, (float2 *)stat, found, (PackedBlock *)(found + n)};
+}
+
 template <int HD>
 int launch(str_ctx *ctx, const str_attn_packed_shape *s, const void *q, const void *k, const void *v, const int32_t *q_start, const int32_t *k_start,
-           float scale, void *o, cudaStream_t st) {
+           float scale, void *o, void *workspace, cudaStream_t st) {
     const int group = s->Hq / s->Hkv, TQ = BQ / group;
     CUtensorMap tq, tk, tv;
     int rc = str_make_tmap_heads_bf16_sw128(ctx, &tq, q, s->d, s->Hq, s->rows_q, group, TQ);
@@ -408,11 +507,16 @@ int launch(str_ctx *ctx, const str_attn_packed_shape *s, const void *q, const vo
     if (rc != STR_OK) return rc;
     rc = str_ensure_smem(ctx, HD == 64 ? STR_SMEM_ATTN_PACKED_64 : STR_SMEM_ATTN_PACKED_128, attn_packed_tc_kernel<HD>, Smem<HD>::BYTES);
     if (rc != STR_OK) return rc;
-    const int blocks = s->rows_q / (2 * TQ) + s->n_seq;               // at least as many as there are blocks of queries
-    attn_packed_tc_kernel<HD><<<blocks * s->Hkv, NUM_THREADS, Smem<HD>::BYTES, st>>>(
-        tq, tk, tv, s->n_seq, s->rows_q, s->rows_k, s->Hq, s->Hkv, s->d, scale * 1.4426950408889634f, q_start, k_start, (const __nv_bfloat16 *)q,
-        (const __nv_bfloat16 *)k, (const __nv_bfloat16 *)v, (__nv_bfloat16 *)o, ctx->status_dev);
-    return str_launch_ok(ctx);
+    const Parts parts = parts_in(s, workspace);
+    const int blocks = blocks_of(s);
+    const float scale_log2 = scale * 1.4426950408889634f;
+    const __nv_bfloat16 *pq = (const __nv_bfloat16 *)q, *pk = (const __nv_bfloat16 *)k, *pv = (const __nv_bfloat16 *)v;
+    attn_packed_tc_kernel<HD><<<blocks * s->Hkv * parts.splits, NUM_THREADS, Smem<HD>::BYTES, st>>>(
+        tq, tk, tv, s->n_seq, s->rows_q, s->rows_k, s->Hq, s->Hkv, s->d, scale_log2, q_start, k_start, pq, pk, pv, (__nv_bfloat16 *)o, parts, ctx->status_dev);
+    if (parts.splits == 1) return str_launch_ok(ctx);
+    attn_packed_join_kernel<HD><<<dim3(blocks * s->Hkv, 16), JOIN_WARPS * 32, 0, st>>>(s->Hq, s->Hkv, s->d, scale_log2, pq, pk, pv, (__nv_bfloat16 *)o, parts,
+                                                                                      ctx->status_dev);
+    return str_launch_ok(ctx, 2);
 }
 
 }  // namespace
@@ -422,7 +526,15 @@ bool str_attn_packed_tc_supported(const str_attn_packed_shape *s, const void *q,
     return (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)o) & 15) == 0;
 }
 
+size_t str_attn_packed_tc_workspace(const str_attn_packed_shape *s) {
+    const int splits = splits_of(s);
+    if (splits == 1) return 0;
+    const size_t n = (size_t)blocks_of(s) * s->Hkv;
+    return align_up(n * splits * (2 * BQ * (padded(s->d) * sizeof(float) + sizeof(float2)) + sizeof(int)) + n * sizeof(PackedBlock), 256);
+}
+
 int str_attn_packed_tc(str_ctx *ctx, const str_attn_packed_shape *s, const void *q, const void *k, const void *v, const int32_t *q_start,
-                       const int32_t *k_start, float scale, void *o, cudaStream_t st) {
-    return s->d <= 64 ? launch<64>(ctx, s, q, k, v, q_start, k_start, scale, o, st) : launch<128>(ctx, s, q, k, v, q_start, k_start, scale, o, st);
+                       const int32_t *k_start, float scale, void *o, void *workspace, cudaStream_t st) {
+    return s->d <= 64 ? launch<64>(ctx, s, q, k, v, q_start, k_start, scale, o, workspace, st)
+                      : launch<128>(ctx, s, q, k, v, q_start, k_start, scale, o, workspace, st);
 }
