@@ -6,7 +6,9 @@
 //   states      The state starts from init_state; its bf16 copy is written before the first chunk, so Y_inter exists for every chunk.
 //   D skip      D_h is added to the diagonal of W: Y_intra = (W + D_h I) X.
 //   accuracy    The final state is an fp32 result.  Xs_j = exp(l_end - l_j) dt_j x_j is formed to 16 bits and enters the tensor pipe as two bf16
-//               pieces, Xs + Xs', relative error 2^-17 instead of 2^-8, and l_end - l_j as a sum from the end of the chunk, not as a difference.
+//               pieces, Xs + Xs', relative error 2^-16 instead of 2^-8, and l_end - l_j as a sum from the end of the chunk, not as a difference.
+//               A third piece brings it to 2^-24 in the last chunk and in those that the rest of the sequence fades by less than 2^-4; what
+//               lies further back is faded with its error.
 //               y is bf16 itself: W and the state's copy are narrowed once, relative error 2^-8 of each term at most, random in sign.
 //               Xs' has no buffer of its own: it takes the X slot of the chunk before, once that chunk's Y_intra is complete and until the
 //               chunk after next is loaded there.
@@ -39,14 +41,15 @@ constexpr int OFF_BARS = OFF_MASK + 2048;
 constexpr int D_LS = 0, D_NLC = 128, D_COLF = 256, D_XW = 384, D_ROWF = 640, D_EROW = 768, D_BLK = 896, D_EEND = 912;
 enum {
     B_XF = 0, B_BCF = 3, B_DECF = 5, B_DECE = 9, B_CBF = 13, B_WF = 15, B_XSF = 17, B_DSF = 19, B_DSE = 21,
-    B_SF, B_YF, B_YE, B_XLF, B_COUNT
+    B_SF, B_YF, B_YE, B_XLF, B_HIF, B_X3F, B_FINE, B_COUNT
 };
-constexpr size_t SMEM_BYTES = (size_t)OFF_BARS + B_COUNT * 8 + 32;
+constexpr size_t SMEM_BYTES = (size_t)OFF_BARS + B_COUNT * 8 + 40;
 constexpr int NUM_WARPS = 16, NUM_THREADS = NUM_WARPS * 32;
 constexpr int W_WARPS = 6;
 constexpr int DEC_READERS = W_WARPS + 4 + 4;              // warps that read a chunk's decay vectors
 constexpr uint32_t TM_CB = 0, TM_YO = 256, TM_YI = 384, TM_DS = 448;
 constexpr float LOG2E = 1.4426950408889634f;
+constexpr float FADED = 4.0f;                             // a chunk takes the third piece unless what is behind it fades it by this many powers of two
 
 // Sixteen fp32 values of a row as bf16: one 32-byte store where the row has room and its address allows it.
 __device__ __forceinline__ void store16(__nv_bfloat16 *to, const uint32_t *v, int room, bool wide) {
@@ -74,7 +77,8 @@ __device__ __forceinline__ void state_warps_sync() { asm volatile("barrier.sync 
 __device__ __forceinline__ uint64_t desc_add(uint64_t d, uint32_t bytes) { return d + (uint64_t)(bytes >> 4); }
 // Half (64 tokens) of Xs and Xs' of one chunk (same swizzled layout as the X tile), 128 threads, four 16-byte units each.  The factor comes as two
 // bf16 pieces, w = w1 + w2 to 2^-17; hi = bf16(w1 x), whose rounding error w1 x - hi is itself a bf16 number, and lo = bf16(w2 x + that error): hi + lo is
-// w x to 2^-16, in three packed instructions a pair.  lo stays in registers until its place is free.  Rows from `valid` on are another sequence's: zeroed, in the X tile too.
+// w x to 2^-16, in three packed instructions a pair.  lo stays in registers until its place is free.  A token's factor: w1 and w2 in the halves of one
+// word, w itself in the next.  Rows from `valid` on are another sequence's: zeroed, in the X tile too.
 __device__ __forceinline__ void split_x(uint8_t *x_tile, uint8_t *hi_tile, uint4 (&lo)[4], const float *dec_xw, int tid_g, int half, int valid) {
     uint4 v[4];
     uint2 w[4];
@@ -93,7 +97,8 @@ __device__ __forceinline__ void split_x(uint8_t *x_tile, uint8_t *hi_tile, uint4
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int u = tid_g + 128 * (4 * half + i);
-        const __nv_bfloat162 w1 = *reinterpret_cast<const __nv_bfloat162 *>(&w[i].x), w2 = *reinterpret_cast<const __nv_bfloat162 *>(&w[i].y);
+        const uint32_t w11 = __byte_perm(w[i].x, 0, 0x1010), w22 = __byte_perm(w[i].x, 0, 0x3232);
+        const __nv_bfloat162 w1 = *reinterpret_cast<const __nv_bfloat162 *>(&w11), w2 = *reinterpret_cast<const __nv_bfloat162 *>(&w22);
         __nv_bfloat162 *x = reinterpret_cast<__nv_bfloat162 *>(&v[i]);
         __nv_bfloat162 *l = reinterpret_cast<__nv_bfloat162 *>(&lo[i]);
 #pragma unroll
@@ -103,6 +108,27 @@ __device__ __forceinline__ void split_x(uint8_t *x_tile, uint8_t *hi_tile, uint4
             x[j] = h;
         }
         ((uint4 *)hi_tile)[u] = v[i];
+    }
+}
+
+// The third piece, bf16(w x - hi - lo) with the product in fp32, over hi once its product is through: w x to 2^-24.
+__device__ __forceinline__ void third_x(const uint8_t *x_tile, uint8_t *hi_tile, const float *dec_xw, int tid_g) {
+#pragma unroll 1
+    for (int i = 0; i < 8; ++i) {
+        const int u = tid_g + 128 * i;
+        const uint4 v = ((const uint4 *)x_tile)[u];
+        const uint2 w = ((const uint2 *)dec_xw)[u >> 3];
+        const uint32_t w11 = __byte_perm(w.x, 0, 0x1010), w22 = __byte_perm(w.x, 0, 0x3232);
+        const __nv_bfloat162 w1 = *reinterpret_cast<const __nv_bfloat162 *>(&w11), w2 = *reinterpret_cast<const __nv_bfloat162 *>(&w22);
+        const __nv_bfloat162 *x = reinterpret_cast<const __nv_bfloat162 *>(&v);
+        uint32_t r[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const __nv_bfloat162 h = __hmul2(x[j], w1), l = __hfma2(x[j], w2, __hfma2(x[j], w1, __hneg2(h)));
+            const float wf = __uint_as_float(w.y);
+            r[j] = tc::pack_bf16x2(fmaf(__low2float(x[j]), wf, -__low2float(h)) - __low2float(l), fmaf(__high2float(x[j]), wf, -__high2float(h)) - __high2float(l));
+        }
+        ((uint4 *)hi_tile)[u] = make_uint4(r[0], r[1], r[2], r[3]);
     }
 }
 
@@ -195,6 +221,7 @@ scan_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_c
     uint32_t *tmem_slot = (uint32_t *)(bars + B_COUNT);
     volatile int *abort_flag = (volatile int *)(tmem_slot + 1);       // [2]
     volatile int *found = abort_flag + 2;                             // the state is not finite
+    volatile int *fine_from = (volatile int *)(tmem_slot + 5);        // the chunks from here on take the third piece
 
     // Role numbers (the `warp` used below) are decoupled from hardware warp numbers: when several warps of a
     // scheduler are ready it favours the lower-numbered one, so the MMA issuer and the decay warp, which need
@@ -230,6 +257,7 @@ scan_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_c
         for (int i = 0; i < DEC_DEPTH; ++i) { tc::mbar_init(bars + B_DECF + i, 1); tc::mbar_init(bars + B_DECE + i, DEC_READERS); }
         tc::mbar_init(bars + B_XSF, 4); tc::mbar_init(bars + B_XSF + 1, 4); tc::mbar_init(bars + B_DSF, 1); tc::mbar_init(bars + B_DSF + 1, 1); tc::mbar_init(bars + B_DSE, 4);
         tc::mbar_init(bars + B_SF, 4); tc::mbar_init(bars + B_YF, 1); tc::mbar_init(bars + B_YE, 4); tc::mbar_init(bars + B_XLF, 4);
+        tc::mbar_init(bars + B_HIF, 1); tc::mbar_init(bars + B_X3F, 4); tc::mbar_init(bars + B_FINE, 1);
         abort_flag[0] = 0; abort_flag[1] = 0; found[0] = 0;
         tc::fence_mbar_init();
         tc::prefetch_tmap(&tmap_x); tc::prefetch_tmap(&tmap_b); tc::prefetch_tmap(&tmap_c);
@@ -322,9 +350,9 @@ scan_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_c
                 o_nlc[i] = tc::lg2(dv[i]) - li;          // exp2(l_t + nlc_j) = exp(l_t - l_j) dt_j; a padded token (dt = 0) gives -inf
                 o_colf[i] = tc::ex2(l_endb - li) * dv[i];
                 const float xw = tc::ex2(behind + tail[i]) * dv[i];
-                o_xw[2 * i] = tc::pack_bf16x2(xw, xw);
-                const float rest = xw - __uint_as_float(o_xw[2 * i] & 0xFFFF0000u);
-                o_xw[2 * i + 1] = tc::pack_bf16x2(rest, rest);
+                const float w1 = __bfloat162float(__float2bfloat16_rn(xw));
+                o_xw[2 * i] = tc::pack_bf16x2(xw, xw - w1);
+                o_xw[2 * i + 1] = __float_as_uint(xw);
                 o_rowf[i] = tc::ex2(li - l_start);
                 o_erow[i] = tc::ex2(li);
             }
@@ -368,7 +396,9 @@ scan_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_c
             const uint64_t dm_xs = tc::make_smem_desc(sbase + OFF_XS, TILE_16K, 1024, tc::SWZ_128B);
             const uint64_t dm_sb = tc::make_smem_desc(sbase + OFF_SB, TILE_16K, 1024, tc::SWZ_128B);
             const uint64_t dm_x0 = tc::make_smem_desc(sbase + OFF_X, TILE_16K, 1024, tc::SWZ_128B);
-            bool ok = true;
+            bool ok = tc::mbar_wait(bars + B_FINE, 0, abort_flag);
+            const int fine_c = ok ? fine_from[0] : 0;
+            int n_fine = 0;
 #pragma unroll 1
             for (int c = 0; c <= nchunks && ok; ++c) {
                 const int s = c & 1;
@@ -400,7 +430,7 @@ scan_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_c
                         // Y_inter_c = C S_{c-1}^T
                         tc::mma8_ss<tc::StepKMajor2x64, tc::StepMNMajor>(tmem + TM_YO + (uint32_t)s * 64, dk_c, dm_sb, id_kn, false);
                     }
-                    // dS_c^T = B^T Xs, half of the tokens after the other, + B^T Xs'
+                    // dS_c^T = B^T Xs, half of the tokens after the other, + B^T Xs' (+ the third piece)
                     const uint64_t dm_b = desc_add(dm_b0, (uint32_t)s * 2 * TILE_16K);
                     const uint64_t dm_lo = desc_add(dm_x0, (uint32_t)((c + X_SLOTS - 1) % X_SLOTS) * TILE_16K);
                     ok = tc::mbar_wait(bars + B_XSF, c & 1, abort_flag) && (c == 0 || tc::mbar_wait(bars + B_DSE, (c - 1) & 1, abort_flag));
@@ -411,10 +441,18 @@ scan_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_c
                     if (!ok) break;
                     tc::tc_fence_after();
                     tc::mma4_ss<tc::StepMNMajor, tc::StepMNMajor>(tmem + TM_DS, desc_add(dm_b, 8192), desc_add(dm_xs, 8192), id_nn, true);
+                    if (c >= fine_c) tc::mma_commit(bars + B_HIF);
                     ok = tc::mbar_wait(bars + B_XLF, c & 1, abort_flag);
                     if (!ok) break;
                     tc::tc_fence_after();
                     tc::mma8_ss<tc::StepMNMajor, tc::StepMNMajor>(tmem + TM_DS, dm_b, dm_lo, id_nn, true);
+                    if (c >= fine_c) {
+                        ok = tc::mbar_wait(bars + B_X3F, n_fine & 1, abort_flag);
+                        if (!ok) break;
+                        ++n_fine;
+                        tc::tc_fence_after();
+                        tc::mma8_ss<tc::StepMNMajor, tc::StepMNMajor>(tmem + TM_DS, dm_b, dm_xs, id_nn, true);
+                    }
                     tc::mma_commit(bars + B_DSF + s);
                 }
             }
@@ -447,22 +485,21 @@ scan_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_c
             if (!tc::mbar_wait(bars + B_CBF + s, (c >> 1) & 1, abort_flag)) { ok = false; break; }
             tc::tc_fence_after();
             const uint32_t tW = tmem + lane_base + TM_CB + (uint32_t)(s * 128);
-            // every piece is fetched before any is worked on: a tensor-memory load takes a few hundred clocks to
-            // return while the tensor pipe is busy
-            uint32_t v[5][16];
-#pragma unroll
-            for (int k = 0; k < 5; ++k)
-                if (k < n_real) tc::tmem_ld16(tW + (uint32_t)(first + 16 * k), v[k]);
+            // the next piece is on its way while one is worked on
+            uint32_t va[16], vb[16];
+            tc::tmem_ld16(tW + (uint32_t)first, va);
             tc::tmem_ld_wait();
+#pragma unroll 1
+            for (int k = 0; k < n_real; ++k) {
+                const int col0 = first + 16 * k, bj = col0 >> 5;
+                if (k + 1 < n_real) tc::tmem_ld16(tW + (uint32_t)(col0 + 16), vb);
+                uint32_t packed[8];
+                if (bj == quad) w_piece_diag(va, packed, dec, (const uint4 *)(smem + OFF_MASK), col0, lane, l_t, skip2);
+                else w_piece_below(va, packed, dec, col0, rf * dec[D_BLK + quad * 4 + bj]);
+                tc::tmem_st8(tW + (uint32_t)col0, packed);
+                tc::tmem_ld_wait();
 #pragma unroll
-            for (int k = 0; k < 5; ++k) {
-                if (k < n_real) {
-                    const int col0 = first + 16 * k, bj = col0 >> 5;
-                    uint32_t packed[8];
-                    if (bj == quad) w_piece_diag(v[k], packed, dec, (const uint4 *)(smem + OFF_MASK), col0, lane, l_t, skip2);
-                    else w_piece_below(v[k], packed, dec, col0, rf * dec[D_BLK + quad * 4 + bj]);
-                    tc::tmem_st8(tW + (uint32_t)col0, packed);
-                }
+                for (int i = 0; i < 16; ++i) va[i] = vb[i];
             }
             if (n_zero > 0) {
                 uint32_t zero[8];
@@ -531,12 +568,13 @@ scan_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_c
 #pragma unroll
                 for (int i = 0; i < 8; ++i) lo_tile[128 * i] = lo[i >> 2][i & 3];
                 tc::fence_proxy_async();
+                // (inputs of the next chunk: waited for before dS, not behind it)
+                if (c + 1 < nchunks && !inputs_there(c + 1)) { ok = false; break; }
                 warp_arrive(bars + B_XLF, lane);
             }
             const float eend = dec[D_EEND];
             __syncwarp();
             if (lane == 0) tc::mbar_arrive(bars + B_DECE + d);
-            if (c + 1 < nchunks && !inputs_there(c + 1)) { ok = false; break; }       // waited for before dS, not behind it
             if (!tc::mbar_wait(bars + B_DSF + (c & 1), (c >> 1) & 1, abort_flag)) { ok = false; break; }
             tc::tc_fence_after();
 #pragma unroll
@@ -580,53 +618,83 @@ scan_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_c
         __nv_bfloat16 *yb = y + ((size_t)row0 * H + h) * p;
         const bool wide = p % 16 == 0 && ((uintptr_t)y & 31) == 0;
         bool ok = true;
+        if (warp == 8) {
+            // While there is nothing to write yet: how far from the end a chunk has faded enough, four chunks' dt at a time.
+            const float *dtb = dt + (size_t)row0 * H + h;
+            const float rate = -A[h] * LOG2E;
+            float faded = 0.f;
+            int from = nchunks - 1, k = nchunks - 1;
 #pragma unroll 1
-        for (int cp = 0; cp < nchunks; ++cp) {
+            while (k > 0 && faded < FADED) {
+                float sum[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    sum[j] = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int t = (k - j) * Q + 32 * i + lane;
+                        if (k - j > 0 && t < Tlen) sum[j] += __ldg(dtb + (size_t)t * H);
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float s = warp_sum(sum[j]) * rate;
+                    if (k - j > 0 && faded < FADED) {
+                        faded += s;
+                        if (faded < FADED) from = k - j - 1;
+                    }
+                }
+                k -= 4;
+            }
+            if (lane == 0) {
+                fine_from[0] = from;
+                tc::mbar_arrive(bars + B_FINE);
+            }
+            __syncwarp();
+        }
+        ok = tc::mbar_wait(bars + B_FINE, 0, abort_flag);
+        const int fine_c = fine_from[0];
+#pragma unroll 1
+        for (int cp = 0; cp < nchunks && ok; ++cp) {
             {
                 const int d = cp & (DEC_DEPTH - 1), t0 = cp * Q;
                 if (!tc::mbar_wait(bars + B_DECF + d, (cp >> 2) & 1, abort_flag)) { ok = false; break; }
                 const float er = decs[d * DEC_FLOATS + D_EROW + row];
+                if (cp >= fine_c) {                   // the third piece, once the product with the first is through
+                    if (!tc::mbar_wait(bars + B_HIF, (cp - fine_c) & 1, abort_flag)) { ok = false; break; }
+                    third_x(smem + OFF_X + cp % X_SLOTS * TILE_16K, smem + OFF_XS, decs + d * DEC_FLOATS + D_XW, row);
+                    tc::fence_proxy_async();
+                    warp_arrive(bars + B_X3F, lane);
+                }
                 __syncwarp();
                 if (lane == 0) tc::mbar_arrive(bars + B_DECE + d);
                 if (!tc::mbar_wait(bars + B_YF, cp & 1, abort_flag)) { ok = false; break; }
                 tc::tc_fence_after();
                 __nv_bfloat16 *dst = yb + (size_t)(t0 + row) * H * p;
                 const bool valid = t0 + row < Tlen;
-                uint32_t ya[32], yb2[32], yo[32];
-                tc::tmem_ld32(tmem + lane_base + TM_YI, ya);
-                if (cp > 0 || init) tc::tmem_ld32(tmem + lane_base + TM_YO + (uint32_t)((cp & 1) * 64), yo);
-                tc::tmem_ld_wait();
-                if (cp > 0 || init) {
-#pragma unroll
-                    for (int i = 0; i < 32; i += 2) {
-                        const float2 r = __ffma2_rn(make_float2(er, er), make_float2(__uint_as_float(yo[i]), __uint_as_float(yo[i + 1])),
-                                                    make_float2(__uint_as_float(ya[i]), __uint_as_float(ya[i + 1])));
-                        ya[i] = __float_as_uint(r.x);
-                        ya[i + 1] = __float_as_uint(r.y);
+#pragma unroll 1
+                for (int hf = 0; hf < 2; ++hf) {
+                    uint32_t ya[32], yo[32];
+                    tc::tmem_ld32(tmem + lane_base + TM_YI + (uint32_t)(hf * 32), ya);
+                    if (cp > 0 || init) tc::tmem_ld32(tmem + lane_base + TM_YO + (uint32_t)((cp & 1) * 64 + hf * 32), yo);
+                    tc::tmem_ld_wait();
+                    if (hf == 1) {                    // both accumulators are in registers
+                        tc::tc_fence_before();
+                        warp_arrive(bars + B_YE, lane);
                     }
-                }
-                // second half in flight while the first is narrowed and stored
-                tc::tmem_ld32(tmem + lane_base + TM_YI + 32, yb2);
-                if (cp > 0 || init) tc::tmem_ld32(tmem + lane_base + TM_YO + (uint32_t)((cp & 1) * 64 + 32), yo);
-                if (valid) {
-                    store16(dst, ya, p, wide);
-                    store16(dst + 16, ya + 16, p - 16, wide);
-                }
-                tc::tmem_ld_wait();
-                tc::tc_fence_before();               // both accumulators are in registers
-                warp_arrive(bars + B_YE, lane);
-                if (cp > 0 || init) {
+                    if (cp > 0 || init) {
 #pragma unroll
-                    for (int i = 0; i < 32; i += 2) {
-                        const float2 r = __ffma2_rn(make_float2(er, er), make_float2(__uint_as_float(yo[i]), __uint_as_float(yo[i + 1])),
-                                                    make_float2(__uint_as_float(yb2[i]), __uint_as_float(yb2[i + 1])));
-                        yb2[i] = __float_as_uint(r.x);
-                        yb2[i + 1] = __float_as_uint(r.y);
+                        for (int i = 0; i < 32; i += 2) {
+                            const float2 r = __ffma2_rn(make_float2(er, er), make_float2(__uint_as_float(yo[i]), __uint_as_float(yo[i + 1])),
+                                                        make_float2(__uint_as_float(ya[i]), __uint_as_float(ya[i + 1])));
+                            ya[i] = __float_as_uint(r.x);
+                            ya[i + 1] = __float_as_uint(r.y);
+                        }
                     }
-                }
-                if (valid) {
-                    store16(dst + 32, yb2, p - 32, wide);
-                    store16(dst + 48, yb2 + 16, p - 48, wide);
+                    if (valid) {
+                        store16(dst + 32 * hf, ya, p - 32 * hf, wide);
+                        store16(dst + 32 * hf + 16, ya + 16, p - 32 * hf - 16, wide);
+                    }
                 }
             }
         }
