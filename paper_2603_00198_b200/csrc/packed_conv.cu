@@ -353,6 +353,9 @@ void dispatch_vec(const ConvCall &k, int W, bool step, cudaStream_t st) {
     else dispatch_width<T, 1>(k, W, step, st);
 }
 
+// Blocks of columns, the dt columns' included, at one channel a thread (vector accesses need fewer).
+long long column_blocks(const ConvDims &c) { return (c.ch + THREADS - 1) / THREADS + 1; }
+
 int check_dims(int dtype, int H, int p, int n, int G, int W, ConvDims *c) {
     if (H <= 0 || p <= 0 || n <= 0 || G <= 0 || H % G != 0 || W <= 0 || !STR_DTYPE_OK(dtype)) return STR_ERR_INVALID_ARG;
     const long long d_inner = (long long)H * p, gn = (long long)G * n, ld = 2 * d_inner + 2 * gn + H;
@@ -371,7 +374,7 @@ extern "C" int str_mamba_conv_packed(str_ctx *ctx, int dtype, int n_seq, int row
     if (rows > 0 && (!zxbcdt || !x_out || !B_out || !C_out || !dt_out)) return STR_ERR_INVALID_ARG;
     const int rc = check_dims(dtype, H, p, n, G, W, &c);
     if (rc != STR_OK) return rc;
-    if (n_seq > 65535 || rows > (1 << 30)) return STR_ERR_UNSUPPORTED_SHAPE;
+    if (n_seq > 65535 || rows > (1 << 30) || (rows / 8 + 1LL + n_seq) * column_blocks(c) > INT32_MAX) return STR_ERR_UNSUPPORTED_SHAPE;
     const size_t es = dtype_size(dtype), wb = (size_t)n_seq * (W - 1) * c.ch * es;
     if (kv4_overlap(window, wb, window_out, wb)) return STR_ERR_INVALID_ARG;
     StrDeviceScope dev(ctx);
@@ -391,7 +394,7 @@ extern "C" int str_mamba_conv_step(str_ctx *ctx, int dtype, int Bz, int T, int H
         return STR_ERR_INVALID_ARG;
     const int rc = check_dims(dtype, H, p, n, G, W, &c);
     if (rc != STR_OK) return rc;
-    if ((long long)Bz * T > (1 << 30)) return STR_ERR_UNSUPPORTED_SHAPE;
+    if ((long long)Bz * T > (1 << 30) || column_blocks(c) > 65535) return STR_ERR_UNSUPPORTED_SHAPE;
     const size_t es = dtype_size(dtype), wb = (size_t)Bz * (W - 1) * c.ch * es;
     if (window != window_out && kv4_overlap(window, wb, window_out, wb)) return STR_ERR_INVALID_ARG;
     StrDeviceScope dev(ctx);

@@ -266,6 +266,45 @@ def test_scan_in_two_turns_continues_the_first(ctx):
     c.check((whole, fs))
 
 
+def test_final_states_of_sequences_whose_last_tokens_count(ctx):
+    """Decays so fast that a state is its last few tokens: every term of it is a product of three bf16 pieces at most 2^-24 off, added up in 24 steps
+    of the matrix instruction that may each lose 2^-24 of the sum: 2^-19 of the sum of absolute terms (the factor's two largest pieces alone would be
+    2^-16 off)."""
+    g = np.random.default_rng(14)
+    for lens in ([300, 129, 20], [64]):
+        c = Scan(g, lens, "bf16", 4, 64, 128, 2, False, True)
+        c.A[:] = -1.0e4
+        _, S = c.run(ctx)
+        _, _, want, mag = packed.scan(c.x, c.dt, c.A, c.B, c.C, None, c.starts, c.state)
+        assert (np.abs(_f64(S) - want) <= 2.0 ** -19 * mag + 1e-30).all()
+
+
+def test_scan_of_short_and_long_sequences_side_by_side(ctx):
+    """Averages on both sides of the length from which the chunked kernel is taken, with and without decay to fade a chunk."""
+    g = np.random.default_rng(15)
+    for lens in ([16, 16], [17, 16], [1, 40, 2], [500, 0, 1, 3, 2]):
+        for decay in (1e-3, 16.0):
+            c = Scan(g, lens, "bf16", 3, 64, 128, 1, True, True, decay=max(decay, 1.0))
+            if decay < 1:
+                c.A[:] = -decay
+            c.check(c.run(ctx))
+
+
+def test_scan_before_a_value_that_is_not_finite(ctx):
+    """Tokens before it are as they would be without it; its own and later ones of its column are not finite."""
+    g = np.random.default_rng(16)
+    for value in (np.nan, np.inf):
+        c = Scan(g, [200], "bf16", 2, 64, 128, 1, True, True)
+        clean = _f64(c.run(ctx)[0])
+        c.x[150, 1, 7] = value
+        y, S = (_f64(t) for t in c.run(ctx))
+        ref, ymag, _, _ = packed.scan(c.x[:150], c.dt[:150], c.A, c.B[:150], c.C[:150], c.D, [0, 150], c.state)
+        rel = 2 * HALF["bf16"] + 2.0 ** -12 + 264 * 2.0 ** -21
+        assert (np.abs(y[:150] - ref) <= rel * ymag + HALF["bf16"] * np.abs(ref)).all()
+        assert not np.isfinite(y[150:, 1, 7]).any() and np.isfinite(np.delete(y[:, 1], 7, 1)).all() and (y[:, 0] == clean[:, 0]).all()
+        assert not np.isfinite(S[0, 1, 7]).any() and np.isfinite(np.delete(S[0, 1], 7, 0)).all()
+
+
 def test_scan_does_not_carry_what_is_not_finite_into_other_sequences(ctx):
     g = np.random.default_rng(13)
     for dims in ((4, 64, 128, 2), (2, 80, 20, 2)):
@@ -380,6 +419,78 @@ def test_attention_hidden_keys_that_are_not_finite_do_not_reach_the_queries_befo
         if where == "k" and np.isnan(value):
             assert touched.isnan().all()
         setattr(c, where, old)
+
+
+def _shared(c):
+    """Does the call share a block's keys out to several CTAs (it then asks for a workspace)?"""
+    s = binding.AttnPackedShape(len(c.qs) - 1, len(c.q), len(c.k), c.q.shape[1], c.k.shape[1], c.d, 1)
+    import ctypes
+    return binding.lib().str_attn_prefill_packed_workspace_size(ctypes.addressof(s)) > 0
+
+
+@pytest.mark.parametrize("Hq, Hkv, d", [(4, 1, 128), (3, 1, 64), (2, 2, 80), (16, 1, 128)])
+@pytest.mark.parametrize("lq, lk", [([3], [2100]), ([40, 1], [1500, 2600]), ([70, 0, 5], [3000, 1200, 2]), ([300], [1100]), ([9, 9], [4000, 6])], ids=str)
+def test_attention_whose_keys_are_shared_out(ctx, Hq, Hkv, d, lq, lk):
+    """Few queries over many keys: shares that some or all rows of a block see nothing of, sequences with fewer keys than queries or than shares."""
+    g = np.random.default_rng([Hq, d, sum(lk)])
+    c = Attend(g, lq, lk, "bf16", Hq, Hkv, d, (2, 3), 5, gain=2.0)
+    assert _shared(c) or Hq == 16
+    c.check(c.run(ctx))
+
+
+def test_attention_shared_out_with_values_that_are_not_finite(ctx):
+    g = np.random.default_rng(26)
+    c = Attend(g, [20, 4], [2000, 1500], "bf16", 4, 1, 128)
+    assert _shared(c)
+    clean = c.run(ctx)
+    for where, value, at, seen_by in (("v", np.nan, 1990, range(10, 20)), ("v", np.inf, 100, range(20)), ("k", np.nan, 1985, range(5, 20)), ("v", np.nan, 3499, range(23, 24))):
+        old = getattr(c, where).copy()
+        getattr(c, where)[at, 0, 5] = value
+        o = c.run(ctx)
+        hit = torch.zeros(24, dtype=torch.bool)
+        hit[list(seen_by)] = True
+        assert ((o.double() - clean.double()).abs() <= 2 * HALF["bf16"] * clean.double().abs() + 2.0 ** -8)[~hit].all(), (where, at)
+        assert (~torch.isfinite(o[hit].double())).any(-1).all()
+        setattr(c, where, old)
+    c.q[3, 2, 0] = np.inf
+    assert c.run(ctx)[3, 2].isnan().all()
+
+
+def test_attention_shared_out_in_two_graphs_at_once_and_the_same_bits(ctx):
+    g = np.random.default_rng(27)
+    c = Attend(g, [30], [3000], "bf16", 8, 2, 128)
+    assert _shared(c)
+    q, k, v = (dev(a, "bf16") for a in (c.q, c.k, c.v))
+    other = [t.flip(0).contiguous() for t in (q, k, v)]
+    qs, ks = _i32(c.qs), _i32(c.ks)
+    call = lambda t: binding.str_attn_prefill_packed(ctx, *t, qs, c.scale, k_start=ks)  # noqa: E731
+    want = [call((q, k, v)).clone(), call(other).clone()]
+    graphs, streams = [], [torch.cuda.Stream(), torch.cuda.Stream()]
+    for t in ((q, k, v), other):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = call(t)
+        graphs.append((graph, out))
+    for _ in range(5):
+        for (graph, _), st in zip(graphs, streams):
+            with torch.cuda.stream(st):
+                graph.replay()
+    torch.cuda.synchronize()
+    for (_, out), w in zip(graphs, want):
+        assert torch.equal(out, w)
+
+
+@pytest.mark.parametrize("starts", [[0, 30, 10], [-3, 10, 4000], [40, 40, -2147483648]], ids=str)
+def test_wrong_starts_with_keys_shared_out(ctx, starts):
+    g = np.random.default_rng(28)
+    c = Attend(g, [20, 20], [1500, 1500], "bf16", 4, 1, 128)
+    assert _shared(c)
+    q, k, v = (dev(a, "bf16") for a in (c.q, c.k, c.v))
+    for qs, ks in ((starts, c.ks), (c.qs, starts)):
+        binding.str_attn_prefill_packed(ctx, q, k, v, _i32(qs), 0.1, k_start=_i32(ks))
+        with pytest.raises(binding.StrError):
+            ctx.check_status()
+    c.check(c.run(ctx))
 
 
 def test_attention_rows_that_are_not_finite_stay_by_themselves(ctx):

@@ -111,6 +111,24 @@ def test_attention():
 
 
 @no_device
+def test_attention_workspace():
+    """Few queries over many keys ask for one; too small, missing, misaligned or shared with the output it is refused."""
+    def call(ws, given, o=1 << 45):
+        c = Call()
+        s = binding.AttnPackedShape(1, 10, 5000, 4, 2, 64, 1)
+        need = binding.lib().str_attn_prefill_packed_workspace_size(ctypes.addressof(s))
+        assert need > 0
+        return binding.lib().str_attn_prefill_packed(ctypes.addressof(c.ctx), ctypes.addressof(s), *(c.buffer() for _ in range(5)), 0.1, o, ws, need + given, None)
+
+    at = 1 << 44
+    assert call(at, 0) == NO_DEVICE and call(at, -1) == -3 and call(None, 0) == INVALID and call(at + 128, 0) == INVALID and call(1 << 45, 0) == INVALID
+    for shape in ((1, 10, 5000, 4, 2, 64, 0), (1, 5000, 5000, 4, 2, 64, 1), (1, 10, 900, 4, 2, 64, 1), (1, 10, 5000, 4, 2, 63, 1), (0, 10, 5000, 4, 2, 64, 1), (1, 0, 0, 4, 2, 64, 1)):
+        s = binding.AttnPackedShape(*shape)
+        assert binding.lib().str_attn_prefill_packed_workspace_size(ctypes.addressof(s)) == 0, shape
+    assert binding.lib().str_attn_prefill_packed_workspace_size(None) == 0
+
+
+@no_device
 def test_rotary():
     assert Call().rope() == NO_DEVICE
     for bad in (dict(rot_dim=0), dict(rot_dim=33), dict(rot_dim=66), dict(layout=2), dict(scaling=3), dict(theta=0.0), dict(theta=float("nan")), dict(amplitude=float("inf")),
