@@ -554,6 +554,41 @@ def micro_case(ctx, pk, name, Bz=1, n_vis=32768, final_bp=5000, attn_denominator
         fn = lambda: binding.str_mamba2_step(ctx, x, dt, A, Bm, Cm, state)
         flops = 5.0 * Bz * H * p * n
         nbytes = 8.0 * Bz * H * p * n
+    elif name in ("conv_packed", "scan_packed", "attn_packed", "rope_ex"):
+        # T rows of Bz packed sequences, sequence s twice as long as the one before it; the Mamba operators continue an earlier turn
+        cuts = [int(round(T * (2.0 ** i - 1) / (2.0 ** Bz - 1))) for i in range(Bz + 1)]
+        start = torch.tensor(cuts, dtype=torch.int32, device=dev)
+        lens = np.diff(cuts).astype(np.float64)
+        H, p, n, G, W = ms_["H"], ms_["p"], ms_["n"], ms_["G"], ms_["conv"]
+        Hq, Hkv, d = at_["Hq"], at_["Hkv"], at_["d"]
+        ch = H * p + 2 * G * n
+        if name == "conv_packed":
+            zx = torch.randn(T, 2 * H * p + 2 * G * n + H, device=dev).to(bf)
+            cw, cb, bias = torch.randn(ch, W, device=dev) * 0.5, torch.randn(ch, device=dev) * 0.1, torch.randn(H, device=dev) - 4.0
+            window = torch.randn(Bz, W - 1, ch, device=dev).to(bf)
+            wout = torch.empty_like(window)
+            fn = lambda: binding.str_mamba_conv_packed(ctx, zx, cw, cb, bias, start, H, p, n, G, window=window, window_out=wout)
+            nbytes = T * (4.0 * ch + 6.0 * H) + 4.0 * Bz * (W - 1) * ch
+        elif name == "scan_packed":
+            x, Bm, Cm = (torch.randn(T, a, b, device=dev).to(bf) for a, b in ((H, p), (G, n), (G, n)))
+            dt = torch.empty(T, H, device=dev).uniform_(1e-3, 1e-1)
+            A = -torch.exp(torch.empty(H, device=dev).uniform_(0.0, float(np.log(16.0))))
+            state = torch.randn(Bz, H, p, n, device=dev)
+            sout = torch.empty_like(state)
+            fn = lambda: binding.str_mamba2_prefill_packed(ctx, x, dt, A, Bm, Cm, start, init_state=state, final_state=sout)
+            nbytes = T * (2.0 * (2 * H * p + 2 * G * n) + 4 * H) + 8.0 * Bz * H * p * n
+        elif name == "attn_packed":
+            q, k, v = (torch.randn(T, h, d, device=dev).to(bf) for h in (Hq, Hkv, Hkv))
+            fn = lambda: binding.str_attn_prefill_packed(ctx, q, k, v, start, d ** -0.5)
+            flops = float(np.sum(lens * (lens + 1) / 2)) * 4.0 * Hq * d
+            nbytes = T * 2.0 * (2 * Hq * d + 2 * Hkv * d)
+            bound = "tensor"
+        else:
+            qkv = torch.randn(T, (Hq + 2 * Hkv) * d, device=dev).to(bf)
+            pos = torch.arange(T, dtype=torch.int32, device=dev)
+            rope = binding.Rope(at_["theta"], d, scaling="banded", factor=8.0, trained_len=32768)
+            fn = lambda: binding.str_rope_split_ex(ctx, rope, qkv, pos, Hq, Hkv, d)
+            nbytes = T * (4.0 * (Hq + 2 * Hkv) * d + 4)
     else:
         raise SystemExit("unknown --micro " + name)
     flush = torch.empty(256 << 20, dtype=torch.uint8, device=dev)
@@ -625,7 +660,8 @@ def main():
     ap.add_argument("--graph", action="store_true", help="also time the step replayed from a CUDA graph")
     ap.add_argument("--no-kernels-alone", action="store_true", help="skip the per-kernel timings after the headline run")
     ap.add_argument("--micro", default="", help="time one kernel alone: ssd | mamba_score | mamba_dyn_score | attn_score | attn_fwd | "
-                                                "topk | compact | gemm | kv4_append | kv4_attn | kv4_evict | mamba_step")
+                                                "topk | compact | gemm | kv4_append | kv4_attn | kv4_evict | mamba_step | "
+                                                "conv_packed | scan_packed | attn_packed | rope_ex")
     args = ap.parse_args()
     if args.warmup < 3 and args.impl == "ours":
         args.warmup = 3

@@ -56,14 +56,16 @@ __device__ __forceinline__ int packed_blocks_of_cost(const PackedAttnSeq &q, int
     const long long below = (long long)(tiles - 1) * key_tile;
     if (q.lk <= below) return 0;
     const long long y = below - q.lk + q.lq;             // the last query of a block has to be number y or later
-    return y <= 0 ? n : n - (int)(y / block);
+    return y <= 0 ? n : n - (int)y / block;              // y < lq
 }
 __device__ __forceinline__ PackedBlock packed_block(const int32_t *q_start, const int32_t *k_start, int n_seq, int rows_q, int rows_k, int block,
                                                     int key_tile, int r) {
     const int lane = threadIdx.x & 31;
+    // the lane's first sequence stays in registers: most calls have no more than 32
+    const PackedAttnSeq own = lane < n_seq ? packed_attn_seq(q_start, k_start, lane, rows_q, rows_k) : PackedAttnSeq{};
     auto blocks = [&](int tiles) {
-        int n = 0;
-        for (int s = lane; s < n_seq; s += 32) n += packed_blocks_of_cost(packed_attn_seq(q_start, k_start, s, rows_q, rows_k), block, key_tile, tiles);
+        int n = packed_blocks_of_cost(own, block, key_tile, tiles);
+        for (int s = lane + 32; s < n_seq; s += 32) n += packed_blocks_of_cost(packed_attn_seq(q_start, k_start, s, rows_q, rows_k), block, key_tile, tiles);
         return (int)__reduce_add_sync(0xffffffffu, (unsigned)n);
     };
     PackedBlock b = {};
@@ -79,7 +81,7 @@ __device__ __forceinline__ PackedBlock packed_block(const int32_t *q_start, cons
         PackedAttnSeq q = {};
         int from = 0, n = 0;
         if (s0 + lane < n_seq) {
-            q = packed_attn_seq(q_start, k_start, s0 + lane, rows_q, rows_k);
+            q = s0 == 0 ? own : packed_attn_seq(q_start, k_start, s0 + lane, rows_q, rows_k);
             const int all = (q.lq + block - 1) / block, more = packed_blocks_of_cost(q, block, key_tile, lo + 1);
             n = packed_blocks_of_cost(q, block, key_tile, lo) - more;
             from = all - more - n;

@@ -12,17 +12,19 @@
 
 namespace {
 
-constexpr int LPR = 4, TB = 16, MAX_THREADS = 256;        // lanes per row, tokens per turn
+constexpr int LPR = 4;                                    // lanes per row
+// Tokens per turn: as many as their b, c and outputs leave registers for.
+template <int NV> constexpr int TOKENS = NV <= 4 ? 32 : 16;
 
-template <typename T, int NV>
-__global__ void __launch_bounds__(MAX_THREADS)
+template <typename T, int NV, int WARPS>
+__global__ void __launch_bounds__(32 * WARPS)
 scan_packed_kernel(int n_seq, int rows, int H, int p, int n, int G, const T *__restrict__ x, const float *__restrict__ dt, const float *__restrict__ A,
                    const T *__restrict__ B, const T *__restrict__ C, const float *__restrict__ Dskip, const int32_t *__restrict__ start,
                    const float *state, T *__restrict__ y, float *final_state, int *status) {
-    constexpr int NP = NV * 4 * LPR;                      // columns, padded
+    constexpr int NP = NV * 4 * LPR, TB = TOKENS<NV>;     // columns, padded; tokens per turn
+    constexpr int threads = 32 * WARPS, R = threads / LPR; // rows of the state per block
     extern __shared__ float4 smem4[];
     float *bs = (float *)smem4, *cs = bs + TB * NP, *xs = cs + TB * NP;
-    const int threads = blockDim.x, R = threads / LPR;    // rows of the state per block
     float *ys = xs + TB * R, *dts = ys + TB * R * LPR, *decay = dts + TB;
     const int h = blockIdx.y, s = blockIdx.z, g = h / (H / G);
     const int tid = threadIdx.x, i0 = blockIdx.x * R, r = tid / LPR, l = tid % LPR;
@@ -47,20 +49,18 @@ scan_packed_kernel(int n_seq, int rows, int H, int p, int n, int G, const T *__r
         }
     }
     const float Ah = A[h], Dh = Dskip ? Dskip[h] : 0.f;
-    // What the thread carries of the next TB tokens: element e = tid + k threads of [TB][NP] and of [TB][R].  A block has at least 2 NP threads' worth of rows
-    // or takes more elements a thread: at most BC of b and c, and TB / LPR of x.
-    constexpr int BC = TB * NP / 32 < 16 ? TB * NP / 32 : 16;
-    T bq[BC], cq[BC], xq[TB / LPR];
+    // What the thread carries of the next TB tokens: elements tid + k threads of [TB][NP] and of [TB][R].
+    constexpr int PER = TB * NP / threads;
+    T bq[PER], cq[PER], xq[TB / LPR];
     float dq = 0.f;
-    const int per = (TB * NP + threads - 1) / threads;
     auto fetch = [&](int tb) {
         const int m = min(TB, t1 - tb);
 #pragma unroll
-        for (int k = 0; k < BC; ++k) {
+        for (int k = 0; k < PER; ++k) {
             const int e = tid + k * threads, t = e / NP, col = e % NP;
             stf(&bq[k], 0.f);
             stf(&cq[k], 0.f);
-            if (k < per && t < m && col < n) {
+            if (t < m && col < n) {
                 const size_t at = ((size_t)(tb + t) * G + g) * n + col;
                 bq[k] = B[at];
                 cq[k] = C[at];
@@ -78,11 +78,10 @@ scan_packed_kernel(int n_seq, int rows, int H, int p, int n, int G, const T *__r
     for (int tb = t0; tb < t1; tb += TB) {
         const int m = min(TB, t1 - tb);
 #pragma unroll
-        for (int k = 0; k < BC; ++k)
-            if (k < per && tid + k * threads < TB * NP) {
-                bs[tid + k * threads] = ldf(&bq[k]);
-                cs[tid + k * threads] = ldf(&cq[k]);
-            }
+        for (int k = 0; k < PER; ++k) {
+            bs[tid + k * threads] = ldf(&bq[k]);
+            cs[tid + k * threads] = ldf(&cq[k]);
+        }
 #pragma unroll
         for (int k = 0; k < TB / LPR; ++k) xs[tid + k * threads] = ldf(&xq[k]);
         if (tid < m) {
@@ -125,24 +124,24 @@ scan_packed_kernel(int n_seq, int rows, int H, int p, int n, int G, const T *__r
     }
 }
 
-template <typename T, int NV>
+template <typename T, int NV, int WARPS>
 int launch(str_ctx *ctx, const str_ssd_packed_shape *s, const void *x, const float *dt, const float *A, const void *B, const void *C, const float *D,
            const int32_t *start, const float *state, void *y, float *final_state, cudaStream_t st) {
-    // As many warps as the head has rows for, and enough that a thread carries no more than sixteen elements of b and c.
-    int warps = s->p >= 64 ? 8 : (s->p * LPR + 31) / 32;
-    if (warps < NV / 2) warps = NV / 2;
-    const int threads = 32 * warps, R = threads / LPR;
-    const size_t smem = sizeof(float) * ((size_t)TB * (2 * NV * 4 * LPR + R + R * LPR) + 2 * TB);
-    if (smem > 48 * 1024) STR_CUDA_OK(cudaFuncSetAttribute(scan_packed_kernel<T, NV>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    scan_packed_kernel<T, NV><<<dim3(ceil_div(s->p, R), s->H, s->n_seq), threads, smem, st>>>(
+    constexpr int TB = TOKENS<NV>, threads = 32 * WARPS, R = threads / LPR;
+    constexpr size_t smem = sizeof(float) * ((size_t)TB * (2 * NV * 4 * LPR + R + threads) + 2 * TB);
+    if (smem > 48 * 1024) STR_CUDA_OK(cudaFuncSetAttribute(scan_packed_kernel<T, NV, WARPS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    scan_packed_kernel<T, NV, WARPS><<<dim3(ceil_div(s->p, R), s->H, s->n_seq), threads, smem, st>>>(
         s->n_seq, s->rows, s->H, s->p, s->n, s->G, (const T *)x, dt, A, (const T *)B, (const T *)C, D, start, state, (T *)y, final_state, ctx->status_dev);
     return str_launch_ok(ctx);
 }
+// Four warps hold 32 rows of a head, eight 64.
 template <typename T>
 int dispatch(str_ctx *ctx, const str_ssd_packed_shape *s, const void *x, const float *dt, const float *A, const void *B, const void *C, const float *D,
              const int32_t *start, const float *state, void *y, float *final_state, cudaStream_t st) {
     const int need = ceil_div(s->n, 4 * LPR);
-#define SCAN(NV) launch<T, NV>(ctx, s, x, dt, A, B, C, D, start, state, y, final_state, st)
+#define SCAN(NV)                                                                                              \
+    (s->p <= 32 && NV < 16 ? launch<T, NV, 4>(ctx, s, x, dt, A, B, C, D, start, state, y, final_state, st) \
+                           : launch<T, NV, 8>(ctx, s, x, dt, A, B, C, D, start, state, y, final_state, st))
     return need <= 1 ? SCAN(1) : need <= 2 ? SCAN(2) : need <= 4 ? SCAN(4) : need <= 8 ? SCAN(8) : SCAN(16);
 #undef SCAN
 }
