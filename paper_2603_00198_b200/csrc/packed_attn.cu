@@ -67,22 +67,49 @@ attn_packed_simt_kernel(int n_seq, int rows_q, int rows_k, int Hq, int Hkv, int 
 #pragma unroll
         for (int c = 0; c < DC * 2; ++c) acc[a][c] = make_float2(0.f, 0.f);
     }
-    for (int c0 = 0; c0 < seen; c0 += BC) {
-        __syncthreads();
-        bool odd = false;                                                // a value that is not finite
+    // fp32 rows travel to shared memory in the background, the next keys during the softmax and the second product, the next values during the first.
+    const bool ahead = sizeof(T) == 4 && vec;
+    auto fetch = [&](const T *from, float *to, int ld, int c0) {
 #pragma unroll 4
         for (int e = tid; e < BC * (DP / 4); e += THREADS) {
             const int r = e / (DP / 4), c = e % (DP / 4) * 4;
-            const size_t at = ((size_t)(b.k0 + c0 + r) * Hkv + kv) * d + c;
-            const int in = c0 + r < seen ? d - c : 0;                    // columns from c on
-            const float4 kk = load4(k + at, in, vec), vv = load4(v + at, in, vec);
-            *(float4 *)(Ks + r * LD + c) = kk;
-            *(float4 *)(Vs + r * DP + c) = vv;
-            odd |= !(isfinite(vv.x) && isfinite(vv.y) && isfinite(vv.z) && isfinite(vv.w));
+            const bool in = c0 + r < seen && c < d;                      // the rest is filled with zeros
+            const T *at = in ? from + ((size_t)(b.k0 + c0 + r) * Hkv + kv) * d + c : from;
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to + r * ld + c)), "l"(at), "r"(in ? 16 : 0) : "memory");
         }
+    };
+    auto sent = [&]() { asm volatile("cp.async.commit_group;" ::: "memory"); };
+    auto all_but_last_here = [&]() { asm volatile("cp.async.wait_group 1;" ::: "memory"); };
+    auto odd4 = [&](const float4 &x) { return !(isfinite(x.x) && isfinite(x.y) && isfinite(x.z) && isfinite(x.w)); };
+    if (ahead && seen > 0) {
+        fetch(k, Ks, LD, 0);
+        sent();
+        fetch(v, Vs, DP, 0);
+        sent();
+    }
+    for (int c0 = 0; c0 < seen; c0 += BC) {
         // Weights of hidden keys are zero, and zero times a value that is not finite is not: a tile that some rows see in part only, with such a
         // value in it, takes the sum that leaves hidden keys out.
-        const bool careful = __syncthreads_or(odd && c0 + BC - 1 > first_limit);
+        const bool hides = c0 + BC - 1 > first_limit;
+        bool careful = false;
+        if (ahead) {
+            all_but_last_here();
+            __syncthreads();
+        } else {
+            __syncthreads();
+            bool odd = false;                                            // a value that is not finite
+#pragma unroll 4
+            for (int e = tid; e < BC * (DP / 4); e += THREADS) {
+                const int r = e / (DP / 4), c = e % (DP / 4) * 4;
+                const size_t at = ((size_t)(b.k0 + c0 + r) * Hkv + kv) * d + c;
+                const int in = c0 + r < seen ? d - c : 0;                // columns from c on
+                const float4 kk = load4(k + at, in, vec), vv = load4(v + at, in, vec);
+                *(float4 *)(Ks + r * LD + c) = kk;
+                *(float4 *)(Vs + r * DP + c) = vv;
+                odd |= odd4(vv);
+            }
+            careful = __syncthreads_or(odd && hides);
+        }
         float2 s2[8][4];                                                 // even and odd columns' sums
 #pragma unroll
         for (int a = 0; a < 8; ++a)
@@ -102,6 +129,11 @@ attn_packed_simt_kernel(int n_seq, int rows_q, int rows_k, int Hq, int Hkv, int 
                     s2[a][j] = __ffma2_rn(make_float2(qq.z, qq.w), make_float2(kk[j].z, kk[j].w), s2[a][j]);
                 }
             }
+        }
+        if (ahead) {
+            __syncthreads();
+            if (c0 + BC < seen) fetch(k, Ks, LD, c0 + BC);
+            sent();
         }
         float s[8][4];
 #pragma unroll
@@ -135,6 +167,13 @@ attn_packed_simt_kernel(int n_seq, int rows_q, int rows_k, int Hq, int Hkv, int 
             for (int c = 0; c < DC * 2; ++c) acc[a][c] = __fmul2_rn(acc[a][c], make_float2(f, f));
         }
         __syncwarp();                                                    // a row's weights are written and read by the same half warp
+        if (ahead) {
+            all_but_last_here();
+            bool odd = false;
+            if (hides)
+                for (int e = tid; e < BC * (DP / 4); e += THREADS) odd |= odd4(*(const float4 *)(Vs + 4 * e));
+            careful = __syncthreads_or(odd);
+        }
         if (!careful) {
 #pragma unroll 2
             for (int j = 0; j < BC; j += 4) {
@@ -169,6 +208,11 @@ attn_packed_simt_kernel(int n_seq, int rows_q, int rows_k, int Hq, int Hkv, int 
                             acc[a][c] = __ffma2_rn(make_float2(p, p), make_float2(vv[0], vv[1]), acc[a][c]);
                         }
                     }
+        }
+        if (ahead) {
+            __syncthreads();
+            if (c0 + BC < seen) fetch(v, Vs, DP, c0 + BC);
+            sent();
         }
     }
 #pragma unroll
