@@ -29,7 +29,7 @@ __device__ __forceinline__ void packed_check(const int32_t *start, int n_seq, in
 }
 
 // ---- the order of attention's query blocks ------------------------------------------------------
-// A query block is `block` consecutive queries of one sequence; it costs as many key tiles as its last query sees.  CTA number r
+// A query block is block.d consecutive queries of one sequence; it costs as many key tiles as its last query sees.  CTA number r
 // takes the r-th most expensive block of all sequences, so that the long ones start first and the short ones fill the gaps.
 // No list is made: the number of blocks that cost `tiles` or more is a sum over the sequences of a closed form, and a binary search over the
 // cost, then a prefix sum over the sequences, find block r.  Run by one whole warp.
@@ -38,34 +38,44 @@ struct PackedBlock {
     int q0, lq, k0, lk;          // the sequence's rows
 };
 
-struct PackedAttnSeq {
-    int q0, lq, k0, lk;
+// Queries a block, and what divides by it: x / d = high half of x * (2^64 / d, rounded up), exact for 32-bit x.
+// (A division by a number known at run time only costs some 40 instructions, and the search makes one a step and sequence.)
+struct PackedBlockSize {
+    int d;
+    unsigned long long m;
+    explicit PackedBlockSize(int size) : d(size), m(size > 1 ? ~0ULL / (unsigned)size + 1 : 0) {}
+    __device__ __forceinline__ int into(int x) const { return d > 1 ? (int)__umul64hi((unsigned long long)(unsigned)x, m) : x; }
 };
-__device__ __forceinline__ PackedAttnSeq packed_attn_seq(const int32_t *q_start, const int32_t *k_start, int s, int rows_q, int rows_k) {
+
+struct PackedAttnSeq {
+    int q0, lq, k0, lk, blocks;
+};
+__device__ __forceinline__ PackedAttnSeq packed_attn_seq(const int32_t *q_start, const int32_t *k_start, int s, int rows_q, int rows_k, const PackedBlockSize &block) {
     PackedAttnSeq r;
     r.q0 = packed_start(q_start, s, rows_q);
     r.lq = max(packed_start(q_start, s + 1, rows_q) - r.q0, 0);
     r.k0 = packed_start(k_start, s, rows_k);
     r.lk = max(packed_start(k_start, s + 1, rows_k) - r.k0, 0);
+    r.blocks = r.lq > 0 ? block.into(r.lq - 1) + 1 : 0;
     return r;
 }
 // Blocks of the sequence whose last query sees more than (tiles - 1) * key_tile keys; all of them for tiles <= 0.
-__device__ __forceinline__ int packed_blocks_of_cost(const PackedAttnSeq &q, int block, int key_tile, int tiles) {
-    const int n = (q.lq + block - 1) / block;
-    if (tiles <= 0) return n;
+__device__ __forceinline__ int packed_blocks_of_cost(const PackedAttnSeq &q, const PackedBlockSize &block, int key_tile, int tiles) {
+    if (tiles <= 0) return q.blocks;
     const long long below = (long long)(tiles - 1) * key_tile;
     if (q.lk <= below) return 0;
-    const long long y = below - q.lk + q.lq;             // the last query of a block has to be number y or later
-    return y <= 0 ? n : n - (int)y / block;              // y < lq
+    const long long y = below - q.lk + q.lq;             // the last query of a block has to be number y (< lq) or later
+    return y <= 0 ? q.blocks : q.blocks - block.into((int)y);
 }
-__device__ __forceinline__ PackedBlock packed_block(const int32_t *q_start, const int32_t *k_start, int n_seq, int rows_q, int rows_k, int block,
+__device__ __forceinline__ PackedBlock packed_block(const int32_t *q_start, const int32_t *k_start, int n_seq, int rows_q, int rows_k, const PackedBlockSize &block,
                                                     int key_tile, int r) {
     const int lane = threadIdx.x & 31;
     // the lane's first sequence stays in registers: most calls have no more than 32
-    const PackedAttnSeq own = lane < n_seq ? packed_attn_seq(q_start, k_start, lane, rows_q, rows_k) : PackedAttnSeq{};
+    const PackedAttnSeq own = lane < n_seq ? packed_attn_seq(q_start, k_start, lane, rows_q, rows_k, block) : PackedAttnSeq{};
     auto blocks = [&](int tiles) {
         int n = packed_blocks_of_cost(own, block, key_tile, tiles);
-        for (int s = lane + 32; s < n_seq; s += 32) n += packed_blocks_of_cost(packed_attn_seq(q_start, k_start, s, rows_q, rows_k), block, key_tile, tiles);
+        for (int s = lane + 32; s < n_seq; s += 32)
+            n += packed_blocks_of_cost(packed_attn_seq(q_start, k_start, s, rows_q, rows_k, block), block, key_tile, tiles);
         return (int)__reduce_add_sync(0xffffffffu, (unsigned)n);
     };
     PackedBlock b = {};
@@ -81,10 +91,10 @@ __device__ __forceinline__ PackedBlock packed_block(const int32_t *q_start, cons
         PackedAttnSeq q = {};
         int from = 0, n = 0;
         if (s0 + lane < n_seq) {
-            q = s0 == 0 ? own : packed_attn_seq(q_start, k_start, s0 + lane, rows_q, rows_k);
-            const int all = (q.lq + block - 1) / block, more = packed_blocks_of_cost(q, block, key_tile, lo + 1);
+            q = s0 == 0 ? own : packed_attn_seq(q_start, k_start, s0 + lane, rows_q, rows_k, block);
+            const int more = packed_blocks_of_cost(q, block, key_tile, lo + 1);
             n = packed_blocks_of_cost(q, block, key_tile, lo) - more;
-            from = all - more - n;
+            from = q.blocks - more - n;
         }
         int upto = n;
 #pragma unroll
@@ -97,12 +107,12 @@ __device__ __forceinline__ PackedBlock packed_block(const int32_t *q_start, cons
             const int l = __ffs(found) - 1;
             const int i = from + left - (upto - n);       // meaningful in lane l only
             b.seq = s0 + l;
-            b.first = __shfl_sync(0xffffffffu, i, l) * block;
+            b.first = __shfl_sync(0xffffffffu, i, l) * block.d;
             b.q0 = __shfl_sync(0xffffffffu, q.q0, l);
             b.lq = __shfl_sync(0xffffffffu, q.lq, l);
             b.k0 = __shfl_sync(0xffffffffu, q.k0, l);
             b.lk = __shfl_sync(0xffffffffu, q.lk, l);
-            b.n = min(block, b.lq - b.first);
+            b.n = min(block.d, b.lq - b.first);
             return b;
         }
         left -= __shfl_sync(0xffffffffu, upto, 31);

@@ -29,7 +29,7 @@ __device__ __forceinline__ float4 load4(const T *p, int in, bool vec) {
 // DP: head size padded to 64 or 128.  Thread (ty, tx) of BR/8 x 16: rows ty + BR/8 a (a < 8), keys tx + 16 j (j < 4), columns 4 tx + 64 c ...
 template <typename T, int DP, int BR>
 __global__ void __launch_bounds__(2 * BR)
-attn_packed_simt_kernel(int n_seq, int rows_q, int rows_k, int Hq, int Hkv, int d, float scale_log2, const int32_t *__restrict__ q_start,
+attn_packed_simt_kernel(int n_seq, int rows_q, int rows_k, int Hq, int Hkv, int d, float scale_log2, const PackedBlockSize per, const int32_t *__restrict__ q_start,
                         const int32_t *__restrict__ k_start, const T *__restrict__ q, const T *__restrict__ k, const T *__restrict__ v, T *__restrict__ o,
                         int *status) {
     constexpr int LD = DP + 4, DC = DP / 64, THREADS = 2 * BR, RS = BR / 8;
@@ -37,7 +37,7 @@ attn_packed_simt_kernel(int n_seq, int rows_q, int rows_k, int Hq, int Hkv, int 
     float *Qs = (float *)smem4, *Ks = Qs + BR * LD, *Vs = Ks + BC * LD, *Ps = Vs + BC * DP;
     __shared__ PackedBlock blk;
     const int tid = threadIdx.x, ty = tid / 16, tx = tid % 16;
-    const int kv = blockIdx.x % Hkv, group = Hq / Hkv, per = BR / group;  // queries per block
+    const int kv = blockIdx.x % Hkv, group = Hq / Hkv;                   // `per` queries a block
     if (blockIdx.x == 0) {
         packed_check(q_start, n_seq, rows_q, status);
         packed_check(k_start, n_seq, rows_k, status);
@@ -237,7 +237,7 @@ int launch(str_ctx *ctx, const str_attn_packed_shape *s, const void *q, const vo
     STR_CUDA_OK(cudaFuncSetAttribute(attn_packed_simt_kernel<T, DP, BR>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     const int per = BR / (s->Hq / s->Hkv);
     attn_packed_simt_kernel<T, DP, BR><<<(s->rows_q / per + s->n_seq) * s->Hkv, 2 * BR, smem, st>>>(
-        s->n_seq, s->rows_q, s->rows_k, s->Hq, s->Hkv, s->d, scale * 1.4426950408889634f, q_start, k_start, (const T *)q, (const T *)k, (const T *)v,
+        s->n_seq, s->rows_q, s->rows_k, s->Hq, s->Hkv, s->d, scale * 1.4426950408889634f, PackedBlockSize(per), q_start, k_start, (const T *)q, (const T *)k, (const T *)v,
         (T *)o, ctx->status_dev);
     return str_launch_ok(ctx);
 }

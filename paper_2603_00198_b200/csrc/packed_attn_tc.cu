@@ -122,8 +122,8 @@ struct Parts {
 template <int HD>
 __global__ void __launch_bounds__(NUM_THREADS, 1)
 attn_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
-                      int n_seq, int rows_q, int rows_k, int Hq, int Hkv, int d, float scale_log2, const int32_t *__restrict__ q_start,
-                      const int32_t *__restrict__ k_start, const __nv_bfloat16 *__restrict__ q, const __nv_bfloat16 *__restrict__ k,
+                      const __grid_constant__ CUtensorMap tmap_o, const PackedBlockSize block_size, int n_seq, int rows_q, int rows_k, int Hq, int Hkv, int d,
+                      float scale_log2, const int32_t *__restrict__ q_start, const int32_t *__restrict__ k_start, const __nv_bfloat16 *__restrict__ q, const __nv_bfloat16 *__restrict__ k,
                       const __nv_bfloat16 *__restrict__ v, __nv_bfloat16 *__restrict__ out, const Parts parts, int *status) {
     typedef Smem<HD> SM;
     constexpr int HALVES = HD / 64;
@@ -143,62 +143,86 @@ attn_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_c
         if (threadIdx.x == 0) atomicCAS(status, 0, STR_ERR_CUDA);
         return;
     }
-    if (tc::cta_should_leave(status)) return;     // an earlier CTA failed: the whole CTA leaves at once
     if (blockIdx.x == 0) {
         packed_check(q_start, n_seq, rows_q, status);
         packed_check(k_start, n_seq, rows_k, status);
     }
-    if (warp == 0) {
-        const PackedBlock b = packed_block(q_start, k_start, n_seq, rows_q, rows_k, 2 * TQ, BKV, rank);
-        if (lane == 0) *blk = b;
-    }
-    if (threadIdx.x == 32) {
-        tc::mbar_init(bars + B_Q, 1);
-        for (int s = 0; s < 2; ++s) {
-            tc::mbar_init(bars + B_KF + s, 1); tc::mbar_init(bars + B_KE + s, 1);
-            tc::mbar_init(bars + B_VF + s, 1); tc::mbar_init(bars + B_VR + s, 1); tc::mbar_init(bars + B_VE + s, 2);
-            tc::mbar_init(bars + B_SF + s, 1); tc::mbar_init(bars + B_PA + s, 4); tc::mbar_init(bars + B_PB + s, 4);
-            tc::mbar_init(bars + B_OF + s, 1);
+    // Query number t of the block sees the keys 0 .. first_limit + t.  Of the key tiles of its row tiles (tile 1 has no fewer than tile 0 unless it is
+    // empty) this CTA takes its share: tiles j0 + j, j < n0 or n1.
+    struct Walk {
+        int first_limit, j0, n0, n1, nt;
+        __device__ __forceinline__ Walk(const PackedBlock &b, int TQ, int splits, int split) {
+            first_limit = b.lk - b.lq + b.first;
+            const int all0 = (max(first_limit + min(b.n, TQ), 0) + BKV - 1) / BKV, all1 = b.n > TQ ? (max(first_limit + b.n, 0) + BKV - 1) / BKV : 0;
+            const int share = (max(all0, all1) + splits - 1) / splits;
+            j0 = split * share;
+            n0 = max(min(all0, j0 + share) - j0, 0), n1 = max(min(all1, j0 + share) - j0, 0), nt = max(n0, n1);
         }
-        abort_flag[0] = 0; abort_flag[1] = 0; found[0] = 0;
-        tc::fence_mbar_init();
-        tc::prefetch_tmap(&tmap_q); tc::prefetch_tmap(&tmap_k); tc::prefetch_tmap(&tmap_v);
+    };
+    auto load_k = [&](const PackedBlock &b, int j0, int j) {
+        tc::mbar_arrive_expect_tx(bars + B_KF + (j & 1), SM::TILE);
+        for (int hf = 0; hf < HALVES; ++hf)
+            tc::tma_load_3d(smem + SM::K + (j & 1) * SM::TILE + hf * TILE_16K, &tmap_k, bars + B_KF + (j & 1), hf * 64, kv, b.k0 + (j0 + j) * BKV);
+    };
+    // The producer finds the block and sends for its queries and first keys while the others make ready (with the bulk store at the end: sixteen sequences of
+    // 1000 rows 76 -> 70 us, one of 16512 rows 1920 -> 1881).  A CTA leaves, whole, when there is no block for it or an earlier one failed.
+    if (warp == 8) {
+        const int failed = *(volatile const int *)status;
+        if (lane == 0) {
+            tc::mbar_init(bars + B_Q, 1);
+            for (int s = 0; s < 2; ++s) {
+                tc::mbar_init(bars + B_KF + s, 1); tc::mbar_init(bars + B_KE + s, 1);
+                tc::mbar_init(bars + B_VF + s, 1); tc::mbar_init(bars + B_VR + s, 1); tc::mbar_init(bars + B_VE + s, 2);
+                tc::mbar_init(bars + B_SF + s, 1); tc::mbar_init(bars + B_PA + s, 4); tc::mbar_init(bars + B_PB + s, 4);
+                tc::mbar_init(bars + B_OF + s, 1);
+            }
+            abort_flag[0] = 0; abort_flag[1] = 0; found[0] = 0;
+            tc::fence_mbar_init();
+            tc::prefetch_tmap(&tmap_q); tc::prefetch_tmap(&tmap_k); tc::prefetch_tmap(&tmap_v);
+        }
+        __syncwarp();
+        PackedBlock b = packed_block(q_start, k_start, n_seq, rows_q, rows_k, block_size, BKV, rank);
+        if (failed) b.n = 0;
+        if (lane == 0) {
+            *blk = b;
+            if (parts.splits > 1 && split == 0) parts.block[(size_t)rank * Hkv + kv] = b;
+            const Walk w(b, TQ, parts.splits, split);
+            if (b.n > 0 && w.nt > 0) {
+                tc::mbar_arrive_expect_tx(bars + B_Q, (uint32_t)(2 * HALVES * TQ * group) * 128u);
+                for (int i = 0; i < 2; ++i)
+                    for (int hf = 0; hf < HALVES; ++hf)
+                        tc::tma_load_3d(smem + SM::Q + i * SM::TILE + hf * TILE_16K, &tmap_q, bars + B_Q, hf * 64, kv * group, b.q0 + b.first + i * TQ);
+                load_k(b, w.j0, 0);
+            }
+        }
+        __syncwarp();
     }
-    __syncthreads();
-    const PackedBlock b = *blk;
-    if (parts.splits > 1 && split == 0 && threadIdx.x == 0) parts.block[(size_t)rank * Hkv + kv] = b;
-    if (b.n <= 0) return;                                             // more CTAs than blocks of queries
     if (warp == 9) { tc::tmem_alloc(tmem_slot, 512); tc::tmem_relinquish(); }
     tc::tc_fence_before();
     __syncthreads();
     tc::tc_fence_after();
     const uint32_t tmem = *tmem_slot;
-
-    // Query number t of the block sees the keys 0 .. first_limit + t.
-    const int first_limit = b.lk - b.lq + b.first;
-    const int all0 = (max(first_limit + min(b.n, TQ), 0) + BKV - 1) / BKV;            // key tiles of row tile 0
-    const int all1 = b.n > TQ ? (max(first_limit + b.n, 0) + BKV - 1) / BKV : 0;      // of row tile 1; not fewer unless it is empty
-    // This CTA's share of them: tiles j0 + j, j < n0 or n1.
-    const int share = (max(all0, all1) + parts.splits - 1) / parts.splits, j0 = split * share;
-    const int n0 = max(min(all0, j0 + share) - j0, 0), n1 = max(min(all1, j0 + share) - j0, 0), nt = max(n0, n1);
+    const PackedBlock b = *blk;
+    if (b.n <= 0) {
+        if (warp == 9) tc::tmem_dealloc(tmem, 512);
+        return;
+    }
+    const Walk walk(b, TQ, parts.splits, split);
+    const int first_limit = walk.first_limit, j0 = walk.j0, n0 = walk.n0, n1 = walk.n1, nt = walk.nt;
 
     if (warp == 8) {
         // ------------------------------------------------------------------ TMA producer
         if (lane == 0 && nt > 0) {
             bool ok = true;
-            tc::mbar_arrive_expect_tx(bars + B_Q, (uint32_t)(2 * HALVES * TQ * group) * 128u);
-            for (int i = 0; i < 2; ++i)
-                for (int hf = 0; hf < HALVES; ++hf)
-                    tc::tma_load_3d(smem + SM::Q + i * SM::TILE + hf * TILE_16K, &tmap_q, bars + B_Q, hf * 64, kv * group, b.q0 + b.first + i * TQ);
-            int issued_k = 0, issued_v = 0;
+            int issued_k = 1, issued_v = 0;                           // the queries and keys of tile 0 are on their way
             for (int j = 0; j < nt; ++j) {
                 const int s = j & 1;
                 const uint32_t ph = ((j >> 1) & 1) ^ 1;
                 if (!tc::mbar_wait(bars + B_KE + s, ph, abort_flag)) { ok = false; break; }
-                tc::mbar_arrive_expect_tx(bars + B_KF + s, SM::TILE);
-                for (int hf = 0; hf < HALVES; ++hf)
-                    tc::tma_load_3d(smem + SM::K + s * SM::TILE + hf * TILE_16K, &tmap_k, bars + B_KF + s, hf * 64, kv, b.k0 + (j0 + j) * BKV);
-                ++issued_k;
+                if (j > 0) {
+                    load_k(b, j0, j);
+                    ++issued_k;
+                }
                 if (!tc::mbar_wait(bars + B_VE + s, ph, abort_flag)) { ok = false; break; }
                 tc::mbar_arrive_expect_tx(bars + B_VF + s, SM::TILE);
                 for (int hf = 0; hf < HALVES; ++hf)
@@ -380,6 +404,11 @@ attn_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_c
             l += sum.x + sum.y;
         }
         if (ok && ni > 0) ok = tc::mbar_wait(bars + B_OF + i, 0, abort_flag);
+        else if (ok && nt > 0) ok = tc::mbar_wait(bars + B_Q, 0, abort_flag);        // nothing to see, but the queries' copy has to have landed
+        // A whole tile goes out through shared memory, over its queries (every product that read them is through), by one bulk store: written by a
+        // thread each, the rows take 3500 clocks a CTA.  The last tile of a sequence, whose rows beyond the end are not its own, is written so.
+        const bool whole = parts.splits == 1 && (i + 1) * TQ <= b.n;
+        uint8_t *tile = smem + SM::Q + i * SM::TILE;
         if (ok) {
             tc::tc_fence_after();
             if (parts.splits > 1) {
@@ -406,21 +435,30 @@ attn_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_c
                         tc::tmem_ld32(tO + c * 32, o);
                         tc::tmem_ld_wait();
                     }
-                    if (live) {
 #pragma unroll
-                        for (int g = 0; g < 4; ++g) {
-                            if (c * 32 + g * 8 >= d) break;
-                            uint32_t r[4];
+                    for (int g = 0; g < 4; ++g) {
+                        uint32_t r[4];
 #pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                r[e] = sees ? tc::pack_bf16x2(__uint_as_float(o[8 * g + 2 * e]) * inv, __uint_as_float(o[8 * g + 2 * e + 1]) * inv) : 0u;
-                            *reinterpret_cast<uint4 *>(dst + c * 32 + g * 8) = make_uint4(r[0], r[1], r[2], r[3]);
-                        }
+                        for (int e = 0; e < 4; ++e)
+                            r[e] = sees ? tc::pack_bf16x2(__uint_as_float(o[8 * g + 2 * e]) * inv, __uint_as_float(o[8 * g + 2 * e + 1]) * inv) : 0u;
+                        const uint4 w4 = make_uint4(r[0], r[1], r[2], r[3]);
+                        if (whole) *(uint4 *)(tile + (c >> 1) * TILE_16K + (row >> 3) * 1024 + (row & 7) * 128 + ((((c & 1) * 4 + g) ^ (row & 7)) << 4)) = w4;
+                        else if (live && c * 32 + g * 8 < d) *reinterpret_cast<uint4 *>(dst + c * 32 + g * 8) = w4;
                     }
                 }
+                if (whole) tc::fence_proxy_async();
             }
         } else if (lane == 0) {
             atomicCAS(status, 0, STR_ERR_TIMEOUT);
+        }
+        if (whole) {                                                  // (alike in the tile's four warps, and all of them come here)
+            asm volatile("barrier.sync %0, 128;" ::"r"(1 + i) : "memory");
+            if (ok && quad == 0 && lane == 0) {
+                for (int hf = 0; hf < HALVES && hf * 64 < d; ++hf) tc::tma_store_3d(&tmap_o, tile + hf * TILE_16K, hf * 64, kv * group, b.q0 + b.first + i * TQ);
+                tc::bulk_commit();
+                tc::bulk_wait_read();
+            }
+            __syncwarp();
         }
     }
     tc::tc_fence_before();
@@ -428,6 +466,8 @@ attn_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_c
     if (warp == 9) { tc::tc_fence_after(); tc::tmem_dealloc(tmem, 512); }
     if (parts.splits > 1 && threadIdx.x == 0) parts.found[part] = found[0];
     if (found[0] == 0 || parts.splits > 1) return;
+    tc::bulk_wait_written();                                          // what the bulk stores wrote is written over
+    __syncthreads();
     for (int r = warp; r < b.n * group; r += NUM_WARPS) {
         const int t = r / group;
         const size_t at = ((size_t)(b.q0 + b.first + t) * Hq + kv * group + r % group) * d, keys = ((size_t)b.k0 * Hkv + kv) * d;
@@ -508,10 +548,11 @@ template <int HD>
 int launch(str_ctx *ctx, const str_attn_packed_shape *s, const void *q, const void *k, const void *v, const int32_t *q_start, const int32_t *k_start,
            float scale, void *o, void *workspace, cudaStream_t st) {
     const int group = s->Hq / s->Hkv, TQ = BQ / group;
-    CUtensorMap tq, tk, tv;
+    CUtensorMap tq, tk, tv, to;
     int rc = str_make_tmap_heads_bf16_sw128(ctx, &tq, q, s->d, s->Hq, s->rows_q, group, TQ);
     if (rc == STR_OK) rc = str_make_tmap_heads_bf16_sw128(ctx, &tk, k, s->d, s->Hkv, s->rows_k, 1, BKV);
     if (rc == STR_OK) rc = str_make_tmap_heads_bf16_sw128(ctx, &tv, v, s->d, s->Hkv, s->rows_k, 1, BKV);
+    if (rc == STR_OK) rc = str_make_tmap_heads_bf16_sw128(ctx, &to, o, s->d, s->Hq, s->rows_q, group, TQ);
     if (rc != STR_OK) return rc;
     rc = str_ensure_smem(ctx, HD == 64 ? STR_SMEM_ATTN_PACKED_64 : STR_SMEM_ATTN_PACKED_128, attn_packed_tc_kernel<HD>, Smem<HD>::BYTES);
     if (rc != STR_OK) return rc;
@@ -520,7 +561,8 @@ int launch(str_ctx *ctx, const str_attn_packed_shape *s, const void *q, const vo
     const float scale_log2 = scale * 1.4426950408889634f;
     const __nv_bfloat16 *pq = (const __nv_bfloat16 *)q, *pk = (const __nv_bfloat16 *)k, *pv = (const __nv_bfloat16 *)v;
     attn_packed_tc_kernel<HD><<<blocks * s->Hkv * parts.splits, NUM_THREADS, Smem<HD>::BYTES, st>>>(
-        tq, tk, tv, s->n_seq, s->rows_q, s->rows_k, s->Hq, s->Hkv, s->d, scale_log2, q_start, k_start, pq, pk, pv, (__nv_bfloat16 *)o, parts, ctx->status_dev);
+        tq, tk, tv, to, PackedBlockSize(2 * TQ), s->n_seq, s->rows_q, s->rows_k, s->Hq, s->Hkv, s->d, scale_log2, q_start, k_start, pq, pk, pv, (__nv_bfloat16 *)o, parts,
+        ctx->status_dev);
     if (parts.splits == 1) return str_launch_ok(ctx);
     attn_packed_join_kernel<HD><<<dim3(blocks * s->Hkv, 16), JOIN_WARPS * 32, 0, st>>>(s->Hq, s->Hkv, s->d, scale_log2, pq, pk, pv, (__nv_bfloat16 *)o, parts,
                                                                                       ctx->status_dev);
