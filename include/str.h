@@ -462,7 +462,7 @@ int str_mamba_conv_packed(str_ctx *ctx, int dtype, int n_seq, int rows, int H, i
                           const float *conv_b, const float *dt_bias, const int32_t *seq_start, const void *window, void *x_out, void *B_out,
                           void *C_out, float *dt_out, void *window_out, void *stream);
 /* The same for T tokens each of Bz sequences (decoding: what str_mamba2_step takes), zxbcdt [Bz*T, ...]; the window (not NULL) may be updated in
- * place (window_out == window).  Time grows with T. */
+ * place (window_out == window).  Time grows with T.  Errors: as above, and UNSUPPORTED_SHAPE for T*H > 2^30. */
 int str_mamba_conv_step(str_ctx *ctx, int dtype, int Bz, int T, int H, int p, int n, int G, int W, const void *zxbcdt, const float *conv_w,
                         const float *conv_b, const float *dt_bias, const void *window, void *x_out, void *B_out, void *C_out, float *dt_out,
                         void *window_out, void *stream);

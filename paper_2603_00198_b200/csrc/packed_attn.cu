@@ -279,7 +279,9 @@ extern "C" int str_attn_prefill_packed(str_ctx *ctx, const str_attn_packed_shape
     if (kv4_overlap(q, qb, o, qb) || kv4_overlap(k, kb, o, qb) || kv4_overlap(v, kb, o, qb)) return STR_ERR_INVALID_ARG;
     const size_t need = str_attn_prefill_packed_workspace_size(s);
     if (workspace_bytes < need) return STR_ERR_WORKSPACE_TOO_SMALL;
-    if (need && (!workspace || ((uintptr_t)workspace & 255) != 0 || kv4_overlap(workspace, need, o, qb))) return STR_ERR_INVALID_ARG;
+    if (need && (!workspace || ((uintptr_t)workspace & 255) != 0 || kv4_overlap(workspace, need, o, qb) || kv4_overlap(workspace, need, q, qb) ||
+                 kv4_overlap(workspace, need, k, kb) || kv4_overlap(workspace, need, v, kb)))
+        return STR_ERR_INVALID_ARG;
     StrDeviceScope dev(ctx);
     if (!dev.ok) return STR_ERR_CUDA;
     StrProfScope prof_scope(ctx, STR_CAT_ATTN_FWD, stream);

@@ -31,6 +31,17 @@ __device__ __forceinline__ Pack<T, VEC> load_pack(const T *p) {
         for (int i = 0; i < VEC; ++i) r.v[i] = p[i];
     return r;
 }
+// The same of memory that the kernel writes too (its window, in place): not through the read-only path.
+template <int VEC, typename T>
+__device__ __forceinline__ Pack<T, VEC> load_pack_written(const T *p) {
+    Pack<T, VEC> r;
+    if constexpr (VEC * sizeof(T) == 16) *(uint4 *)&r = *(const uint4 *)p;
+    else if constexpr (VEC * sizeof(T) == 8) *(uint2 *)&r = *(const uint2 *)p;
+    else
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) r.v[i] = p[i];
+    return r;
+}
 template <int VEC, typename T>
 __device__ __forceinline__ void store_pack(T *p, const Pack<T, VEC> &r) {
     if constexpr (VEC * sizeof(T) == 16) *(uint4 *)p = *(const uint4 *)&r;
@@ -291,7 +302,7 @@ conv_step_kernel(ConvDims c, int T_new, const T *__restrict__ zx, const float *_
     Pack<T, VEC> before[W - 1];                           // the window moves by whole elements: kept as they are stored
     Row<VEC> hist[W - 1];
 #pragma unroll
-    for (int j = 0; j < W - 1; ++j) before[j] = load_pack<VEC>(window + ((size_t)b * (W - 1) + j) * c.ch + ch0);
+    for (int j = 0; j < W - 1; ++j) before[j] = load_pack_written<VEC>(window + ((size_t)b * (W - 1) + j) * c.ch + ch0);
     const Taps<VEC, W> taps(conv_w, conv_b, ch0);
 #pragma unroll
     for (int j = 0; j < W - 1; ++j) hist[j] = widen(before[j]);
@@ -394,7 +405,7 @@ extern "C" int str_mamba_conv_step(str_ctx *ctx, int dtype, int Bz, int T, int H
         return STR_ERR_INVALID_ARG;
     const int rc = check_dims(dtype, H, p, n, G, W, &c);
     if (rc != STR_OK) return rc;
-    if ((long long)Bz * T > (1 << 30) || column_blocks(c) > 65535) return STR_ERR_UNSUPPORTED_SHAPE;
+    if ((long long)Bz * T > (1 << 30) || (long long)T * H > (1 << 30) || column_blocks(c) > 65535) return STR_ERR_UNSUPPORTED_SHAPE;
     const size_t es = dtype_size(dtype), wb = (size_t)Bz * (W - 1) * c.ch * es;
     if (window != window_out && kv4_overlap(window, wb, window_out, wb)) return STR_ERR_INVALID_ARG;
     StrDeviceScope dev(ctx);

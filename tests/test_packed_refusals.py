@@ -71,6 +71,7 @@ def test_convolution(step):
     assert Call().conv(step, window=1 << 40, wout=1 << 40) == (NO_DEVICE if step else INVALID)
     if step:
         assert Call().conv(step, window=None) == INVALID and Call().conv(step, wout=None) == INVALID and Call().conv(step, rows=0) == INVALID
+        assert Call().conv(step, n_seq=1, rows=1 << 28, H=8) == UNSUPPORTED and Call().conv(step, n_seq=1, rows=1 << 28) == NO_DEVICE
     else:
         assert Call().conv(window=None) == NO_DEVICE and Call().conv(wout=None) == NO_DEVICE and Call().conv(start=None) == INVALID
         assert Call().conv(rows=0, zx=None, x=None, B=None, C=None, dt=None) == NO_DEVICE
@@ -112,16 +113,18 @@ def test_attention():
 
 @no_device
 def test_attention_workspace():
-    """Few queries over many keys ask for one; too small, missing, misaligned or shared with the output it is refused."""
-    def call(ws, given, o=1 << 45):
+    """Few queries over many keys ask for one; too small, missing, misaligned or shared with the output or an input it is refused."""
+    def call(ws, given, o=1 << 45, **at):
         c = Call()
         s = binding.AttnPackedShape(1, 10, 5000, 4, 2, 64, 1)
         need = binding.lib().str_attn_prefill_packed_workspace_size(ctypes.addressof(s))
         assert need > 0
-        return binding.lib().str_attn_prefill_packed(ctypes.addressof(c.ctx), ctypes.addressof(s), *(c.buffer() for _ in range(5)), 0.1, o, ws, need + given, None)
+        return binding.lib().str_attn_prefill_packed(ctypes.addressof(c.ctx), ctypes.addressof(s), *(at.get(n) or c.buffer() for n in ("q", "k", "v", "qs", "ks")), 0.1, o, ws, need + given, None)
 
     at = 1 << 44
     assert call(at, 0) == NO_DEVICE and call(at, -1) == -3 and call(None, 0) == INVALID and call(at + 128, 0) == INVALID and call(1 << 45, 0) == INVALID
+    for name in ("q", "k", "v"):
+        assert call(at, 0, **{name: at + 256}) == INVALID, name
     for shape in ((1, 10, 5000, 4, 2, 64, 0), (1, 5000, 5000, 4, 2, 64, 1), (1, 10, 900, 4, 2, 64, 1), (1, 10, 5000, 4, 2, 63, 1), (0, 10, 5000, 4, 2, 64, 1), (1, 0, 0, 4, 2, 64, 1)):
         s = binding.AttnPackedShape(*shape)
         assert binding.lib().str_attn_prefill_packed_workspace_size(ctypes.addressof(s)) == 0, shape
@@ -142,9 +145,9 @@ def test_rotary():
 
 def test_the_description_of_a_rotary_embedding_is_checked():
     with pytest.raises(ValueError, match="layout"):
-        binding.Rope(1e4, 64, "neox")
+        binding.Rope(1e4, 64, "quarters")
     with pytest.raises(ValueError, match="scaling"):
-        binding.Rope(1e4, 64, scaling="dynamic")
+        binding.Rope(1e4, 64, scaling="square")
 
 
 def test_tensors_are_checked():
