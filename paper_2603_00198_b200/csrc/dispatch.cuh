@@ -100,6 +100,7 @@ bool str_attn_packed_tc_supported(const str_attn_packed_shape *s, const void *q,
 int str_attn_packed_tc(str_ctx *ctx, const str_attn_packed_shape *s, const void *q, const void *k, const void *v, const int32_t *q_start,
                        const int32_t *k_start, float scale, void *o, void *workspace, cudaStream_t st);
 size_t str_attn_packed_tc_workspace(const str_attn_packed_shape *s);
+bool str_scan_packed_tc_shape(const str_ssd_packed_shape *s);
 bool str_scan_packed_tc_supported(const str_ssd_packed_shape *s, const void *x, const void *B, const void *C, const void *y);
 int str_scan_packed_tc(str_ctx *ctx, const str_ssd_packed_shape *s, const void *x, const float *dt, const float *A, const void *B, const void *C,
-                       const float *D, const int32_t *start, const float *init_state, void *y, float *final_state, cudaStream_t st);
+                       const float *D, const int32_t *start, const float *init_state, void *y, float *final_state, float *faded, cudaStream_t st);

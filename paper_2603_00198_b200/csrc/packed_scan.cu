@@ -10,6 +10,8 @@
 //
 // Bound by the chain of tokens where sequences are few (five turns of 1237 rows, 24 heads of 32 x 20: 67 us, 120 ns a token of the longest), by fp32
 // arithmetic and the reading of b and c from shared memory where there are many (5000 rows, 128 heads of 64 x 128: 1.88 ms, 17 TFLOP/s).
+#include <algorithm>
+
 #include "dispatch.cuh"
 #include "packed.cuh"
 
@@ -19,11 +21,12 @@ constexpr int LPR = 4;                                    // lanes per row
 // Tokens per turn: as many as their b, c and outputs leave registers for.
 template <int NV> constexpr int TOKENS = NV <= 4 ? 32 : 16;
 
-template <typename T, int NV, int WARPS>
+// Y: outputs are wanted; else the final state and the sum of dt A (in powers of two) of every sequence are.
+template <typename T, int NV, int WARPS, bool Y>
 __global__ void __launch_bounds__(32 * WARPS)
 scan_packed_kernel(int n_seq, int rows, int H, int p, int n, int G, const T *__restrict__ x, const float *__restrict__ dt, const float *__restrict__ A,
                    const T *__restrict__ B, const T *__restrict__ C, const float *__restrict__ Dskip, const int32_t *__restrict__ start,
-                   const float *state, T *__restrict__ y, float *final_state, int *status) {
+                   const float *state, T *__restrict__ y, float *final_state, float *__restrict__ faded, int *status) {
     constexpr int NP = NV * 4 * LPR, TB = TOKENS<NV>;     // columns, padded; tokens per turn
     constexpr int threads = 32 * WARPS, R = threads / LPR; // rows of the state per block
     extern __shared__ float4 smem4[];
@@ -33,7 +36,7 @@ scan_packed_kernel(int n_seq, int rows, int H, int p, int n, int G, const T *__r
     const int tid = threadIdx.x, i0 = blockIdx.x * R, r = tid / LPR, l = tid % LPR;
     if (blockIdx.x == 0 && h == 0 && s == 0) packed_check(start, n_seq, rows, status);
     const int t0 = packed_start(start, s, rows), t1 = packed_start(start, s + 1, rows);
-    if (t1 <= t0 && (!final_state || (state == final_state))) return;
+    if (t1 <= t0 && (Y ? !final_state || state == final_state : false)) return;
     const size_t base = (((size_t)s * H + h) * p + i0 + r) * n;
     // Four columns at a time where a row has whole vectors of them.
     const bool vec = n % 4 == 0 && (((uintptr_t)state | (uintptr_t)final_state) & 15) == 0;
@@ -55,7 +58,7 @@ scan_packed_kernel(int n_seq, int rows, int H, int p, int n, int G, const T *__r
     // What the thread carries of the next TB tokens: elements tid + k threads of [TB][NP] and of [TB][R].
     constexpr int PER = TB * NP / threads;
     T bq[PER], cq[PER], xq[TB / LPR];
-    float dq = 0.f;
+    float dq = 0.f, fade = 0.f;
     auto fetch = [&](int tb) {
         const int m = min(TB, t1 - tb);
 #pragma unroll
@@ -66,7 +69,7 @@ scan_packed_kernel(int n_seq, int rows, int H, int p, int n, int G, const T *__r
             if (t < m && col < n) {
                 const size_t at = ((size_t)(tb + t) * G + g) * n + col;
                 bq[k] = B[at];
-                cq[k] = C[at];
+                if (Y) cq[k] = C[at];
             }
         }
 #pragma unroll
@@ -83,13 +86,14 @@ scan_packed_kernel(int n_seq, int rows, int H, int p, int n, int G, const T *__r
 #pragma unroll
         for (int k = 0; k < PER; ++k) {
             bs[tid + k * threads] = ldf(&bq[k]);
-            cs[tid + k * threads] = ldf(&cq[k]);
+            if (Y) cs[tid + k * threads] = ldf(&cq[k]);
         }
 #pragma unroll
         for (int k = 0; k < TB / LPR; ++k) xs[tid + k * threads] = ldf(&xq[k]);
         if (tid < m) {
             dts[tid] = dq;
             decay[tid] = expf(dq * Ah);
+            if (!Y) fade = fmaf(dq, Ah * 1.4426950408889634f, fade);
         }
         __syncthreads();
         if (tb + TB < t1) fetch(tb + TB);
@@ -99,21 +103,34 @@ scan_packed_kernel(int n_seq, int rows, int H, int p, int n, int G, const T *__r
             float acc[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
-                const float4 b = *(const float4 *)(bs + t * NP + (v * LPR + l) * 4), c = *(const float4 *)(cs + t * NP + (v * LPR + l) * 4);
-                S[v][0] = fmaf(a, S[v][0], dx * b.x); acc[0] = fmaf(S[v][0], c.x, acc[0]);
-                S[v][1] = fmaf(a, S[v][1], dx * b.y); acc[1] = fmaf(S[v][1], c.y, acc[1]);
-                S[v][2] = fmaf(a, S[v][2], dx * b.z); acc[2] = fmaf(S[v][2], c.z, acc[2]);
-                S[v][3] = fmaf(a, S[v][3], dx * b.w); acc[3] = fmaf(S[v][3], c.w, acc[3]);
+                const float4 b = *(const float4 *)(bs + t * NP + (v * LPR + l) * 4);
+                S[v][0] = fmaf(a, S[v][0], dx * b.x);
+                S[v][1] = fmaf(a, S[v][1], dx * b.y);
+                S[v][2] = fmaf(a, S[v][2], dx * b.z);
+                S[v][3] = fmaf(a, S[v][3], dx * b.w);
+                if (Y) {
+                    const float4 c = *(const float4 *)(cs + t * NP + (v * LPR + l) * 4);
+                    acc[0] = fmaf(S[v][0], c.x, acc[0]);
+                    acc[1] = fmaf(S[v][1], c.y, acc[1]);
+                    acc[2] = fmaf(S[v][2], c.z, acc[2]);
+                    acc[3] = fmaf(S[v][3], c.w, acc[3]);
+                }
             }
-            ys[t * threads + tid] = (acc[0] + acc[1]) + (acc[2] + acc[3]);
+            if (Y) ys[t * threads + tid] = (acc[0] + acc[1]) + (acc[2] + acc[3]);
         }
         __syncthreads();
-        for (int e = tid; e < m * R; e += threads) {
-            const int t = e / R, i = e % R;
-            const float4 part = *(const float4 *)(ys + e * LPR);
-            if (i0 + i < p) stf(y + ((size_t)(tb + t) * H + h) * p + i0 + i, fmaf(Dh, xs[e], (part.x + part.y) + (part.z + part.w)));
+        if (Y) {
+            for (int e = tid; e < m * R; e += threads) {
+                const int t = e / R, i = e % R;
+                const float4 part = *(const float4 *)(ys + e * LPR);
+                if (i0 + i < p) stf(y + ((size_t)(tb + t) * H + h) * p + i0 + i, fmaf(Dh, xs[e], (part.x + part.y) + (part.z + part.w)));
+            }
+            __syncthreads();
         }
-        __syncthreads();
+    }
+    if (!Y && i0 == 0 && tid < 32) {
+        fade = warp_sum(fade);
+        if (tid == 0) faded[(size_t)s * H + h] = fade;
     }
     if (!final_state || i0 + r >= p) return;
 #pragma unroll
@@ -127,36 +144,177 @@ scan_packed_kernel(int n_seq, int rows, int H, int p, int n, int G, const T *__r
     }
 }
 
+// Arguments of a call, or of one of its two passes.
+struct ScanCall {
+    const str_ssd_packed_shape *s;                        // of the call; the pass has n_seq sequences
+    int n_seq;
+    const void *x, *B, *C;
+    const float *dt, *A, *D;
+    const int32_t *start;
+    const float *state;
+    void *y;
+    float *final_state, *faded;
+};
 template <typename T, int NV, int WARPS>
-int launch(str_ctx *ctx, const str_ssd_packed_shape *s, const void *x, const float *dt, const float *A, const void *B, const void *C, const float *D,
-           const int32_t *start, const float *state, void *y, float *final_state, cudaStream_t st) {
+int launch(str_ctx *ctx, const ScanCall &k, cudaStream_t st) {
+    const str_ssd_packed_shape *s = k.s;
     constexpr int TB = TOKENS<NV>, threads = 32 * WARPS, R = threads / LPR;
     constexpr size_t smem = sizeof(float) * ((size_t)TB * (2 * NV * 4 * LPR + R + threads) + 2 * TB);
-    if (smem > 48 * 1024) STR_CUDA_OK(cudaFuncSetAttribute(scan_packed_kernel<T, NV, WARPS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    scan_packed_kernel<T, NV, WARPS><<<dim3(ceil_div(s->p, R), s->H, s->n_seq), threads, smem, st>>>(
-        s->n_seq, s->rows, s->H, s->p, s->n, s->G, (const T *)x, dt, A, (const T *)B, (const T *)C, D, start, state, (T *)y, final_state, ctx->status_dev);
+    auto *kernel = k.y ? scan_packed_kernel<T, NV, WARPS, true> : scan_packed_kernel<T, NV, WARPS, false>;
+    if (smem > 48 * 1024) STR_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    kernel<<<dim3(ceil_div(s->p, R), s->H, k.n_seq), threads, smem, st>>>(k.n_seq, s->rows, s->H, s->p, s->n, s->G, (const T *)k.x, k.dt, k.A, (const T *)k.B, (const T *)k.C, k.D,
+                                                                         k.start, k.state, (T *)k.y, k.final_state, k.faded, ctx->status_dev);
     return str_launch_ok(ctx);
 }
 // Four warps hold 32 rows of a head, eight 64.
 template <typename T>
-int dispatch(str_ctx *ctx, const str_ssd_packed_shape *s, const void *x, const float *dt, const float *A, const void *B, const void *C, const float *D,
-             const int32_t *start, const float *state, void *y, float *final_state, cudaStream_t st) {
-    const int need = ceil_div(s->n, 4 * LPR);
-#define SCAN(NV)                                                                                              \
-    (s->p <= 32 && NV < 16 ? launch<T, NV, 4>(ctx, s, x, dt, A, B, C, D, start, state, y, final_state, st) \
-                           : launch<T, NV, 8>(ctx, s, x, dt, A, B, C, D, start, state, y, final_state, st))
+int dispatch(str_ctx *ctx, const ScanCall &k, cudaStream_t st) {
+    const int need = ceil_div(k.s->n, 4 * LPR);
+#define SCAN(NV) (k.s->p <= 32 && NV < 16 ? launch<T, NV, 4>(ctx, k, st) : launch<T, NV, 8>(ctx, k, st))
     return need <= 1 ? SCAN(1) : need <= 2 ? SCAN(2) : need <= 4 ? SCAN(4) : need <= 8 ? SCAN(8) : SCAN(16);
 #undef SCAN
+}
+int pass(str_ctx *ctx, const ScanCall &k, bool tc, cudaStream_t st) {
+    if (tc) {
+        str_ssd_packed_shape s = *k.s;
+        s.n_seq = k.n_seq;
+        return str_scan_packed_tc(ctx, &s, k.x, k.dt, k.A, k.B, k.C, k.D, k.start, k.state, k.y, k.final_state, k.faded, st);
+    }
+    return k.s->dtype == STR_BF16 ? dispatch<__nv_bfloat16>(ctx, k, st) : dispatch<float>(ctx, k, st);
+}
+
+// ---- long sequences of few heads ----------------------------------------------------------------
+// A sequence is a chain of tokens, and few chains leave most SMs without work.  Then sequences are cut into segments of equal length: one pass forms every
+// segment's state from zero, S <- 2^(sum of dt A) S + (that state) from segment to segment gives the states they start from, and a second pass
+// forms the outputs.  Twice the work, in as many chains as there are segments.  How many is decided from the shape alone (the lengths are on the
+// device), so that the workspace is known beforehand.
+struct Segments {
+    int len, n;                  // rows of one, number of them at most; len 0: sequences are walked whole
+};
+constexpr int SMS = 148, MAX_SEGMENTS = 4 * SMS;
+Segments segments_of(const str_ssd_packed_shape *s) {
+    const bool tc = str_scan_packed_tc_shape(s);
+    // Blocks that run at a time, those of one sequence, and the shortest segment that is worth a pass (token by token 64 rows, 8 us; 24 heads of 32 x 20: one
+    // sequence of 256 rows 31 us whole, 21 in fours, one of 128 rows 17 whole, 20 in halves; chunked 512 rows, of which a CTA's start and end are a third).
+    const int rows_at_a_time = s->p <= 32 && s->n <= 128 ? 32 : 64;
+    const long long room = tc ? SMS : s->n > 128 ? SMS : s->p > 32 ? 2 * SMS : 4 * SMS, least = tc ? 512 : 64;
+    const long long per = (long long)s->H * (tc ? 1 : ceil_div(s->p, rows_at_a_time));
+    const long long more = room / per - s->n_seq;         // segments beside the one that every sequence ends with
+    if (more < 1) return {0, 0};
+    const long long len = align_up((size_t)std::max<long long>((s->rows + more - 1) / more, least), tc ? 128 : 32);
+    // Two passes over a segment against one over the sequence: two and a half segments a sequence on average are where they meet (chunked, 24 heads: two
+    // sequences of 5000 rows in 2 segments each 121 us, whole 101; one of 2000 in 4: 45, whole 60).
+    if (2LL * s->rows < 5 * len * s->n_seq) return {0, 0};
+    return {(int)len, (int)(s->rows / len + s->n_seq)};
+}
+struct Workspace {
+    float *states, *faded;       // [n][H][p][n], [n][H]
+    int32_t *start, *first;      // [n + 1]: the segments' rows; [n_seq + 1]: the sequences' segments
+    size_t bytes;
+    Workspace(const str_ssd_packed_shape *s, const Segments &g, void *at) {
+        const size_t states_bytes = (size_t)g.n * s->H * s->p * s->n * sizeof(float), faded_bytes = (size_t)g.n * s->H * sizeof(float);
+        states = (float *)at;
+        faded = (float *)((uint8_t *)at + states_bytes);
+        start = (int32_t *)((uint8_t *)at + states_bytes + faded_bytes);
+        first = start + g.n + 1;
+        bytes = align_up(states_bytes + faded_bytes + sizeof(int32_t) * ((size_t)g.n + 1 + s->n_seq + 1), 256);
+    }
+};
+
+// One block: the segments of all sequences, in their order.  (n_seq < MAX_SEGMENTS.)
+__global__ void __launch_bounds__(1024) segments_kernel(int n_seq, int rows, Segments g, const int32_t *__restrict__ start, int32_t *__restrict__ seg_start,
+                                                        int32_t *__restrict__ first, int *status) {
+    __shared__ int upto[1024];
+    packed_check(start, n_seq, rows, status);
+    const int s = threadIdx.x;
+    const int r0 = s < n_seq ? packed_start(start, s, rows) : 0, len = s < n_seq ? max(packed_start(start, s + 1, rows) - r0, 0) : 0;
+    const int mine = min((len + g.len - 1) / g.len, g.n); // (fewer than g.n in all, unless the starts are wrong)
+    upto[s] = mine;
+    __syncthreads();
+    for (int o = 1; o < 1024; o <<= 1) {
+        const int v = s >= o ? upto[s - o] : 0;
+        __syncthreads();
+        upto[s] += v;
+        __syncthreads();
+    }
+    const int all = min(upto[1023], g.n), at = upto[s] - mine, end = packed_start(start, n_seq, rows);
+    if (s < n_seq) {
+        first[s] = min(at, g.n);
+        for (int j = 0; j < mine && at + j < g.n; ++j) seg_start[at + j] = r0 + j * g.len;
+    }
+    if (s == 0) first[n_seq] = all;
+    for (int v = all + s; v <= g.n; v += 1024) seg_start[v] = end;
+}
+
+// The states that a sequence's segments start from, over those that they arrive at from zero; a thread VEC elements of one head's state.
+template <int VEC>
+__global__ void __launch_bounds__(256) segment_states_kernel(int H, int elements, const int32_t *__restrict__ first, const float *__restrict__ faded, const float *init_state,
+                                                             float *__restrict__ states, float *final_state) {
+    constexpr int AHEAD = 8;
+    const int e = (blockIdx.x * 256 + threadIdx.x) * VEC, h = blockIdx.y, s = blockIdx.z;
+    if (e >= elements) return;
+    const int v0 = first[s], v1 = first[s + 1];
+    const size_t at = ((size_t)s * H + h) * elements + e;
+    alignas(16) float S[VEC], W[AHEAD][VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) S[i] = init_state ? init_state[at + i] : 0.f;
+    for (int v = v0; v < v1; v += AHEAD) {
+        float f[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k)
+            if (v + k < v1) {
+                const float *w = states + ((size_t)(v + k) * H + h) * elements + e;
+                if constexpr (VEC == 4) *(float4 *)W[k] = *(const float4 *)w;
+                else W[k][0] = w[0];
+                f[k] = exp2f(faded[(size_t)(v + k) * H + h]);
+            }
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k)
+            if (v + k < v1) {
+                float *w = states + ((size_t)(v + k) * H + h) * elements + e;
+                if constexpr (VEC == 4) *(float4 *)w = *(const float4 *)S;
+                else w[0] = S[0];
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) S[i] = fmaf(f[k], S[i], W[k][i]);
+            }
+    }
+    if (final_state)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) final_state[at + i] = S[i];
+}
+
+int in_segments(str_ctx *ctx, const ScanCall &k, const Segments &g, void *workspace, bool tc, cudaStream_t st) {
+    const str_ssd_packed_shape *s = k.s;
+    const Workspace w(s, g, workspace);
+    segments_kernel<<<1, 1024, 0, st>>>(s->n_seq, s->rows, g, k.start, w.start, w.first, ctx->status_dev);
+    int rc = str_launch_ok(ctx);
+    ScanCall states = k, outputs = k;
+    states.n_seq = outputs.n_seq = g.n;
+    states.start = outputs.start = w.start;
+    states.state = nullptr, states.final_state = w.states, states.faded = w.faded, states.y = nullptr;
+    outputs.state = w.states, outputs.final_state = nullptr;
+    if (rc == STR_OK) rc = pass(ctx, states, tc, st);
+    if (rc != STR_OK) return rc;
+    const int elements = s->p * s->n;
+    if (elements % 4 == 0)
+        segment_states_kernel<4><<<dim3(ceil_div(elements, 1024), s->H, s->n_seq), 256, 0, st>>>(s->H, elements, w.first, w.faded, k.state, w.states, k.final_state);
+    else
+        segment_states_kernel<1><<<dim3(ceil_div(elements, 256), s->H, s->n_seq), 256, 0, st>>>(s->H, elements, w.first, w.faded, k.state, w.states, k.final_state);
+    rc = str_launch_ok(ctx);
+    return rc == STR_OK ? pass(ctx, outputs, tc, st) : rc;
 }
 
 }  // namespace
 
-extern "C" size_t str_mamba2_prefill_packed_workspace_size(const str_ssd_packed_shape *) { return 0; }
+extern "C" size_t str_mamba2_prefill_packed_workspace_size(const str_ssd_packed_shape *s) {
+    if (!s || s->n_seq <= 0 || s->rows <= 0 || s->H <= 0 || s->p <= 0 || s->n <= 0 || s->n > 256 || s->p > (1 << 20)) return 0;
+    const Segments g = segments_of(s);
+    return g.len ? Workspace(s, g, nullptr).bytes : 0;
+}
 
 extern "C" int str_mamba2_prefill_packed(str_ctx *ctx, const str_ssd_packed_shape *s, const void *x, const float *dt, const float *A, const void *B,
                                          const void *C, const float *D, const int32_t *seq_start, const float *init_state, void *y,
                                          float *final_state, void *workspace, size_t workspace_bytes, void *stream) {
-    (void)workspace;
     if (!ctx || !s || !A || !seq_start) return STR_ERR_INVALID_ARG;
     if (s->n_seq <= 0 || s->rows < 0 || s->H <= 0 || s->p <= 0 || s->n <= 0 || s->G <= 0 || s->H % s->G != 0 ||
         (s->dtype != STR_F32 && s->dtype != STR_BF16))
@@ -167,16 +325,21 @@ extern "C" int str_mamba2_prefill_packed(str_ctx *ctx, const str_ssd_packed_shap
     const size_t xb = (size_t)s->rows * s->H * s->p * es, bb = (size_t)s->rows * s->G * s->n * es;
     if (final_state != init_state && kv4_overlap(init_state, state_bytes, final_state, state_bytes)) return STR_ERR_INVALID_ARG;
     if (kv4_overlap(x, xb, y, xb) || kv4_overlap(B, bb, y, xb) || kv4_overlap(C, bb, y, xb)) return STR_ERR_INVALID_ARG;
-    if (workspace_bytes < str_mamba2_prefill_packed_workspace_size(s)) return STR_ERR_WORKSPACE_TOO_SMALL;
+    const size_t need = str_mamba2_prefill_packed_workspace_size(s);
+    if (workspace_bytes < need) return STR_ERR_WORKSPACE_TOO_SMALL;
+    if (need && (!workspace || ((uintptr_t)workspace & 255) != 0)) return STR_ERR_INVALID_ARG;
+    const size_t db = (size_t)s->rows * s->H * sizeof(float);
+    const struct { const void *at; size_t bytes; } others[] = {{x, xb}, {B, bb}, {C, bb}, {y, xb}, {dt, db}, {init_state, state_bytes}, {final_state, state_bytes}};
+    for (const auto &o : others)
+        if (need && kv4_overlap(workspace, need, o.at, o.bytes)) return STR_ERR_INVALID_ARG;
     StrDeviceScope dev(ctx);
     if (!dev.ok) return STR_ERR_CUDA;
     StrProfScope prof_scope(ctx, STR_CAT_SSD, stream);
     cudaStream_t st = (cudaStream_t)stream;
     // The chunked kernel's CTAs cost what a chunk of 128 rows costs however few there are.  Sequences of 16 rows on average are where the two meet (one
     // sequence, 128 heads of 64 x 128: 8 rows 6.6 us token by token against 9.0, 16 rows 9.5 against 9.0; 33 sequences, 24 heads: 16 rows 15 against 49).
-    if (!str_force_simt() && s->rows > 16LL * s->n_seq && str_scan_packed_tc_supported(s, x, B, C, y))
-        return ++ctx->tc_calls, str_scan_packed_tc(ctx, s, x, dt, A, B, C, D, seq_start, init_state, y, final_state, st);
-    ++ctx->fallback_calls;
-    if (s->dtype == STR_BF16) return dispatch<__nv_bfloat16>(ctx, s, x, dt, A, B, C, D, seq_start, init_state, y, final_state, st);
-    return dispatch<float>(ctx, s, x, dt, A, B, C, D, seq_start, init_state, y, final_state, st);
+    const bool tc = !str_force_simt() && s->rows > 16LL * s->n_seq && str_scan_packed_tc_supported(s, x, B, C, y);
+    ++(tc ? ctx->tc_calls : ctx->fallback_calls);
+    const ScanCall call = {s, s->n_seq, x, B, C, dt, A, D, seq_start, init_state, y, final_state, nullptr};
+    return need ? in_segments(ctx, call, segments_of(s), workspace, tc, st) : pass(ctx, call, tc, st);
 }

@@ -189,7 +189,7 @@ __device__ __noinline__ void scan_rows(const __nv_bfloat16 *x, const float *dt, 
             }
 #pragma unroll
         for (int o = 1; o < 8; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        if (l == 0 && r < p) stf(y + (size_t)t * H * p + r, D != 0.f ? fmaf(D, xv, sum) : sum);
+        if (y && l == 0 && r < p) stf(y + (size_t)t * H * p + r, D != 0.f ? fmaf(D, xv, sum) : sum);
     }
 #pragma unroll
     for (int i = 0; i < 16; ++i)
@@ -220,7 +220,7 @@ scan_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_c
                       const __grid_constant__ CUtensorMap tmap_c, int n_seq, int rows, int H, int p, int n, int G, const float *__restrict__ dt,
                       const float *__restrict__ A, const float *__restrict__ Dskip, const int32_t *__restrict__ start, const __nv_bfloat16 *__restrict__ x,
                       const __nv_bfloat16 *__restrict__ B, const __nv_bfloat16 *__restrict__ C, const float *init_state, __nv_bfloat16 *__restrict__ y,
-                      float *final_state, int *status) {
+                      float *final_state, float *__restrict__ faded, int *status) {
     extern __shared__ __align__(1024) uint8_t smem[];
     float *decs = (float *)(smem + OFF_DEC);
     uint64_t *bars = (uint64_t *)(smem + OFF_BARS);
@@ -249,6 +249,7 @@ scan_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_c
     const float *init = init_state ? init_state + ((size_t)b * H + h) * p * n : nullptr;
     float *fin = final_state ? final_state + ((size_t)b * H + h) * p * n : nullptr;
     if (nchunks == 0) {
+        if (faded && threadIdx.x == 0) faded[(size_t)b * H + h] = 0.f;
         if (fin && fin != init)
             for (int e = threadIdx.x; e < p * n; e += NUM_THREADS) fin[e] = init ? init[e] : 0.f;
         return;
@@ -305,7 +306,7 @@ scan_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_c
             if (nchunks > 1) load_chunk(1);
         }
         __syncwarp();
-        float dv[4], dn[4];
+        float dv[4], dn[4], fade = 0.f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) dn[i] = (4 * lane + i < Tlen) ? __ldg(dtb + (size_t)(4 * lane + i) * H) : 0.f;
 #pragma unroll 1
@@ -332,6 +333,7 @@ scan_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_c
             const float l_start = __shfl_sync(0xffffffffu, excl, lane & ~7);     // start of this 32-token block
             const float l_endb = __shfl_sync(0xffffffffu, incl, lane | 7);       // end of this 32-token block
             const float l_end = __shfl_sync(0xffffffffu, incl, 31);
+            fade += l_end;
             // sums over what comes behind a token: what l_end - l_j is, without the difference of two large numbers
             float tail[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -378,6 +380,7 @@ scan_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_c
                 __syncwarp();
             }
         }
+        if (faded && lane == 0) faded[(size_t)b * H + h] = fade;
         if (!ok && lane == 0) {
             atomicCAS(status, 0, STR_ERR_TIMEOUT);
             for (int back = 1; back <= 2 && back <= n_loaded; ++back) {       // let copies already issued land before the CTA goes away
@@ -621,7 +624,7 @@ scan_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_c
         // ------------------------------------------------------------------ y of chunk c
         const int quad = warp & 3, row = quad * 32 + lane;
         const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
-        __nv_bfloat16 *yb = y + ((size_t)row0 * H + h) * p;
+        __nv_bfloat16 *yb = y + ((size_t)row0 * H + h) * p;   // (y NULL: only the final state and the sum of dt A are wanted)
         const bool wide = p % 16 == 0 && ((uintptr_t)y & 31) == 0;
         bool ok = true;
         if (warp == 8) {
@@ -677,7 +680,7 @@ scan_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_c
                 if (!tc::mbar_wait(bars + B_YF, cp & 1, abort_flag)) { ok = false; break; }
                 tc::tc_fence_after();
                 __nv_bfloat16 *dst = yb + (size_t)(t0 + row) * H * p;
-                const bool valid = t0 + row < Tlen;
+                const bool valid = y && t0 + row < Tlen;
 #pragma unroll 1
                 for (int hf = 0; hf < 2; ++hf) {
                     uint32_t ya[32], yo[32];
@@ -711,18 +714,21 @@ scan_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_c
     if (warp == 13) { tc::tc_fence_after(); tc::tmem_dealloc(tmem, 512); }
     if (found[0])
         scan_rows(x + ((size_t)row0 * H + h) * p, dt + (size_t)row0 * H + h, A[h], B + ((size_t)row0 * G + g) * n, C + ((size_t)row0 * G + g) * n, skip, init,
-                  y + ((size_t)row0 * H + h) * p, fin, Tlen, H, G, p, n);
+                  y ? y + ((size_t)row0 * H + h) * p : nullptr, fin, Tlen, H, G, p, n);
 }
 
 }  // namespace
 
+bool str_scan_packed_tc_shape(const str_ssd_packed_shape *s) {
+    return s->dtype == STR_BF16 && s->p <= P && s->n <= NS && s->p % 8 == 0 && s->n % 8 == 0 && s->rows > 0;
+}
+
 bool str_scan_packed_tc_supported(const str_ssd_packed_shape *s, const void *x, const void *B, const void *C, const void *y) {
-    if (s->dtype != STR_BF16 || s->p > P || s->n > NS || s->p % 8 != 0 || s->n % 8 != 0 || s->rows == 0) return false;
-    return (((uintptr_t)x | (uintptr_t)B | (uintptr_t)C | (uintptr_t)y) & 15) == 0 && (long long)s->H * s->n_seq <= INT32_MAX;
+    return str_scan_packed_tc_shape(s) && (((uintptr_t)x | (uintptr_t)B | (uintptr_t)C | (uintptr_t)y) & 15) == 0 && (long long)s->H * s->n_seq <= INT32_MAX;
 }
 
 int str_scan_packed_tc(str_ctx *ctx, const str_ssd_packed_shape *s, const void *x, const float *dt, const float *A, const void *B, const void *C,
-                       const float *D, const int32_t *start, const float *init_state, void *y, float *final_state, cudaStream_t st) {
+                       const float *D, const int32_t *start, const float *init_state, void *y, float *final_state, float *faded, cudaStream_t st) {
     CUtensorMap tx, tb, tcm;
     int rc = str_make_tmap_heads_bf16_sw128(ctx, &tx, x, s->p, s->H, s->rows, 1, Q);
     if (rc == STR_OK) rc = str_make_tmap_heads_bf16_sw128(ctx, &tb, B, s->n, s->G, s->rows, 1, Q);
@@ -732,6 +738,6 @@ int str_scan_packed_tc(str_ctx *ctx, const str_ssd_packed_shape *s, const void *
     if (rc != STR_OK) return rc;
     scan_packed_tc_kernel<<<s->H * s->n_seq, NUM_THREADS, SMEM_BYTES, st>>>(
         tx, tb, tcm, s->n_seq, s->rows, s->H, s->p, s->n, s->G, dt, A, D, start, (const __nv_bfloat16 *)x, (const __nv_bfloat16 *)B, (const __nv_bfloat16 *)C,
-        init_state, (__nv_bfloat16 *)y, final_state, ctx->status_dev);
+        init_state, (__nv_bfloat16 *)y, final_state, faded, ctx->status_dev);
     return str_launch_ok(ctx);
 }

@@ -317,6 +317,103 @@ def test_scan_does_not_carry_what_is_not_finite_into_other_sequences(ctx):
         assert S2[1].isnan().any()
 
 
+def _segmented(c):
+    """Does the call cut its sequences into segments (it then asks for a workspace)?"""
+    import ctypes
+    rows, H, p = c.x.shape
+    s = binding.SsdPackedShape(len(c.lens), rows, H, p, c.B.shape[2], c.B.shape[1], 1 if c.dtype == "bf16" else 0)
+    return binding.lib().str_mamba2_prefill_packed_workspace_size(ctypes.addressof(s)) > 0
+
+
+LONG_SCAN = [("bf16", (2, 64, 128, 1), [3000]), ("bf16", (4, 32, 64, 2), [2561, 0, 1, 130, 4000]), ("bf16", (1, 16, 16, 1), [1281]), ("bf16", (2, 80, 20, 2), [700, 0, 1]),
+             ("f32", (6, 32, 20, 3), [0, 483, 1, 200]), ("f32", (2, 64, 128, 1), [640]), ("f32", (1, 5, 3, 1), [65, 64, 900, 63]), ("f32", (1, 70, 200, 1), [515])]
+
+
+@pytest.mark.parametrize("skip, state", [(False, False), (True, True)])
+@pytest.mark.parametrize("dtype, dims, lens", LONG_SCAN, ids=str)
+def test_scan_of_long_sequences_of_few_heads(ctx, dtype, dims, lens, skip, state):
+    """Sequences that are walked in segments: as many rows as a segment, one more, empty ones between, rows of nobody around."""
+    g = np.random.default_rng([dims[0], sum(lens), int(skip)])
+    c = Scan(g, lens, dtype, *dims, skip, state, *((0, 0) if skip else (3, 7)))
+    assert _segmented(c)
+    y, S = c.run(ctx)
+    c.check((y, S))
+    assert torch.equal(c.run(ctx, final=False)[: len(c.x)], y)
+    if state:
+        at = dev(c.state)
+        y2, S2 = binding.str_mamba2_prefill_packed(ctx, dev(c.x, dtype), dev(c.dt), dev(c.A), dev(c.B, dtype), dev(c.C, dtype), _i32(c.starts), D=dev(c.D), init_state=at, final_state=at)
+        assert S2 is at and torch.equal(S2, S) and torch.equal(y2, y)
+
+
+@pytest.mark.parametrize("decay", [1e-4, 1e4])
+@pytest.mark.parametrize("dtype, dims, lens", [LONG_SCAN[0], LONG_SCAN[4]], ids=str)
+def test_segments_of_slow_and_fast_decays(ctx, dtype, dims, lens, decay):
+    """Everything from segment to segment, and nothing."""
+    g = np.random.default_rng(17)
+    c = Scan(g, lens, dtype, *dims, True, True)
+    c.A[:] = -decay
+    assert _segmented(c)
+    c.check(c.run(ctx))
+
+
+@pytest.mark.parametrize("dtype, dims, lens, at", [("bf16", (2, 64, 128, 1), [1500], 700), ("f32", (2, 32, 20, 1), [500], 300)], ids=str)
+def test_segments_before_a_value_that_is_not_finite(ctx, dtype, dims, lens, at):
+    """Tokens of earlier segments, and of the same one before the value, are as they would be without it; later ones of its column are not finite."""
+    g = np.random.default_rng(18)
+    c = Scan(g, lens, dtype, *dims, True, True)
+    assert _segmented(c)
+    clean = c.run(ctx)
+    c.check(clean)
+    for value in (np.nan, np.inf):
+        c.x[at, 1, 7] = value
+        y, S = (_f64(t) for t in c.run(ctx))
+        ref, ymag, _, _ = packed.scan(c.x[:at], c.dt[:at], c.A, c.B[:at], c.C[:at], c.D, [0, at], c.state)
+        walk = (lens[0] + 64) * 2.0 ** -21
+        rel = 2 * HALF["bf16"] + 2.0 ** -12 + walk if dtype == "bf16" else walk
+        assert (np.abs(y[:at] - ref) <= rel * ymag + HALF[dtype] * np.abs(ref)).all()
+        assert not np.isfinite(y[at:, 1, 7]).any() and np.isfinite(np.delete(y[:, 1], 7, 1)).all() and (y[:, 0] == _f64(clean[0])[:, 0]).all()
+        assert not np.isfinite(S[0, 1, 7]).any() and np.isfinite(np.delete(S[0, 1], 7, 0)).all()
+
+
+def test_segments_in_two_graphs_at_once_and_the_same_bits(ctx):
+    g = np.random.default_rng(19)
+    for dtype, dims, lens in (LONG_SCAN[0], LONG_SCAN[4]):
+        runs = []
+        for _ in range(2):
+            c = Scan(g, lens, dtype, *dims, False, True)
+            args = (dev(c.x, dtype), dev(c.dt), dev(c.A), dev(c.B, dtype), dev(c.C, dtype), _i32(c.starts))
+            init, final = dev(c.state), dev(c.state)
+            call = lambda args=args, init=init, final=final: binding.str_mamba2_prefill_packed(ctx, *args, init_state=init, final_state=final)  # noqa: E731
+            want = [t.clone() for t in call()]
+            final.zero_()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph):
+                got = call()
+            runs.append((graph, torch.cuda.Stream(), got, want, args, init))
+        for _ in range(4):
+            for graph, stream, *_ in runs:
+                with torch.cuda.stream(stream):
+                    graph.replay()
+        torch.cuda.synchronize()
+        for _, _, got, want, _, _ in runs:
+            assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("starts", [[0, 900, 200], [-3, 10, 4000000], [0, 2147483647, 2147483647], [1400, 1400, -2147483648], [1500, 0, 1500]], ids=str)
+def test_wrong_starts_of_segments(ctx, starts):
+    g = np.random.default_rng(20)
+    for dtype, dims in (("bf16", (2, 64, 128, 1)), ("f32", (2, 32, 20, 1))):
+        c = Scan(g, [1400, 1500], dtype, *dims, False, True)
+        assert _segmented(c)
+        right, c.starts = c.starts, starts
+        c.run(ctx)
+        with pytest.raises(binding.StrError):
+            ctx.check_status()
+        ctx.check_status()
+        c.starts = right
+        c.check(c.run(ctx))
+
+
 # ------------------------------------------------------------------------------------------------ attention
 class Attend:
     def __init__(self, g, lq, lk, dtype, Hq, Hkv, d, first=(0, 0), tail=0, gain=1.0):

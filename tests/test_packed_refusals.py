@@ -95,6 +95,29 @@ def test_scan():
 
 
 @no_device
+def test_scan_workspace():
+    """Long sequences of few heads ask for one; too small, missing, misaligned or shared with another tensor it is refused."""
+    names = ("x", "dt", "A", "B", "C", "D", "start", "init", "y", "final")
+
+    def call(ws, given, **at):
+        c = Call()
+        s = binding.SsdPackedShape(1, 2000, 4, 64, 128, 2, 1)
+        need = binding.lib().str_mamba2_prefill_packed_workspace_size(ctypes.addressof(s))
+        assert need > 0
+        return binding.lib().str_mamba2_prefill_packed(ctypes.addressof(c.ctx), ctypes.addressof(s), *(at.get(n) or c.buffer() for n in names), ws, need + given, None)
+
+    at = 1 << 44
+    assert call(at, 0) == NO_DEVICE and call(at, -1) == -3 and call(None, 0) == INVALID and call(at + 128, 0) == INVALID
+    for name in ("x", "dt", "B", "C", "init", "y", "final"):
+        assert call(at, 0, **{name: at + 256}) == INVALID, name
+    for shape in ((1, 1000, 4, 64, 128, 2, 1), (1, 24576, 128, 64, 128, 8, 1), (1, 100, 4, 64, 128, 2, 0), (200, 20000, 4, 64, 128, 2, 1), (1, 0, 4, 64, 128, 2, 1), (0, 2000, 4, 64, 128, 2, 1),
+                  (1, 2000, 4, 64, 257, 2, 1)):
+        s = binding.SsdPackedShape(*shape)
+        assert binding.lib().str_mamba2_prefill_packed_workspace_size(ctypes.addressof(s)) == 0, shape
+    assert binding.lib().str_mamba2_prefill_packed_workspace_size(None) == 0
+
+
+@no_device
 def test_attention():
     assert Call().attn() == NO_DEVICE
     for bad in (dict(n_seq=0), dict(rows_q=-1), dict(rows_k=-1), dict(Hq=0), dict(Hkv=0), dict(Hq=3), dict(d=0), dict(dtype=2), dict(q=None), dict(k=None), dict(v=None),
