@@ -2,14 +2,16 @@
 //   S <- exp(dt A_h) S + (dt x) b^T,   y = S c + D_h x.
 // The entry point, and the kernel that runs the recurrence token by token in fp32: every type and shape.
 //
-// A row of the state (one of p) lies across four lanes, NV vectors of four columns each; a block holds the rows of one head of one
+// Two rows of the state (of p) lie across four or eight lanes, NV vectors of four columns each; a block holds the rows of one head of one
 // sequence in registers from the first token to the last.  Tokens come through shared memory TB at a time; the next ones are already on their way to
-// registers.  A lane leaves its part of y in shared memory, and the four parts are added when the tokens' outputs are written: no shuffles between
-// tokens, whose chain is then one fused operation a token.  Per token and head that is p n (one multiplication and two fused ones): as many
-// operations as the chunked form in fp32 needs, without its two roundings more, and a state that never leaves the registers.
+// registers.  A lane leaves its part of y in shared memory, half of a row's lanes after one exchange with the other half's, and the parts are added when
+// the tokens' outputs are written; the chain from token to token is one fused operation.  Per token and head that is p n (one multiplication and two
+// fused ones, two elements an instruction): as many operations as the chunked form in fp32 needs, without its two roundings more, and a state that never
+// leaves the registers.
 //
-// Bound by the chain of tokens where sequences are few (five turns of 1237 rows, 24 heads of 32 x 20: 67 us, 120 ns a token of the longest), by fp32
-// arithmetic and the reading of b and c from shared memory where there are many (5000 rows, 128 heads of 64 x 128: 1.88 ms, 17 TFLOP/s).
+// Bound by the reading of b and c from shared memory: two rows a lane, so that a vector read serves eight fused operations (one row a lane: 1.88 ms where
+// two take 1.22, 25.8 TFLOP/s, 5000 rows, 128 heads of 64 x 128), and several tokens' reads before the first one's output is stored.  Few sequences are
+// bound by the chain of tokens, 77 ns each, whence the segments below (five turns of 1237 rows, the longest 547, 24 heads of 32 x 20: 30 us, whole 45).
 #include <algorithm>
 
 #include "dispatch.cuh"
@@ -17,47 +19,52 @@
 
 namespace {
 
-constexpr int LPR = 4;                                    // lanes per row
-// Tokens per turn: as many as their b, c and outputs leave registers for.
-template <int NV> constexpr int TOKENS = NV <= 4 ? 32 : 16;
+// Tokens per turn: as many as their b, c and outputs leave registers for.  Tokens at a time, whose outputs are kept until all are formed: a store
+// between two tokens would hold up the second one's reads.
+template <int NV> constexpr int TOKENS = NV <= 2 ? 32 : 16;
+template <int NV> constexpr int TOGETHER = NV <= 1 ? 8 : NV <= 2 ? 4 : 2;
 
 // Y: outputs are wanted; else the final state and the sum of dt A (in powers of two) of every sequence are.
-template <typename T, int NV, int WARPS, bool Y>
+template <typename T, int NV, int LPR, int WARPS, bool Y>
 __global__ void __launch_bounds__(32 * WARPS)
 scan_packed_kernel(int n_seq, int rows, int H, int p, int n, int G, const T *__restrict__ x, const float *__restrict__ dt, const float *__restrict__ A,
                    const T *__restrict__ B, const T *__restrict__ C, const float *__restrict__ Dskip, const int32_t *__restrict__ start,
                    const float *state, T *__restrict__ y, float *final_state, float *__restrict__ faded, int *status) {
-    constexpr int NP = NV * 4 * LPR, TB = TOKENS<NV>;     // columns, padded; tokens per turn
-    constexpr int threads = 32 * WARPS, R = threads / LPR; // rows of the state per block
+    constexpr int NP = NV * 4 * LPR, TB = TOKENS<NV>, TG = TOGETHER<NV>;  // columns, padded; tokens per turn, at a time
+    constexpr int threads = 32 * WARPS, R = threads / LPR * 2, PARTS = LPR / 2; // rows of the state per block; what a row's sums come in
     extern __shared__ float4 smem4[];
-    float *bs = (float *)smem4, *cs = bs + TB * NP, *xs = cs + TB * NP;
-    float *ys = xs + TB * R, *dts = ys + TB * R * LPR, *decay = dts + TB;
+    float *bs = (float *)smem4, *cs = bs + TB * NP, *ys = cs + TB * NP, *xs = ys + TB * threads;
+    float2 *rate = (float2 *)(xs + TB * R);               // dt, exp(dt A)
     const int h = blockIdx.y, s = blockIdx.z, g = h / (H / G);
-    const int tid = threadIdx.x, i0 = blockIdx.x * R, r = tid / LPR, l = tid % LPR;
+    const int tid = threadIdx.x, i0 = blockIdx.x * R, r = tid / LPR * 2, l = tid % LPR;
     if (blockIdx.x == 0 && h == 0 && s == 0) packed_check(start, n_seq, rows, status);
     const int t0 = packed_start(start, s, rows), t1 = packed_start(start, s + 1, rows);
     if (t1 <= t0 && (Y ? !final_state || state == final_state : false)) return;
     const size_t base = (((size_t)s * H + h) * p + i0 + r) * n;
     // Four columns at a time where a row has whole vectors of them.
     const bool vec = n % 4 == 0 && (((uintptr_t)state | (uintptr_t)final_state) & 15) == 0;
-    alignas(16) float S[NV][4];
+    alignas(16) float2 S[2][NV][2];
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-        const int col = (v * LPR + l) * 4;
+    for (int j = 0; j < 2; ++j)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) S[v][i] = 0.f;
-        if (state && i0 + r < p && col < n) {
-            if (vec) *(float4 *)S[v] = *(const float4 *)(state + base + col);
-            else
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (col + i < n) S[v][i] = state[base + col + i];
+        for (int v = 0; v < NV; ++v) {
+            const int col = (v * LPR + l) * 4;
+            const float *from = state + base + (size_t)j * n + col;
+            S[j][v][0] = S[j][v][1] = make_float2(0.f, 0.f);
+            if (state && i0 + r + j < p && col < n) {
+                if (vec) *(float4 *)S[j][v] = *(const float4 *)from;
+                else {
+                    S[j][v][0].x = from[0];
+                    if (col + 1 < n) S[j][v][0].y = from[1];
+                    if (col + 2 < n) S[j][v][1].x = from[2];
+                    if (col + 3 < n) S[j][v][1].y = from[3];
+                }
+            }
         }
-    }
     const float Ah = A[h], Dh = Dskip ? Dskip[h] : 0.f;
     // What the thread carries of the next TB tokens: elements tid + k threads of [TB][NP] and of [TB][R].
-    constexpr int PER = TB * NP / threads;
-    T bq[PER], cq[PER], xq[TB / LPR];
+    constexpr int PER = TB * NP / threads, PER_X = TB * R / threads;
+    T bq[PER], cq[PER], xq[PER_X];
     float dq = 0.f, fade = 0.f;
     auto fetch = [&](int tb) {
         const int m = min(TB, t1 - tb);
@@ -73,7 +80,7 @@ scan_packed_kernel(int n_seq, int rows, int H, int p, int n, int G, const T *__r
             }
         }
 #pragma unroll
-        for (int k = 0; k < TB / LPR; ++k) {
+        for (int k = 0; k < PER_X; ++k) {
             const int e = tid + k * threads, t = e / R, i = e % R;
             stf(&xq[k], 0.f);
             if (t < m && i0 + i < p) xq[k] = x[((size_t)(tb + t) * H + h) * p + i0 + i];
@@ -89,41 +96,71 @@ scan_packed_kernel(int n_seq, int rows, int H, int p, int n, int G, const T *__r
             if (Y) cs[tid + k * threads] = ldf(&cq[k]);
         }
 #pragma unroll
-        for (int k = 0; k < TB / LPR; ++k) xs[tid + k * threads] = ldf(&xq[k]);
+        for (int k = 0; k < PER_X; ++k) xs[tid + k * threads] = ldf(&xq[k]);
         if (tid < m) {
-            dts[tid] = dq;
-            decay[tid] = expf(dq * Ah);
+            rate[tid] = make_float2(dq, expf(dq * Ah));
             if (!Y) fade = fmaf(dq, Ah * 1.4426950408889634f, fade);
         }
         __syncthreads();
         if (tb + TB < t1) fetch(tb + TB);
-#pragma unroll (NV >= 8 ? 2 : 4)
-        for (int t = 0; t < m; ++t) {
-            const float dx = dts[t] * xs[t * R + r], a = decay[t];
-            float acc[4] = {0.f, 0.f, 0.f, 0.f};
+        auto token = [&](int t) -> float {                // one token; its output's part that this thread leaves
+            const float2 da = rate[t], xv = *(const float2 *)(xs + t * R + r), a = make_float2(da.y, da.y);
+            const float2 dx[2] = {make_float2(da.x * xv.x, da.x * xv.x), make_float2(da.x * xv.y, da.x * xv.y)};
+            float2 acc[2][2];
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
                 const float4 b = *(const float4 *)(bs + t * NP + (v * LPR + l) * 4);
-                S[v][0] = fmaf(a, S[v][0], dx * b.x);
-                S[v][1] = fmaf(a, S[v][1], dx * b.y);
-                S[v][2] = fmaf(a, S[v][2], dx * b.z);
-                S[v][3] = fmaf(a, S[v][3], dx * b.w);
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    S[j][v][0] = __ffma2_rn(a, S[j][v][0], __fmul2_rn(dx[j], make_float2(b.x, b.y)));
+                    S[j][v][1] = __ffma2_rn(a, S[j][v][1], __fmul2_rn(dx[j], make_float2(b.z, b.w)));
+                }
                 if (Y) {
                     const float4 c = *(const float4 *)(cs + t * NP + (v * LPR + l) * 4);
-                    acc[0] = fmaf(S[v][0], c.x, acc[0]);
-                    acc[1] = fmaf(S[v][1], c.y, acc[1]);
-                    acc[2] = fmaf(S[v][2], c.z, acc[2]);
-                    acc[3] = fmaf(S[v][3], c.w, acc[3]);
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        acc[j][0] = v == 0 ? __fmul2_rn(S[j][v][0], make_float2(c.x, c.y)) : __ffma2_rn(S[j][v][0], make_float2(c.x, c.y), acc[j][0]);
+                        acc[j][1] = v == 0 ? __fmul2_rn(S[j][v][1], make_float2(c.z, c.w)) : __ffma2_rn(S[j][v][1], make_float2(c.z, c.w), acc[j][1]);
+                    }
                 }
             }
-            if (Y) ys[t * threads + tid] = (acc[0] + acc[1]) + (acc[2] + acc[3]);
+            if (Y) {                                  // of two neighbours one keeps the first row's sum of both, the other the second's
+                const float2 s0 = __fadd2_rn(acc[0][0], acc[0][1]), s1 = __fadd2_rn(acc[1][0], acc[1][1]);
+                const float o0 = s0.x + s0.y, o1 = s1.x + s1.y;
+                return (l & 1 ? o1 : o0) + __shfl_xor_sync(0xffffffffu, l & 1 ? o0 : o1, 1);
+            }
+            return 0.f;
+        };
+        auto part = [&](int t) -> float & { return ys[(t * R + r + (l & 1)) * PARTS + (l >> 1)]; };
+        int tg = 0;
+#pragma unroll 1
+        for (; tg + TG <= m; tg += TG) {
+            float out[TG];
+#pragma unroll
+            for (int u = 0; u < TG; ++u) out[u] = token(tg + u);
+            if (Y)
+#pragma unroll
+                for (int u = 0; u < TG; ++u) part(tg + u) = out[u];
+        }
+#pragma unroll 1
+        for (; tg < m; ++tg) {
+            const float out = token(tg);
+            if (Y) part(tg) = out;
         }
         __syncthreads();
         if (Y) {
-            for (int e = tid; e < m * R; e += threads) {
-                const int t = e / R, i = e % R;
-                const float4 part = *(const float4 *)(ys + e * LPR);
-                if (i0 + i < p) stf(y + ((size_t)(tb + t) * H + h) * p + i0 + i, fmaf(Dh, xs[e], (part.x + part.y) + (part.z + part.w)));
+#pragma unroll
+            for (int k = 0; k < PER_X; ++k) {
+                const int e = tid + k * threads, t = e / R, i = e % R;
+                float sum;
+                if constexpr (PARTS == 4) {
+                    const float4 part = *(const float4 *)(ys + e * PARTS);
+                    sum = (part.x + part.y) + (part.z + part.w);
+                } else {
+                    const float2 part = *(const float2 *)(ys + e * PARTS);
+                    sum = part.x + part.y;
+                }
+                if (t < m && i0 + i < p) stf(y + ((size_t)(tb + t) * H + h) * p + i0 + i, fmaf(Dh, xs[e], sum));
             }
             __syncthreads();
         }
@@ -132,16 +169,22 @@ scan_packed_kernel(int n_seq, int rows, int H, int p, int n, int G, const T *__r
         fade = warp_sum(fade);
         if (tid == 0) faded[(size_t)s * H + h] = fade;
     }
-    if (!final_state || i0 + r >= p) return;
+    if (!final_state) return;
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-        const int col = (v * LPR + l) * 4;
-        if (vec && col < n) *(float4 *)(final_state + base + col) = *(const float4 *)S[v];
-        if (!vec)
+    for (int j = 0; j < 2; ++j)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (col + i < n) final_state[base + col + i] = S[v][i];
-    }
+        for (int v = 0; v < NV; ++v) {
+            const int col = (v * LPR + l) * 4;
+            float *to = final_state + base + (size_t)j * n + col;
+            if (i0 + r + j >= p || col >= n) continue;
+            if (vec) *(float4 *)to = *(const float4 *)S[j][v];
+            else {
+                to[0] = S[j][v][0].x;
+                if (col + 1 < n) to[1] = S[j][v][0].y;
+                if (col + 2 < n) to[2] = S[j][v][1].x;
+                if (col + 3 < n) to[3] = S[j][v][1].y;
+            }
+        }
 }
 
 // Arguments of a call, or of one of its two passes.
@@ -155,23 +198,23 @@ struct ScanCall {
     void *y;
     float *final_state, *faded;
 };
-template <typename T, int NV, int WARPS>
+template <typename T, int NV, int LPR, int WARPS>
 int launch(str_ctx *ctx, const ScanCall &k, cudaStream_t st) {
     const str_ssd_packed_shape *s = k.s;
-    constexpr int TB = TOKENS<NV>, threads = 32 * WARPS, R = threads / LPR;
+    constexpr int TB = TOKENS<NV>, threads = 32 * WARPS, R = threads / LPR * 2;
     constexpr size_t smem = sizeof(float) * ((size_t)TB * (2 * NV * 4 * LPR + R + threads) + 2 * TB);
-    auto *kernel = k.y ? scan_packed_kernel<T, NV, WARPS, true> : scan_packed_kernel<T, NV, WARPS, false>;
+    auto *kernel = k.y ? scan_packed_kernel<T, NV, LPR, WARPS, true> : scan_packed_kernel<T, NV, LPR, WARPS, false>;
     if (smem > 48 * 1024) STR_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     kernel<<<dim3(ceil_div(s->p, R), s->H, k.n_seq), threads, smem, st>>>(k.n_seq, s->rows, s->H, s->p, s->n, s->G, (const T *)k.x, k.dt, k.A, (const T *)k.B, (const T *)k.C, k.D,
                                                                          k.start, k.state, (T *)k.y, k.final_state, k.faded, ctx->status_dev);
     return str_launch_ok(ctx);
 }
-// Four warps hold 32 rows of a head, eight 64.
+// Blocks of 32 rows of a head, or of 64: four warps or eight, half of that where four lanes hold a row.
 template <typename T>
 int dispatch(str_ctx *ctx, const ScanCall &k, cudaStream_t st) {
-    const int need = ceil_div(k.s->n, 4 * LPR);
-#define SCAN(NV) (k.s->p <= 32 && NV < 16 ? launch<T, NV, 4>(ctx, k, st) : launch<T, NV, 8>(ctx, k, st))
-    return need <= 1 ? SCAN(1) : need <= 2 ? SCAN(2) : need <= 4 ? SCAN(4) : need <= 8 ? SCAN(8) : SCAN(16);
+    const int n = k.s->n;
+#define SCAN(NV, LPR) (k.s->p <= 32 && NV < 8 ? launch<T, NV, LPR, LPR / 2>(ctx, k, st) : launch<T, NV, LPR, LPR>(ctx, k, st))
+    return n <= 16 ? SCAN(1, 4) : n <= 32 ? SCAN(1, 8) : n <= 64 ? SCAN(2, 8) : n <= 128 ? SCAN(4, 8) : SCAN(8, 8);
 #undef SCAN
 }
 int pass(str_ctx *ctx, const ScanCall &k, bool tc, cudaStream_t st) {
@@ -191,20 +234,21 @@ int pass(str_ctx *ctx, const ScanCall &k, bool tc, cudaStream_t st) {
 struct Segments {
     int len, n;                  // rows of one, number of them at most; len 0: sequences are walked whole
 };
-constexpr int SMS = 148, MAX_SEGMENTS = 4 * SMS;
+constexpr int SMS = 148;
 Segments segments_of(const str_ssd_packed_shape *s) {
     const bool tc = str_scan_packed_tc_shape(s);
-    // Blocks that run at a time, those of one sequence, and the shortest segment that is worth a pass (token by token 64 rows, 8 us; 24 heads of 32 x 20: one
-    // sequence of 256 rows 31 us whole, 21 in fours, one of 128 rows 17 whole, 20 in halves; chunked 512 rows, of which a CTA's start and end are a third).
+    // Blocks that run at a time, those of one sequence, and the shortest segment that is worth a pass (token by token 64 rows, 5 us: 24 heads of 32 x 20, one
+    // sequence of 256 rows 18.8 us in fours, 21.9 whole; chunked 512 rows, of which a CTA's start and end are a third).
     const int rows_at_a_time = s->p <= 32 && s->n <= 128 ? 32 : 64;
     const long long room = tc ? SMS : s->n > 128 ? SMS : s->p > 32 ? 2 * SMS : 4 * SMS, least = tc ? 512 : 64;
     const long long per = (long long)s->H * (tc ? 1 : ceil_div(s->p, rows_at_a_time));
     const long long more = room / per - s->n_seq;         // segments beside the one that every sequence ends with
     if (more < 1) return {0, 0};
-    const long long len = align_up((size_t)std::max<long long>((s->rows + more - 1) / more, least), tc ? 128 : 32);
-    // Two passes over a segment against one over the sequence: two and a half segments a sequence on average are where they meet (chunked, 24 heads: two
-    // sequences of 5000 rows in 2 segments each 121 us, whole 101; one of 2000 in 4: 45, whole 60).
-    if (2LL * s->rows < 5 * len * s->n_seq) return {0, 0};
+    const long long len = align_up((size_t)std::max<long long>((s->rows + more - 1) / more, least), tc ? 128 : 4);
+    // Two passes over a segment against one over the sequence: two and a half segments are where they meet (chunked, 24 heads: one sequence of 2000 rows in 4
+    // 44 us, whole 60).  Several sequences are seldom of one length, and the longest is what is waited for: there somewhat fewer on average will do (16 heads,
+    // sequences of 20000, 3000 and 1000 rows 158 us, whole 365; two of 5000, 24 heads, 121, whole 101).
+    if (s->n_seq == 1 ? 2LL * s->rows < 5 * len : 8LL * s->rows < 15 * len * s->n_seq) return {0, 0};
     return {(int)len, (int)(s->rows / len + s->n_seq)};
 }
 struct Workspace {
@@ -221,7 +265,7 @@ struct Workspace {
     }
 };
 
-// One block: the segments of all sequences, in their order.  (n_seq < MAX_SEGMENTS.)
+// One block: the segments of all sequences, in their order.  (n_seq < 4 * SMS.)
 __global__ void __launch_bounds__(1024) segments_kernel(int n_seq, int rows, Segments g, const int32_t *__restrict__ start, int32_t *__restrict__ seg_start,
                                                         int32_t *__restrict__ first, int *status) {
     __shared__ int upto[1024];
@@ -336,9 +380,10 @@ extern "C" int str_mamba2_prefill_packed(str_ctx *ctx, const str_ssd_packed_shap
     if (!dev.ok) return STR_ERR_CUDA;
     StrProfScope prof_scope(ctx, STR_CAT_SSD, stream);
     cudaStream_t st = (cudaStream_t)stream;
-    // The chunked kernel's CTAs cost what a chunk of 128 rows costs however few there are.  Sequences of 16 rows on average are where the two meet (one
-    // sequence, 128 heads of 64 x 128: 8 rows 6.6 us token by token against 9.0, 16 rows 9.5 against 9.0; 33 sequences, 24 heads: 16 rows 15 against 49).
-    const bool tc = !str_force_simt() && s->rows > 16LL * s->n_seq && str_scan_packed_tc_supported(s, x, B, C, y);
+    // The chunked kernel's CTAs cost what a chunk of 128 rows costs however few there are.  Sequences of 32 rows on average are where the two meet (128 heads of
+    // 64 x 128: one sequence of 32 rows 10.3 us token by token, 10.4 chunked, of 64 rows 17.9 and 10.6; 33 sequences of 32 rows 204 and 276, of 64 rows 387 and
+    // 277; 24 heads of 32 x 64: one of 32 rows 5.5 and 9.2).
+    const bool tc = !str_force_simt() && s->rows > 32LL * s->n_seq && str_scan_packed_tc_supported(s, x, B, C, y);
     ++(tc ? ctx->tc_calls : ctx->fallback_calls);
     const ScanCall call = {s, s->n_seq, x, B, C, dt, A, D, seq_start, init_state, y, final_state, nullptr};
     return need ? in_segments(ctx, call, segments_of(s), workspace, tc, st) : pass(ctx, call, tc, st);

@@ -282,7 +282,7 @@ def test_final_states_of_sequences_whose_last_tokens_count(ctx):
 def test_scan_of_short_and_long_sequences_side_by_side(ctx):
     """Averages on both sides of the length from which the chunked kernel is taken, with and without decay to fade a chunk."""
     g = np.random.default_rng(15)
-    for lens in ([16, 16], [17, 16], [1, 40, 2], [500, 0, 1, 3, 2]):
+    for lens in ([16, 16], [17, 16], [32, 32], [33, 32], [1, 40, 2], [500, 0, 1, 3, 2]):
         for decay in (1e-3, 16.0):
             c = Scan(g, lens, "bf16", 3, 64, 128, 1, True, True, decay=max(decay, 1.0))
             if decay < 1:
