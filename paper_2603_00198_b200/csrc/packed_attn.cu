@@ -3,8 +3,8 @@
 //
 // One pass over the keys with the running maximum and sum of the softmax.  The BR rows of a block are (query, head) pairs: the queries of a
 // key head's group lie in one block, so that its keys and values are fetched once for all of them.  Bound by fp32 arithmetic: both products
-// are formed two elements an instruction, from 16-byte pieces of shared memory (4000 rows, 12 / 4 heads of 128: 1.36 ms, 36 TFLOP/s, half of what the
-// FMA pipes do; half of shared memory's bandwidth goes with it).
+// are formed two elements an instruction, from 16-byte pieces of shared memory (4000 rows, 12 / 4 heads of 128: 1.31 ms, 38 TFLOP/s, half of what the
+// FMA pipes do; half of shared memory's bandwidth goes with it).  Unrolled so far that reads run ahead of the products (by 2 and 2: 1.36 ms).
 #include <math.h>
 
 #include "dispatch.cuh"
@@ -116,7 +116,7 @@ attn_packed_simt_kernel(int n_seq, int rows_q, int rows_k, int Hq, int Hkv, int 
         for (int a = 0; a < 8; ++a)
 #pragma unroll
             for (int j = 0; j < 4; ++j) s2[a][j] = make_float2(0.f, 0.f);
-#pragma unroll 2
+#pragma unroll 4
         for (int c = 0; c < DP; c += 4) {
             float4 kk[4];
 #pragma unroll
@@ -176,7 +176,7 @@ attn_packed_simt_kernel(int n_seq, int rows_q, int rows_k, int Hq, int Hkv, int 
             careful = __syncthreads_or(odd);
         }
         if (!careful) {
-#pragma unroll 2
+#pragma unroll 8
             for (int j = 0; j < BC; j += 4) {
                 float4 vv[4][DC];
 #pragma unroll
@@ -243,12 +243,16 @@ int launch(str_ctx *ctx, const str_attn_packed_shape *s, const void *q, const vo
 }
 
 // Small heads: blocks of 64 rows, three of which fit an SM; blocks of 128 where a group needs them or the head is wide (one block fits, and has to
-// bring its warps along).
+// bring its warps along), but 64 for wide heads too where blocks of 128 would not reach every SM (4 / 4 heads of 128: 1000 rows 148 us against 231,
+// 4000 rows of 12 / 4 heads, 380 blocks of 128, 1466 against 1306).
 template <typename T>
 int dispatch(str_ctx *ctx, const str_attn_packed_shape *s, const void *q, const void *k, const void *v, const int32_t *q_start, const int32_t *k_start,
              float scale, void *o, cudaStream_t st) {
+    const int group = s->Hq / s->Hkv;
+    const bool few = group <= 64 && ((long long)s->rows_q / (128 / group) + s->n_seq) * s->Hkv <= ctx->sm_count;
+    if (s->d > 64 && few) return launch<T, 128, 64>(ctx, s, q, k, v, q_start, k_start, scale, o, st);
     if (s->d > 64) return launch<T, 128, 128>(ctx, s, q, k, v, q_start, k_start, scale, o, st);
-    if (s->Hq / s->Hkv > 64) return launch<T, 64, 128>(ctx, s, q, k, v, q_start, k_start, scale, o, st);
+    if (group > 64) return launch<T, 64, 128>(ctx, s, q, k, v, q_start, k_start, scale, o, st);
     return launch<T, 64, 64>(ctx, s, q, k, v, q_start, k_start, scale, o, st);
 }
 

@@ -611,6 +611,15 @@ def test_attention_without_key_starts_is_that_of_the_unpacked_call(ctx):
     assert (a.flatten(0, 1).double() - b.double()).abs().max() <= 2.0 ** -6
 
 
+@pytest.mark.parametrize("Hq, Hkv, d", [(4, 2, 128), (3, 3, 80), (6, 2, 100)])
+def test_fp32_attention_of_few_and_of_many_blocks_of_wide_heads(ctx, Hq, Hkv, d):
+    """Blocks of 64 rows and of 128."""
+    g = np.random.default_rng(26)
+    for lens in ([200, 0, 65], [int(v) for v in g.integers(0, 5, 160)] + [70, 300]):
+        c = Attend(g, lens, [v + int(w) for v, w in zip(lens, g.integers(0, 90, len(lens)))], "f32", Hq, Hkv, d, (1, 2), 3)
+        c.check(c.run(ctx))
+
+
 def test_attention_of_many_sequences_and_groups_as_large_as_a_block(ctx):
     g = np.random.default_rng(25)
     lens = [int(v) for v in g.integers(0, 6, 500)]
