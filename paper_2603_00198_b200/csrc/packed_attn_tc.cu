@@ -49,17 +49,18 @@ template <int HD> struct Smem {
 };
 
 // 2^x of two numbers on the FMA pipe: x = n + f with n the nearest whole number, a cubic in f on [-1/2, 1/2] (minimax, relative error 7.5e-5: a
-// fiftieth of the rounding to bf16 that follows), and n added to the exponent.  x <= 2^7; below -126 it stays at 2^-126.
+// fiftieth of the rounding to bf16 that follows), and n added to the exponent.  x <= 2^7; below -126 it is zero, as the special-function unit's is: a
+// hidden key's weight (x minus infinity) has to be nothing, whatever it is multiplied by.
 __device__ __forceinline__ float2 ex2_poly(float2 x) {
     const float2 magic = make_float2(12582912.f, 12582912.f);         // 1.5 * 2^23: the sum's last bits are the whole number
-    x = make_float2(fmaxf(x.x, -126.f), fmaxf(x.y, -126.f));
     const float2 t = __fadd2_rn(x, magic);
     const float2 n = __fadd2_rn(t, make_float2(-12582912.f, -12582912.f));
     const float2 f = __ffma2_rn(n, make_float2(-1.f, -1.f), x);
     float2 p = __ffma2_rn(make_float2(0.05517166853f, 0.05517166853f), f, make_float2(0.24261112511f, 0.24261112511f));
     p = __ffma2_rn(p, f, make_float2(0.69326096773f, 0.69326096773f));
     p = __ffma2_rn(p, f, make_float2(0.99992805719f, 0.99992805719f));
-    return make_float2(__uint_as_float(__float_as_uint(p.x) + (__float_as_uint(t.x) << 23)), __uint_as_float(__float_as_uint(p.y) + (__float_as_uint(t.y) << 23)));
+    return make_float2(x.x < -126.f ? 0.f : __uint_as_float(__float_as_uint(p.x) + (__float_as_uint(t.x) << 23)),
+                       x.y < -126.f ? 0.f : __uint_as_float(__float_as_uint(p.y) + (__float_as_uint(t.y) << 23)));
 }
 
 // Weights of 64 keys, exp2(scale (s - m)), narrowed and in pairs; their sum is added up as it was before.

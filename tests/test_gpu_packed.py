@@ -639,6 +639,58 @@ def test_attention_of_no_keys_at_all(ctx):
     assert binding.str_attn_prefill_packed(ctx, q[:0], q[:0], q[:0], _i32([0, 0]), 0.1).shape == (0, 2, 64)
 
 
+HUGE = {"bf16": 3.3e38, "f32": 3.4e38}
+
+
+@pytest.mark.parametrize("lq, lk", [([200], [200]), ([150, 40], [400, 40]), ([5, 9], [140, 0]), ([20], [2000]), ([9, 9], [4000, 6])], ids=str)
+@pytest.mark.parametrize("dtype, Hq, Hkv, d", [("bf16", 8, 2, 128), ("bf16", 2, 1, 64), ("bf16", 3, 3, 80), ("bf16", 2, 1, 20), ("f32", 3, 1, 64)])
+def test_attention_hidden_values_of_the_largest_magnitude_weigh_nothing(ctx, dtype, Hq, Hkv, d, lq, lk):
+    """The second half of each sequence's queries see such values, the first half's rows have the bits that they have without them."""
+    g = np.random.default_rng([29, Hq, d])
+    c = Attend(g, lq, lk, dtype, Hq, Hkv, d)
+    assert dtype == "f32" or d == 20 or Hq == 8 or lk[0] < 2000 or _shared(c)
+    clean = c.run(ctx)
+    keep = torch.zeros(sum(lq), dtype=torch.bool)
+    for s, (a, b) in enumerate(zip(lq, lk)):
+        keep[c.qs[s]:c.qs[s] + a - a // 2] = True
+        c.v[max(c.ks[s], c.ks[s + 1] - a // 2):c.ks[s + 1]] = inputs.to_grid(np.array(HUGE[dtype]), dtype)
+    assert torch.equal(c.run(ctx)[keep], clean[keep])
+    c.v[:] = np.where(np.abs(c.v) > 1e38, -c.v, c.v)
+    assert torch.equal(c.run(ctx)[keep], clean[keep])
+
+
+@pytest.mark.parametrize("lq, lk", [([200], [200]), ([7], [300]), ([3], [2100])], ids=str)
+@pytest.mark.parametrize("dtype, Hq, Hkv, d", [("bf16", 4, 1, 128), ("bf16", 2, 1, 64), ("bf16", 2, 1, 20), ("f32", 3, 1, 64)])
+def test_attention_values_whose_weights_underflow_weigh_nothing(ctx, dtype, Hq, Hkv, d, lq, lk):
+    """Every second key is seen with a score of -640 or less below the others': exp of that is 2^-923, and times the largest value still zero."""
+    g = np.random.default_rng([30, d])
+    c = Attend(g, lq, lk, dtype, Hq, Hkv, d)
+    c.scale = 1.0
+    c.q[:], c.k[::2], c.k[1::2] = 1.0, 0.0, -32.0
+    c.v[1::2] = 0.0
+    clean = c.run(ctx)
+    c.v[1::2] = inputs.to_grid(np.array(HUGE[dtype]), dtype)
+    assert torch.equal(c.run(ctx), clean)
+
+
+@pytest.mark.parametrize("lq, lk", [([150, 30], [150, 30]), ([100], [400]), ([3], [2100])], ids=str)
+@pytest.mark.parametrize("dtype, Hq, Hkv, d", [("bf16", 4, 1, 128), ("bf16", 2, 1, 64), ("f32", 3, 1, 64)])
+def test_attention_scores_of_minus_infinity(ctx, dtype, Hq, Hkv, d, lq, lk):
+    """A row that sees nothing else has no softmax: NaN.  Beside finite scores they weigh nothing."""
+    g = np.random.default_rng([31, d])
+    c = Attend(g, lq, lk, dtype, Hq, Hkv, d)
+    c.q[..., 0] = 1.0
+    first = lk[0] // 3                                           # keys of the first sequence from here on are finite
+    c.k[:first, :, 0] = -np.inf
+    o = c.run(ctx)
+    blind = torch.arange(lq[0]) + lk[0] - lq[0] < first
+    assert o[:lq[0]][blind].isnan().all()
+    c.k[:first, :, 0] = -30000.0
+    assert torch.equal(c.run(ctx)[lq[0]:], o[lq[0]:]) and torch.equal(c.run(ctx)[:lq[0]][~blind], o[:lq[0]][~blind])
+    c.k[..., 0] = -np.inf
+    assert c.run(ctx).isnan().all()
+
+
 # ------------------------------------------------------------------------------------------------ rotary positions
 @pytest.mark.parametrize("scaling", ["none", "linear", "banded"])
 @pytest.mark.parametrize("layout", ["half", "interleaved"])
