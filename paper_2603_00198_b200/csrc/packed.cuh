@@ -33,6 +33,12 @@ __device__ __forceinline__ void packed_check(const int32_t *start, int n_seq, in
 // takes the r-th most expensive block of all sequences, so that the long ones start first and the short ones fill the gaps.
 // No list is made: the number of blocks that cost `tiles` or more is a sum over the sequences of a closed form, and a binary search over the
 // cost, then a prefix sum over the sequences, find block r.  Run by one whole warp.
+//
+// Starts that descend can name more blocks than an int counts.  A lane's count is held to MOST_BLOCKS, so that the sum over a warp stays an int, grows
+// with the cost's bound falling as the search supposes, and an index within a sequence is never negative.  Right calls never get there: with
+// rows_q * group * Hkv below 2^31 and blocks of 64 (query, head) pairs or more there are 6.6e7 at most (a group of 33 in blocks of one query).
+constexpr int MOST_BLOCKS = (1 << 26) - 1;
+
 struct PackedBlock {
     int seq, first, n;           // sequence, first query within it, queries (0: there is no block r)
     int q0, lq, k0, lk;          // the sequence's rows
@@ -73,9 +79,9 @@ __device__ __forceinline__ PackedBlock packed_block(const int32_t *q_start, cons
     // the lane's first sequence stays in registers: most calls have no more than 32
     const PackedAttnSeq own = lane < n_seq ? packed_attn_seq(q_start, k_start, lane, rows_q, rows_k, block) : PackedAttnSeq{};
     auto blocks = [&](int tiles) {
-        int n = packed_blocks_of_cost(own, block, key_tile, tiles);
+        int n = min(packed_blocks_of_cost(own, block, key_tile, tiles), MOST_BLOCKS);
         for (int s = lane + 32; s < n_seq; s += 32)
-            n += packed_blocks_of_cost(packed_attn_seq(q_start, k_start, s, rows_q, rows_k, block), block, key_tile, tiles);
+            n = min(n + packed_blocks_of_cost(packed_attn_seq(q_start, k_start, s, rows_q, rows_k, block), block, key_tile, tiles), MOST_BLOCKS);
         return (int)__reduce_add_sync(0xffffffffu, (unsigned)n);
     };
     PackedBlock b = {};
@@ -95,6 +101,7 @@ __device__ __forceinline__ PackedBlock packed_block(const int32_t *q_start, cons
             const int more = packed_blocks_of_cost(q, block, key_tile, lo + 1);
             n = packed_blocks_of_cost(q, block, key_tile, lo) - more;
             from = q.blocks - more - n;
+            n = min(n, MOST_BLOCKS);
         }
         int upto = n;
 #pragma unroll

@@ -691,6 +691,27 @@ def test_attention_scores_of_minus_infinity(ctx, dtype, Hq, Hkv, d, lq, lk):
     assert c.run(ctx).isnan().all()
 
 
+@pytest.mark.parametrize("dtype, blocks", [("f32", 1), ("bf16", 2)])
+def test_wrong_starts_that_name_more_blocks_than_an_int_counts(ctx, dtype, blocks):
+    """16384 sequences of all rows each, one behind the other, in blocks of one query or two: a count that wrapped would find no block at all, or one before
+    the first.  Nothing around the output is touched, and the next call is right."""
+    rows, group, d = blocks * ((1 << 17) + 100), 128, 8
+    q = torch.zeros(rows, group, d, dtype=TORCH[dtype], device="cuda")
+    around = torch.full((rows + 2 * 4096, group, d), UNTOUCHED, dtype=TORCH[dtype], device="cuda")
+    k = torch.zeros(3, 1, d, dtype=TORCH[dtype], device="cuda")
+    starts = torch.zeros(32769, dtype=torch.int32, device="cuda")
+    starts[1::2] = rows
+    starts[1] = 1
+    assert 16383 * -(-rows // blocks) + 1 > 2 ** 31
+    binding.str_attn_prefill_packed(ctx, q, k, k, starts, 0.1, k_start=torch.zeros_like(starts), out=around[4096:-4096])
+    with pytest.raises(binding.StrError):
+        ctx.check_status()
+    assert (around[:4096] == UNTOUCHED).all() and (around[-4096:] == UNTOUCHED).all() and (around[4096:4097] == 0).all()
+    del q, around
+    c = Attend(np.random.default_rng(35), [40, 3], [40, 90], dtype, group, 1, d)
+    c.check(c.run(ctx))
+
+
 # ------------------------------------------------------------------------------------------------ rotary positions
 @pytest.mark.parametrize("scaling", ["none", "linear", "banded"])
 @pytest.mark.parametrize("layout", ["half", "interleaved"])
