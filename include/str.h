@@ -457,6 +457,7 @@ int str_mamba2_step(str_ctx *ctx, const str_ssd_shape *s, const void *x, const f
  *   window_out  the same for what follows (of a sequence with fewer than W-1 rows, rows of `window` among them), or NULL.  Shares no memory with
  *               `window`.
  *   x_out [rows,H,p], B_out, C_out [rows,G,n] dtype, dt_out [rows,H] fp32.
+ * Outputs share no memory with any input (refused), nor with one another.
  * Errors: INVALID_ARG, UNSUPPORTED_SHAPE (other W, n_seq > 65535). */
 int str_mamba_conv_packed(str_ctx *ctx, int dtype, int n_seq, int rows, int H, int p, int n, int G, int W, const void *zxbcdt, const float *conv_w,
                           const float *conv_b, const float *dt_bias, const int32_t *seq_start, const void *window, void *x_out, void *B_out,

@@ -375,6 +375,20 @@ int check_dims(int dtype, int H, int p, int n, int G, int W, ConvDims *c) {
     return STR_OK;
 }
 
+// Does an output share memory with what other blocks may still have to read?  (The step's window in place, whose elements are read and written by one
+// thread, is its caller's to allow.)
+bool outputs_overlap(const ConvDims &c, size_t es, int n_seq, size_t rows, int W, const void *zx, const float *conv_w, const float *conv_b, const float *dt_bias,
+                     const int32_t *start, const void *window, const void *x, const void *B, const void *C, const void *dt, const void *window_out, bool in_place) {
+    const size_t wb = (size_t)n_seq * (W - 1) * c.ch * es;
+    const struct { const void *at; size_t bytes; } in[] = {{zx, rows * c.ld * es}, {window, wb}, {conv_w, (size_t)c.ch * W * sizeof(float)}, {conv_b, c.ch * sizeof(float)},
+                                                           {dt_bias, c.H * sizeof(float)}, {start, ((size_t)n_seq + 1) * sizeof(int32_t)}},
+        out[] = {{x, rows * c.d_inner * es}, {B, rows * c.gn * es}, {C, rows * c.gn * es}, {dt, rows * c.H * sizeof(float)}, {window_out, wb}};
+    for (const auto &i : in)
+        for (const auto &o : out)
+            if (kv4_overlap(i.at, i.bytes, o.at, o.bytes) && !(in_place && &i == in + 1 && &o == out + 4)) return true;
+    return false;
+}
+
 }  // namespace
 
 extern "C" int str_mamba_conv_packed(str_ctx *ctx, int dtype, int n_seq, int rows, int H, int p, int n, int G, int W, const void *zxbcdt,
@@ -386,8 +400,8 @@ extern "C" int str_mamba_conv_packed(str_ctx *ctx, int dtype, int n_seq, int row
     const int rc = check_dims(dtype, H, p, n, G, W, &c);
     if (rc != STR_OK) return rc;
     if (n_seq > 65535 || rows > (1 << 30) || (rows / 8 + 1LL + n_seq) * column_blocks(c) > INT32_MAX) return STR_ERR_UNSUPPORTED_SHAPE;
-    const size_t es = dtype_size(dtype), wb = (size_t)n_seq * (W - 1) * c.ch * es;
-    if (kv4_overlap(window, wb, window_out, wb)) return STR_ERR_INVALID_ARG;
+    if (outputs_overlap(c, dtype_size(dtype), n_seq, rows, W, zxbcdt, conv_w, conv_b, dt_bias, seq_start, window, x_out, B_out, C_out, dt_out, window_out, false))
+        return STR_ERR_INVALID_ARG;
     StrDeviceScope dev(ctx);
     if (!dev.ok) return STR_ERR_CUDA;
     StrProfScope prof_scope(ctx, STR_CAT_ELEMENTWISE, stream);
@@ -406,8 +420,9 @@ extern "C" int str_mamba_conv_step(str_ctx *ctx, int dtype, int Bz, int T, int H
     const int rc = check_dims(dtype, H, p, n, G, W, &c);
     if (rc != STR_OK) return rc;
     if ((long long)Bz * T > (1 << 30) || (long long)T * H > (1 << 30) || column_blocks(c) > 65535) return STR_ERR_UNSUPPORTED_SHAPE;
-    const size_t es = dtype_size(dtype), wb = (size_t)Bz * (W - 1) * c.ch * es;
-    if (window != window_out && kv4_overlap(window, wb, window_out, wb)) return STR_ERR_INVALID_ARG;
+    if (outputs_overlap(c, dtype_size(dtype), Bz, (size_t)Bz * T, W, zxbcdt, conv_w, conv_b, dt_bias, nullptr, window, x_out, B_out, C_out, dt_out, window_out,
+                        window == window_out))
+        return STR_ERR_INVALID_ARG;
     StrDeviceScope dev(ctx);
     if (!dev.ok) return STR_ERR_CUDA;
     StrProfScope prof_scope(ctx, STR_CAT_ELEMENTWISE, stream);

@@ -210,3 +210,20 @@ def test_a_call_before_setup_is_refused():
             "try:\n    m.setup_packed(*[0] * 7)\nexcept ValueError:\n    print('refused')\n")
     res = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
     assert res.returncode == 0 and res.stdout.split() == ["refused"] * 3, res.stderr[-3000:]
+
+
+@no_device
+@pytest.mark.parametrize("step", [False, True])
+def test_convolution_whose_outputs_share_memory_with_its_inputs(step):
+    """Rows that one block writes are another's history: every input against every output, whole and by the last element."""
+    at, rows = 1 << 40, 150 if step else 50
+    ch, cols = 4 * 16 + 2 * 2 * 8, 2 * 4 * 16 + 2 * 2 * 8 + 4
+    inputs = dict(zx=rows * cols * 2, window=3 * 3 * ch * 2, w=ch * 4 * 4, b=ch * 4, bias=4 * 4)
+    if not step:
+        inputs["start"] = 4 * 4
+    for i, size in inputs.items():
+        for o in ("x", "B", "C", "dt", "wout"):
+            in_place = step and (i, o) == ("window", "wout")
+            assert Call().conv(step, **{i: at, o: at}) == (NO_DEVICE if in_place else INVALID), (i, o)
+            assert Call().conv(step, **{i: at, o: at + size - 2}) == INVALID, (i, o)
+            assert Call().conv(step, **{i: at, o: at + size}) == NO_DEVICE, (i, o)
