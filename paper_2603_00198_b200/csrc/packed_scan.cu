@@ -367,15 +367,18 @@ extern "C" int str_mamba2_prefill_packed(str_ctx *ctx, const str_ssd_packed_shap
     if (s->n > 256 || s->n_seq > 65535 || s->H > 65535 || s->rows > (1 << 30) || s->p > (1 << 20)) return STR_ERR_UNSUPPORTED_SHAPE;
     const size_t state_bytes = (size_t)s->n_seq * s->H * s->p * s->n * sizeof(float), es = dtype_size(s->dtype);
     const size_t xb = (size_t)s->rows * s->H * s->p * es, bb = (size_t)s->rows * s->G * s->n * es;
-    if (final_state != init_state && kv4_overlap(init_state, state_bytes, final_state, state_bytes)) return STR_ERR_INVALID_ARG;
-    if (kv4_overlap(x, xb, y, xb) || kv4_overlap(B, bb, y, xb) || kv4_overlap(C, bb, y, xb)) return STR_ERR_INVALID_ARG;
-    const size_t need = str_mamba2_prefill_packed_workspace_size(s);
+    const size_t need = str_mamba2_prefill_packed_workspace_size(s), db = (size_t)s->rows * s->H * sizeof(float), hb = s->H * sizeof(float);
     if (workspace_bytes < need) return STR_ERR_WORKSPACE_TOO_SMALL;
     if (need && (!workspace || ((uintptr_t)workspace & 255) != 0)) return STR_ERR_INVALID_ARG;
-    const size_t db = (size_t)s->rows * s->H * sizeof(float);
-    const struct { const void *at; size_t bytes; } others[] = {{x, xb}, {B, bb}, {C, bb}, {y, xb}, {dt, db}, {init_state, state_bytes}, {final_state, state_bytes}};
-    for (const auto &o : others)
-        if (need && kv4_overlap(workspace, need, o.at, o.bytes)) return STR_ERR_INVALID_ARG;
+    // What is written against what is read, and against one another; a state may be updated where it lies.
+    const struct { const void *at; size_t bytes; } in[] = {{x, xb}, {dt, db}, {A, hb}, {B, bb}, {C, bb}, {D, hb}, {seq_start, ((size_t)s->n_seq + 1) * sizeof(int32_t)},
+                                                           {init_state, state_bytes}},
+        out[] = {{y, xb}, {final_state, state_bytes}, {workspace, need}};
+    for (const auto &o : out)
+        for (const auto &i : in)
+            if (kv4_overlap(i.at, i.bytes, o.at, o.bytes) && !(&i == in + 7 && &o == out + 1 && init_state == final_state)) return STR_ERR_INVALID_ARG;
+    for (int i = 0; i < 3; ++i)
+        if (kv4_overlap(out[i].at, out[i].bytes, out[(i + 1) % 3].at, out[(i + 1) % 3].bytes)) return STR_ERR_INVALID_ARG;
     StrDeviceScope dev(ctx);
     if (!dev.ok) return STR_ERR_CUDA;
     StrProfScope prof_scope(ctx, STR_CAT_SSD, stream);

@@ -227,3 +227,16 @@ def test_convolution_whose_outputs_share_memory_with_its_inputs(step):
             assert Call().conv(step, **{i: at, o: at}) == (NO_DEVICE if in_place else INVALID), (i, o)
             assert Call().conv(step, **{i: at, o: at + size - 2}) == INVALID, (i, o)
             assert Call().conv(step, **{i: at, o: at + size}) == NO_DEVICE, (i, o)
+
+
+@no_device
+def test_scan_whose_outputs_share_memory():
+    """y and the final state against every input and against each other, whole and by the last element."""
+    at = 1 << 40
+    x, B, state, head = 50 * 4 * 16 * 2, 50 * 2 * 8 * 2, 3 * 4 * 16 * 8 * 4, 4 * 4
+    inputs = dict(x=x, dt=50 * 4 * 4, A=head, B=B, C=B, D=head, start=4 * 4, init=state)
+    for o in ("y", "final"):
+        for i, size in (*inputs.items(), *((("y", x),) if o == "final" else ())):
+            same = (i, o) == ("init", "final")
+            assert Call().scan(**{i: at, o: at}) == (NO_DEVICE if same else INVALID), (i, o)
+            assert Call().scan(**{i: at, o: at + size - 2}) == INVALID and Call().scan(**{i: at, o: at + size}) == NO_DEVICE, (i, o)
