@@ -471,6 +471,8 @@ int str_mamba_conv_step(str_ctx *ctx, int dtype, int Bz, int T, int H, int p, in
 /* The scan (1) on packed sequences: x, y [rows,H,p], dt [rows,H], B, C [rows,G,n], A, D as in (1); init_state [n_seq,H,p,n] fp32 or NULL (zeros);
  * final_state the same shape or NULL, may be init_state itself.  An empty sequence's final state is its initial one.
  * Else what is written (y, final_state, the workspace) shares no memory with what is read, nor with one another.
+ * An x that is not finite leaves the tokens before it, the other elements of its head and the other heads as they would be without it; its own element of
+ * the state and of y is not finite from there on (infinite as the recurrence has it, or NaN).
  * final_state is accurate to fp32 arithmetic whatever the dtype.
  * Workspace: size from the query (0 unless long sequences have few heads), 256-byte aligned; calls that may run at the same time, two captured
  * graphs among them, need their own.

@@ -160,7 +160,7 @@ scan_packed_kernel(int n_seq, int rows, int H, int p, int n, int G, const T *__r
                     const float2 part = *(const float2 *)(ys + e * PARTS);
                     sum = part.x + part.y;
                 }
-                if (t < m && i0 + i < p) stf(y + ((size_t)(tb + t) * H + h) * p + i0 + i, fmaf(Dh, xs[e], sum));
+                if (t < m && i0 + i < p) stf(y + ((size_t)(tb + t) * H + h) * p + i0 + i, Dskip ? fmaf(Dh, xs[e], sum) : sum);
             }
             __syncthreads();
         }

@@ -172,7 +172,7 @@ __device__ __forceinline__ void w_piece_below(const uint32_t (&v)[16], uint32_t 
 }
 
 // The recurrence of one head of one sequence token by token, in fp32, by the whole CTA: eight lanes a row of the state (one of p).
-__device__ __noinline__ void scan_rows(const __nv_bfloat16 *x, const float *dt, float A, const __nv_bfloat16 *B, const __nv_bfloat16 *C, float D, const float *init,
+__device__ __noinline__ void scan_rows(const __nv_bfloat16 *x, const float *dt, float A, const __nv_bfloat16 *B, const __nv_bfloat16 *C, const float *D, const float *init,
                                        __nv_bfloat16 *y, float *fin, int T, int H, int G, int p, int n) {
     const int r = threadIdx.x / 8, l = threadIdx.x % 8;
     float S[16];
@@ -189,7 +189,7 @@ __device__ __noinline__ void scan_rows(const __nv_bfloat16 *x, const float *dt, 
             }
 #pragma unroll
         for (int o = 1; o < 8; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        if (y && l == 0 && r < p) stf(y + (size_t)t * H * p + r, D != 0.f ? fmaf(D, xv, sum) : sum);
+        if (y && l == 0 && r < p) stf(y + (size_t)t * H * p + r, D ? fmaf(*D, xv, sum) : sum);
     }
 #pragma unroll
     for (int i = 0; i < 16; ++i)
@@ -713,7 +713,7 @@ scan_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_c
     __syncthreads();
     if (warp == 13) { tc::tc_fence_after(); tc::tmem_dealloc(tmem, 512); }
     if (found[0])
-        scan_rows(x + ((size_t)row0 * H + h) * p, dt + (size_t)row0 * H + h, A[h], B + ((size_t)row0 * G + g) * n, C + ((size_t)row0 * G + g) * n, skip, init,
+        scan_rows(x + ((size_t)row0 * H + h) * p, dt + (size_t)row0 * H + h, A[h], B + ((size_t)row0 * G + g) * n, C + ((size_t)row0 * G + g) * n, Dskip ? Dskip + h : nullptr, init,
                   y ? y + ((size_t)row0 * H + h) * p : nullptr, fin, Tlen, H, G, p, n);
 }
 

@@ -414,6 +414,22 @@ def test_wrong_starts_of_segments(ctx, starts):
         c.check(c.run(ctx))
 
 
+@pytest.mark.parametrize("dtype, dims, lens", [("f32", (2, 32, 16, 1), [40]), ("f32", (2, 64, 128, 1), [40]), ("bf16", (2, 64, 128, 1), [20]), ("bf16", (2, 80, 32, 1), [150]),
+                                               ("bf16", (2, 64, 128, 1), [200])], ids=str)
+def test_scan_of_an_infinite_value_with_and_without_skip(ctx, dtype, dims, lens):
+    """Positive B and C: the state's row is infinite from the value on, and y with it.  A skip of zero multiplies the value, no skip does not."""
+    g = np.random.default_rng(32)
+    c = Scan(g, lens, dtype, *dims, False, True)
+    c.B, c.C, c.state = np.abs(c.B) + 1.0, np.abs(c.C) + 1.0, np.abs(c.state)
+    c.B, c.C = inputs.to_grid(c.B, dtype), inputs.to_grid(c.C, dtype)
+    c.x[11, 1, 7] = np.inf
+    y, S = (_f64(t) for t in c.run(ctx))
+    assert (y[11:, 1, 7] == np.inf).all() and np.isfinite(y[:11]).all() and (S[0, 1, 7] == np.inf).all()
+    c.D = np.zeros(dims[0], dtype=np.float32)
+    z, _ = (_f64(t) for t in c.run(ctx))
+    assert np.isnan(z[11, 1, 7]) and (z[12:, 1, 7] == np.inf).all() and np.array_equal(np.delete(z[:, 1], 7, 1), np.delete(y[:, 1], 7, 1))
+
+
 # ------------------------------------------------------------------------------------------------ attention
 class Attend:
     def __init__(self, g, lq, lk, dtype, Hq, Hkv, d, first=(0, 0), tail=0, gain=1.0):
