@@ -282,6 +282,9 @@ scan_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_c
     if (warp == 12) {
         // ------------------------------------------------------------------ decay vectors
         const float Ah2 = A[h] * LOG2E;
+        // A token that fades what lies before it by 2^-256 leaves nothing of it, and counts as no more: the chunk's sums stay above -2^15, so that their
+        // differences are right to 2^-9 however fast the decay (at -2^21 the weight of a token's own x would be 6 % off).
+        const float longest = Ah2 < 0.f ? -256.f / Ah2 : INFINITY;
         const float *dtb = dt + (size_t)row0 * H + h;
         bool ok = true;
         // Lane 0 is the TMA producer too.  The operands of chunk c go into the slots of chunk c-2 (B, C: ring of 2) and chunk c-3 (X: ring of 3)
@@ -319,10 +322,12 @@ scan_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_c
                 dn[i] = t < Tlen ? __ldg(dtb + (size_t)t * H) : 0.f;
             }
             if (!tc::mbar_wait(bars + B_DECE + d, ((c >> 2) & 1) ^ 1, abort_flag)) { ok = false; break; }
-            float l[4];
-            l[0] = dv[0] * Ah2;
+            float l[4], dl[4];
 #pragma unroll
-            for (int i = 1; i < 4; ++i) l[i] = fmaf(dv[i], Ah2, l[i - 1]);
+            for (int i = 0; i < 4; ++i) dl[i] = dv[i] > longest ? longest : dv[i];          // (NaN stays)
+            l[0] = dl[0] * Ah2;
+#pragma unroll
+            for (int i = 1; i < 4; ++i) l[i] = fmaf(dl[i], Ah2, l[i - 1]);
             float incl = l[3];
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -337,8 +342,8 @@ scan_packed_tc_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_c
             // sums over what comes behind a token: what l_end - l_j is, without the difference of two large numbers
             float tail[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int i = 2; i >= 0; --i) tail[i] = fmaf(dv[i + 1], Ah2, tail[i + 1]);
-            float rev = fmaf(dv[0], Ah2, tail[0]);                    // the lane's four tokens together
+            for (int i = 2; i >= 0; --i) tail[i] = fmaf(dl[i + 1], Ah2, tail[i + 1]);
+            float rev = fmaf(dl[0], Ah2, tail[0]);                    // the lane's four tokens together
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
                 const float v = __shfl_down_sync(0xffffffffu, rev, o);

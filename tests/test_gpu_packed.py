@@ -430,6 +430,19 @@ def test_scan_of_an_infinite_value_with_and_without_skip(ctx, dtype, dims, lens)
     assert np.isnan(z[11, 1, 7]) and (z[12:, 1, 7] == np.inf).all() and np.array_equal(np.delete(z[:, 1], 7, 1), np.delete(y[:, 1], 7, 1))
 
 
+@pytest.mark.parametrize("decay", [1e5, 1e6, 1e30])
+@pytest.mark.parametrize("dims, lens", [((4, 64, 128, 2), [300, 77]), ((3, 32, 64, 3), [40, 128]), ((2, 64, 128, 1), [3000])], ids=str)
+def test_scan_whose_tokens_fade_all_before_them(ctx, dims, lens, decay):
+    """Decays beyond what a sum of logarithms in fp32 could keep apart: y is each token's own term, with the bound of any other scan."""
+    g = np.random.default_rng(33)
+    c = Scan(g, lens, "bf16", *dims, True, True)
+    c.A[:] = -decay
+    c.check(c.run(ctx))
+    c.A[1:] = -0.01                                              # heads side by side, and tokens within one
+    c.dt[::5] = 1e-12
+    c.check(c.run(ctx))
+
+
 # ------------------------------------------------------------------------------------------------ attention
 class Attend:
     def __init__(self, g, lq, lk, dtype, Hq, Hkv, d, first=(0, 0), tail=0, gain=1.0):
