@@ -473,7 +473,8 @@ int str_mamba_conv_step(str_ctx *ctx, int dtype, int Bz, int T, int H, int p, in
  * Else what is written (y, final_state, the workspace) shares no memory with what is read, nor with one another.
  * An x that is not finite leaves the tokens before it, the other elements of its head and the other heads as they would be without it; its own element of
  * the state and of y is not finite from there on (infinite as the recurrence has it, or NaN).
- * final_state is accurate to fp32 arithmetic whatever the dtype.
+ * final_state is an fp32 result whatever the dtype: for bf16 storage its terms are right to 2^-20 (to 2^-24 where what follows fades them by less than
+ * 2^-4), and their sum to what a sum in fp32 loses.
  * Workspace: size from the query (0 unless long sequences have few heads), 256-byte aligned; calls that may run at the same time, two captured
  * graphs among them, need their own.
  * Errors: INVALID_ARG, UNSUPPORTED_SHAPE (n > 256, n_seq > 65535), WORKSPACE_TOO_SMALL. */

@@ -443,6 +443,29 @@ def test_scan_whose_tokens_fade_all_before_them(ctx, dims, lens, decay):
     c.check(c.run(ctx))
 
 
+@pytest.mark.parametrize("dims, lens", [((148, 64, 16, 1), [512, 0, 200]), ((2, 64, 128, 1), [1500])], ids=str)
+def test_final_states_that_nothing_fades_take_all_pieces_in_every_chunk(ctx, dims, lens):
+    """No decay, and of a chunk's tokens four equal ones that count: rounding errors of a term's pieces add up instead of averaging out, and few products are cut
+    off where they meet the sum.  Two pieces alone would be up to 1.4e-5 of the sum off (worked out on the host below).  With the third the terms are right to
+    2^-24; a chunk's 12 products and 24 steps of the sum lose 2^-23 of it each at most, the sum over the chunks 2^-24 a chunk."""
+    g = np.random.default_rng(36)
+    c = Scan(g, lens, "bf16", *dims, False, False)
+    assert _segmented(c) == (len(lens) == 1)
+    c.x[:], c.B[:], c.A[:] = inputs.to_grid(g.standard_normal(64), "bf16"), 1.0, 0.0
+    dt = (0.001 * 100.0 ** g.random(dims[0])).astype(np.float32)
+    c.dt[:] = np.where((np.arange(len(c.dt)) % 32 == 5)[:, None], dt, np.float32(1e-30))
+    bound = 36 * 2.0 ** -23 + 13 * 2.0 ** -24
+    bf = lambda a: inputs.to_grid(np.asarray(a, dtype=np.float64), "bf16").astype(np.float64)  # noqa: E731
+    x, w = c.x[0].astype(np.float64), dt.astype(np.float64)[:, None]
+    w1 = bf(w)
+    high = bf(x * w1)
+    two = high + bf(x * bf(w - w1) + (x * w1 - high))
+    assert (np.abs(two - x * w) > 2 * bound * np.abs(x * w)).any()
+    _, S = c.run(ctx)
+    _, _, want, mag = packed.scan(c.x, c.dt, c.A, c.B, c.C, None, c.starts, None)
+    assert (np.abs(_f64(S) - want) <= bound * mag).all()
+
+
 # ------------------------------------------------------------------------------------------------ attention
 class Attend:
     def __init__(self, g, lq, lk, dtype, Hq, Hkv, d, first=(0, 0), tail=0, gain=1.0):
