@@ -240,3 +240,12 @@ def test_scan_whose_outputs_share_memory():
             same = (i, o) == ("init", "final")
             assert Call().scan(**{i: at, o: at}) == (NO_DEVICE if same else INVALID), (i, o)
             assert Call().scan(**{i: at, o: at + size - 2}) == INVALID and Call().scan(**{i: at, o: at + size}) == NO_DEVICE, (i, o)
+
+
+@no_device
+def test_rotary_descriptions_beyond_what_an_angle_or_an_output_holds():
+    """An amplitude that fp32 has not, and frequencies whose quarter turns a 64-bit number does not count any more."""
+    for bad in (dict(amplitude=1e39), dict(amplitude=-1e300), dict(theta=1e-300), dict(scaling=1, factor=1e-200), dict(scaling=1, factor=1e-8), dict(scaling=2, factor=5e-324)):
+        assert Call().rope(**bad) == INVALID, bad
+    for good in (dict(amplitude=-3e38), dict(theta=1e300), dict(theta=1e-6), dict(scaling=1, factor=1e-6), dict(scaling=2, factor=1e300)):
+        assert Call().rope(**good) == NO_DEVICE, good
