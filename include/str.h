@@ -508,7 +508,7 @@ int str_attn_prefill_packed(str_ctx *ctx, const str_attn_packed_shape *s, const 
  *            frequency, slow ones are stretched, those between are blended
  *   amplitude  multiplies what is turned (1: a rotation)
  * qkv device [rows, (Hq+2Hkv)*d]; positions device [rows] int32, any values; q_out [rows,Hq,d], k_out, v_out [rows,Hkv,d].  Angles are formed
- * in 64 bits.  Outputs share no memory with qkv.  Errors: INVALID_ARG (also an amplitude beyond fp32, or f_i of 2^20 turns a position
+ * in 64 bits.  Outputs share no memory with qkv, the positions or one another.  Errors: INVALID_ARG (also an amplitude beyond fp32, or f_i of 2^20 turns a position
  * and more), UNSUPPORTED_SHAPE (rot_dim > 256; odd d with INTERLEAVED). */
 enum { STR_ROPE_HALF = 0, STR_ROPE_INTERLEAVED = 1 };
 enum { STR_ROPE_NONE = 0, STR_ROPE_LINEAR = 1, STR_ROPE_BANDED = 2 };

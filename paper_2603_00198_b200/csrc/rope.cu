@@ -157,8 +157,11 @@ extern "C" int str_rope_split_ex(str_ctx *ctx, const str_rope_desc *r, int dtype
     if (r->rot_dim > 2 * MAX_PAIRS || rows > (1 << 30) || ((long long)Hq + 2LL * Hkv) * d > (1 << 28)) return STR_ERR_UNSUPPORTED_SHAPE;
     if (d % 2 != 0 && r->layout == STR_ROPE_INTERLEAVED) return STR_ERR_UNSUPPORTED_SHAPE;
     const size_t row = dtype_size(dtype) * d, in = row * (Hq + 2 * Hkv) * rows;
-    if (kv4_overlap(qkv, in, q_out, row * Hq * rows) || kv4_overlap(qkv, in, k_out, row * Hkv * rows) || kv4_overlap(qkv, in, v_out, row * Hkv * rows))
-        return STR_ERR_INVALID_ARG;
+    const struct { const void *at; size_t bytes; } out[] = {{q_out, row * Hq * rows}, {k_out, row * Hkv * rows}, {v_out, row * Hkv * rows}};
+    for (int i = 0; i < 3; ++i)
+        if (kv4_overlap(qkv, in, out[i].at, out[i].bytes) || kv4_overlap(positions, sizeof(int32_t) * rows, out[i].at, out[i].bytes) ||
+            kv4_overlap(out[i].at, out[i].bytes, out[(i + 1) % 3].at, out[(i + 1) % 3].bytes))
+            return STR_ERR_INVALID_ARG;
     RopeTable tab = {};
     for (int i = 0; i < r->rot_dim / 2; ++i) {
         double f = pow(r->theta, -2.0 * i / r->rot_dim) / 6.283185307179586476925;

@@ -249,3 +249,13 @@ def test_rotary_descriptions_beyond_what_an_angle_or_an_output_holds():
         assert Call().rope(**bad) == INVALID, bad
     for good in (dict(amplitude=-3e38), dict(theta=1e300), dict(theta=1e-6), dict(scaling=1, factor=1e-6), dict(scaling=2, factor=1e300)):
         assert Call().rope(**good) == NO_DEVICE, good
+
+
+@no_device
+def test_rotary_outputs_share_no_memory():
+    at, q, k = 1 << 40, 9 * 4 * 64 * 2, 9 * 2 * 64 * 2
+    for i, size in (("qkv", 9 * 8 * 64 * 2), ("pos", 9 * 4), ("q", q), ("k", k), ("v", k)):
+        for o in ("q", "k", "v"):
+            if i != o:
+                assert Call().rope(at={i: at, o: at}) == INVALID and Call().rope(at={i: at, o: at + size - 2}) == INVALID, (i, o)
+                assert Call().rope(at={i: at, o: at + size}) == NO_DEVICE, (i, o)
