@@ -490,6 +490,7 @@ int str_mamba2_prefill_packed(str_ctx *ctx, const str_ssd_packed_shape *s, const
  * queries are the newest lq of lk tokens.  A query without any key to see (lk < lq) gives zeros.
  *   q, o device [rows_q,Hq,d]; k, v device [rows_k,Hkv,d]; q_start, k_start device int32 [n_seq+1]; k_start NULL: the keys' rows are the queries'.
  * Keys that a query does not see have no influence on it, infinities and NaN among them.  softmax_scale > 0.
+ * The output and the workspace share no memory with an input or each other.
  * Workspace: size from the query (0 unless a few queries meet many keys), 256-byte aligned; calls that may run at the same time, two captured
  * graphs among them, need their own.
  * Errors: INVALID_ARG, UNSUPPORTED_SHAPE (d > 128, more than 128 query heads per key head, n_seq > 32768), WORKSPACE_TOO_SMALL. */

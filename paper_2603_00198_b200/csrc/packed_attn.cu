@@ -280,12 +280,14 @@ extern "C" int str_attn_prefill_packed(str_ctx *ctx, const str_attn_packed_shape
         ((long long)s->rows_q * group + s->n_seq) * s->Hkv > INT32_MAX)
         return STR_ERR_UNSUPPORTED_SHAPE;
     const size_t es = dtype_size(s->dtype), qb = es * s->rows_q * s->Hq * s->d, kb = es * s->rows_k * s->Hkv * s->d;
-    if (kv4_overlap(q, qb, o, qb) || kv4_overlap(k, kb, o, qb) || kv4_overlap(v, kb, o, qb)) return STR_ERR_INVALID_ARG;
-    const size_t need = str_attn_prefill_packed_workspace_size(s);
+    const size_t need = str_attn_prefill_packed_workspace_size(s), sb = ((size_t)s->n_seq + 1) * sizeof(int32_t);
+    const struct { const void *at; size_t bytes; } in[] = {{q, qb}, {k, kb}, {v, kb}, {q_start, sb}, {k_start, sb}};
+    for (const auto &i : in)
+        if (kv4_overlap(i.at, i.bytes, o, qb)) return STR_ERR_INVALID_ARG;
     if (workspace_bytes < need) return STR_ERR_WORKSPACE_TOO_SMALL;
-    if (need && (!workspace || ((uintptr_t)workspace & 255) != 0 || kv4_overlap(workspace, need, o, qb) || kv4_overlap(workspace, need, q, qb) ||
-                 kv4_overlap(workspace, need, k, kb) || kv4_overlap(workspace, need, v, kb)))
-        return STR_ERR_INVALID_ARG;
+    if (need && (!workspace || ((uintptr_t)workspace & 255) != 0 || kv4_overlap(workspace, need, o, qb))) return STR_ERR_INVALID_ARG;
+    for (const auto &i : in)
+        if (kv4_overlap(i.at, i.bytes, workspace, need)) return STR_ERR_INVALID_ARG;
     StrDeviceScope dev(ctx);
     if (!dev.ok) return STR_ERR_CUDA;
     StrProfScope prof_scope(ctx, STR_CAT_ATTN_FWD, stream);

@@ -259,3 +259,17 @@ def test_rotary_outputs_share_no_memory():
             if i != o:
                 assert Call().rope(at={i: at, o: at}) == INVALID and Call().rope(at={i: at, o: at + size - 2}) == INVALID, (i, o)
                 assert Call().rope(at={i: at, o: at + size}) == NO_DEVICE, (i, o)
+
+
+@no_device
+def test_attention_starts_that_share_memory_with_what_is_written():
+    at = 1 << 40
+    for name in ("qs", "ks"):
+        assert Call().attn(**{name: at, "o": at}) == INVALID and Call().attn(**{name: at, "o": at + 12}) == INVALID and Call().attn(**{name: at, "o": at + 16}) == NO_DEVICE, name
+    c, s = Call(), binding.AttnPackedShape(1, 10, 5000, 4, 2, 64, 1)
+    need = binding.lib().str_attn_prefill_packed_workspace_size(ctypes.addressof(s))
+    for n in (3, 4):                                       # the starts' places among the arguments, in the workspace's last 256 bytes and behind it
+        for shift, want in ((-256, INVALID), (0, NO_DEVICE)):
+            p = [c.buffer() for _ in range(5)]
+            p[n] = at + need + shift
+            assert binding.lib().str_attn_prefill_packed(ctypes.addressof(c.ctx), ctypes.addressof(s), *p, 0.1, c.buffer(), at, need, None) == want, (n, shift)
