@@ -606,7 +606,8 @@ class Rope:
 
 
 def str_rope_split_ex(ctx, rope, qkv, positions, Hq, Hkv, d):
-    """(q [rows,Hq,d], k, v [rows,Hkv,d]) of qkv [rows,(Hq+2Hkv)*d], q and k turned as the Rope says at positions [rows] int32."""
+    """(q [rows,Hq,d], k, v [rows,Hkv,d]) of qkv [rows,(Hq+2Hkv)*d], q and k turned as the Rope says at positions [rows] int32.  Outputs of up to
+    2 MiB together are slices of one allocation (``clone`` one that is to outlive the others or be resized); larger ones have their own."""
     return _marshal().rope(ctx.address, ctx.device, rope.desc_ref, qkv, positions, Hq, Hkv, d)
 
 
@@ -620,7 +621,7 @@ def str_mamba_conv_packed(ctx, zxbcdt, conv_w, conv_b, dt_bias, seq_start, H, p,
 
 def str_mamba_conv_step(ctx, zxbcdt, conv_w, conv_b, dt_bias, window, Bz, T, H, p, n, G, window_out=None):
     """The pre-scan step of T tokens each of Bz sequences, zxbcdt [Bz*T, ...]; returns (x [Bz,T,H,p], B, C [Bz,T,G,n], dt [Bz,T,H]).  Without
-    ``window_out`` the window [Bz, W-1, H*p + 2*G*n] is updated in place."""
+    ``window_out`` the window [Bz, W-1, H*p + 2*G*n] is updated in place.  Outputs of up to 2 MiB together are slices of one allocation."""
     return _marshal().conv_step(ctx.address, ctx.device, zxbcdt, conv_w, conv_b, dt_bias, H, p, n, G, window, Bz, T, window if window_out is None else window_out)
 
 

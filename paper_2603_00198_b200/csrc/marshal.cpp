@@ -97,8 +97,11 @@ at::Tensor empty(at::IntArrayRef shape, at::ScalarType dtype, int device) {
     return at::empty(shape, at::TensorOptions().dtype(dtype).device(at::kCUDA, device));
 }
 
-// Several outputs of one call in one allocation, 256 bytes apart: an allocation costs 0.6 us, as much as the rest of a small call's marshalling.
+// Several small outputs of one call in one allocation, 256 bytes apart: an allocation costs 0.6 us, as much as the rest of a small call's marshalling.
+// They share a storage then, as the slices of a tensor do.  Beyond SHARED bytes together (kernels of 5 us and more) each has its own, so
+// that keeping one does not keep the others' memory.
 struct Parts {
+    static constexpr int64_t SHARED = 2 << 20;
     struct Part {
         at::IntArrayRef shape;
         at::ScalarType dtype;
@@ -112,6 +115,10 @@ struct Parts {
     static void make(std::initializer_list<Part> parts, int device, at::Tensor *out) {
         int64_t total = 0, at = 0;
         for (const Part &p : parts) total += bytes(p);
+        if (total > SHARED) {
+            for (const Part &p : parts) *out++ = empty(p.shape, p.dtype, device);
+            return;
+        }
         const at::Tensor base = empty({total}, at::kByte, device);
         for (const Part &p : parts) {
             *out = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(base.storage()), base.key_set(), c10::scalarTypeToTypeMeta(p.dtype));

@@ -814,6 +814,17 @@ def test_rotary_at_addresses_that_allow_no_vectors(ctx, off):
             assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
+def test_large_outputs_have_memory_of_their_own(ctx):
+    """Keeping the keys of a prompt does not keep its queries."""
+    qkv, pos = torch.randn(3000, 8 * 64, device="cuda").bfloat16(), torch.arange(3000, dtype=torch.int32, device="cuda")
+    q, k, v = binding.str_rope_split_ex(ctx, binding.Rope(1e4, 64), qkv, pos, 4, 2, 64)
+    g = np.random.default_rng(34)
+    c = Conv(g, [1] * 5000, "bf16", 8, 16, 32, 2, 4)
+    step = binding.str_mamba_conv_step(ctx, dev(c.zx, "bf16"), *c.on, dev(c.window, "bf16"), 5000, 1, *c.dims)
+    for t in (q, k, v, *step):
+        assert t.untyped_storage().nbytes() == t.numel() * t.element_size() and t.storage_offset() == 0
+
+
 # ------------------------------------------------------------------------------------------------ together, streams, graphs, wrong starts
 def _layer(g, rows):
     H, p, n, G, W = 4, 64, 128, 2, 4
