@@ -20,8 +20,8 @@
 // Warps: 0-3 softmax of tile 0, 4-7 softmax of tile 1 (warp w may touch TMEM lanes 32 (w % 4)...), 8 TMA producer (Q once, then a 2-slot ring for K and
 // one for V), 9 MMA issuer, 10 the guard that zeroes and looks through tiles of V.
 //
-// Measured: one prompt of 16512 rows, 32 / 8 heads of 128: 1.82 to 1.88 ms, 1190 to 1230 TFLOP/s, 0.72 of the measured burst figure and 0.86 of the sustained
-// one; twelve turns of 8200 rows over 24800 keys 222 us; 300 rows over 4396 keys 43 us, 74 without sharing the walk.  A key tile takes 3600 clocks for 2048 of
+// Measured: one prompt of 16512 rows, 32 / 8 heads of 128: 1.80 to 1.85 ms on a cool card, 1207 to 1240 TFLOP/s, 0.72 to 0.74 of the measured burst figure; again and again, under the
+// power cap, 2.09 to 2.15 ms, 0.74 to 0.76 of the sustained one; twelve turns of 8200 rows over 24800 keys 191 to 229 us; 300 rows over 4396 keys 44 us, 74 without sharing the walk.  A key tile takes 3600 clocks for 2048 of
 // products: after its last weights a row tile waits 1200 to 1500 for the second half of P V, the next S and the barriers between them, in
 // which the other tile's softmax runs; the special-function unit (2048 clocks for all exponentials) is the next limit, hence one pair in six on
 // the FMA pipe.  Tried and not kept: steps of 64 keys with two S buffers a tile, which takes the wait away but makes every S product re-read Q for half the

@@ -355,7 +355,7 @@ void dispatch_width(const ConvCall &k, int W, bool step, cudaStream_t st) {
     else if (W == 3) launch<T, VEC, 3>(k, step, st);
     else launch<T, VEC, 4>(k, step, st);
 }
-// Sixteen bytes of channels a thread where rows, columns and pointers allow it, else one channel.
+// Four channels a thread (16 bytes of fp32, 8 of bf16) where rows, columns and pointers allow it, else one channel.
 template <typename T>
 void dispatch_vec(const ConvCall &k, int W, bool step, cudaStream_t st) {
     constexpr int VEC = 4;

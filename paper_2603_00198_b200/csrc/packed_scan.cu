@@ -11,7 +11,7 @@
 //
 // Bound by the reading of b and c from shared memory: two rows a lane, so that a vector read serves eight fused operations (one row a lane: 1.88 ms where
 // two take 1.22, 25.8 TFLOP/s, 5000 rows, 128 heads of 64 x 128), and several tokens' reads before the first one's output is stored.  Few sequences are
-// bound by the chain of tokens, 77 ns each, whence the segments below (five turns of 1237 rows, the longest 547, 24 heads of 32 x 20: 30 us, whole 45).
+// bound by the chain of tokens, 77 ns each, whence the segments below (five turns of 1237 rows, the longest 547, 24 heads of 32 x 20: 31 to 34 us, whole 45).
 #include <algorithm>
 
 #include "dispatch.cuh"

@@ -20,8 +20,8 @@
 // dS -> state (and its copy) -> Xs -> dS; the state warps, who wait for dS anyhow, form Xs, so that no other role's work lies on it (formed by
 // the epilogue's warps, in front of each epilogue, it took 4400 clocks a chunk).
 //
-// Measured: eight sequences of 24576 rows, 128 heads: 451 us, 2.2 TB/s, 0.33 of the measured copy bandwidth; one sequence of 32896 rows 609 us, 2.37 us
-// (4300 clocks) a chunk; a turn of 300 rows 16 us.  Bound by shared memory: of a chunk's clocks its 128 bytes a clock are busy for about 3500 (operands of
+// Measured: eight sequences of 24576 rows, 128 heads: 451 us, 2.2 TB/s, 0.33 of the measured copy bandwidth (497 to 508 with inputs that change from call to call); one sequence of 32896
+// rows 606 us, 2.36 us (4300 clocks) a chunk; a turn of 300 rows 16 us.  With decays so slow that every chunk takes the third piece 689 and 1020 us.  Bound by shared memory: of a chunk's clocks its 128 bytes a clock are busy for about 3500 (operands of
 // the products 1750, tiles coming in 640, the warps' own accesses 1130), and the stores of y, 32 rows a warp, hold the load/store units for 800 more.
 // The two pieces of x cost 0.5 us a chunk over one.  The loops are rolled wherever registers allow: with the pieces of W unrolled the instruction cache
 // no longer held the roles, and the same work took 527 us.
